@@ -309,6 +309,130 @@ int qg_gemm_autotune(const void *const *packed_sets /* HOST */, int sets, int64_
  * i >= 1: microseconds per call, -1 = dropped by the price, -2 = not a plan of its own (or the layout has no such kernel). */
 int qg_gemm_autotune_report(float *us /* HOST */, int capacity, int *timed, int *dropped);
 
+/* ---------------------------------------------------------------------------------------------
+ * Between the products of a token's step: the norm in front of them, the paged key-value cache
+ * they fill, the attention that reads it, and the bookkeeping of its pages.  The conventions
+ * above hold; an empty batch (no rows, no tokens, no sequences) is QG_OK and enqueues nothing.
+ * Arithmetic is fp32; a result is rounded once, to nearest even, where it is stored.
+ *
+ * 8-bit values (QG_E4M3: sign, 4 exponent bits of bias 7, 3 of significand, no infinities, the type torch
+ * calls float8_e4m3fn) come with fp32 scales: over the values that share one, s = max|y| / 448, or 1 where all are
+ * zero, and what is stored is y / s; it stands for code * s.  A NaN or an infinity among them makes s and their codes NaN.
+ * --------------------------------------------------------------------------------------------- */
+typedef enum { QG_F32 = 0, QG_BF16 = 1, QG_F16 = 2, QG_E4M3 = 3 } qg_type;
+
+/* Root-mean-square norm of rows with the residual's addition:
+ *   h = x + residual (h = x without one),   y[k] = h[k] / sqrt(mean(h^2) + eps) * weight[k]
+ * h is stored rounded to `type`; y is computed from h as it is before that rounding. */
+typedef struct qg_norm_desc {
+    const void *x;         /* [rows][K] of `type`, rows x_stride elements apart */
+    const void *residual;  /* the same, rows residual_stride apart; NULL: none */
+    const void *weight;    /* [K] of weight_type */
+    void *h;               /* [rows][K] of `type`, may be x or residual itself where its rows lie K apart; NULL if residual is, or if not wanted */
+    void *y;               /* [rows][K] of y_type */
+    float *scales;         /* [rows][K / group], y_type QG_E4M3 only */
+    int64_t rows, K, x_stride, residual_stride;
+    int type, weight_type; /* QG_F32, QG_BF16 or QG_F16 */
+    int y_type;            /* any */
+    int group;             /* values that share a scale (divides K), 0: the whole row; 0 unless y_type is QG_E4M3 */
+    float eps;
+} qg_norm_desc;
+int qg_rms_norm(const qg_norm_desc *d /* HOST */, void *stream);
+
+/* A cache of keys and values in pages of `page` tokens (a power of two, 16 ... 4096).  Token i of sequence b is cell
+ * i % page of page tables[b][i / page].  Keys (and values) of a page lie together by head, so that attention, which
+ * works head by head, reads runs of page * head_dim values. */
+typedef struct qg_kv_cache {
+    void *k, *v;              /* [pages][kv_heads][page][head_dim] of `type` */
+    float *k_scale, *v_scale; /* [pages][kv_heads][page], QG_E4M3 only: a scale for each token and head */
+    const int32_t *tables;    /* [rows][max_pages], rows table_stride apart; entries past a sequence's end are never used */
+    int64_t table_stride, pages;
+    int rows, max_pages, kv_heads, page;
+    int head_dim;             /* a multiple of 8, 8 ... 256 */
+    int type;                 /* QG_BF16, QG_F16 or QG_E4M3 */
+} qg_kv_cache;
+
+/* Rotates q and k of new tokens by their positions and stores k and v in the cache.
+ * Over the first rope_dim elements of each head (even; 0: no rotation) pairs turn by the position's angles,
+ *   (a, b) -> (a cos - b sin, b cos + a sin),
+ * the pair of angle j being elements j and j + rope_dim / 2, or 2 j and 2 j + 1 if interleaved.  A token whose row
+ * or position has no page in the table (row or position < 0 or past the table, a page id that is none, a
+ * position past cos_sin) is padding: nothing is stored for it, and its q comes out zero. */
+typedef struct qg_append_desc {
+    qg_kv_cache cache;
+    const int32_t *rows;       /* [tokens]: each token's row of the tables */
+    const int32_t *positions;  /* [tokens] */
+    const void *q, *k, *v;     /* [tokens][heads][head_dim] (q), [tokens][kv_heads][head_dim] of `type`, tokens *_stride apart;
+                                  q may be NULL (heads 0).  16-byte aligned, strides multiples of 8 */
+    void *q_out;               /* [tokens][heads][head_dim] of `type` */
+    const float *cos_sin;      /* [cos_sin_rows][rope_dim]: rope_dim / 2 cosines, then as many sines; NULL if rope_dim is 0 */
+    int64_t tokens, q_stride, k_stride, v_stride, cos_sin_rows;
+    int type, heads, rope_dim, interleaved;
+} qg_append_desc;
+int qg_kv_append(const qg_append_desc *d /* HOST */, void *stream);
+
+/* Attention of one new token of each sequence over the cache.  Head h of `heads` reads key head
+ * h / (heads / kv_heads).  With the keys i of [max(first, len - window), len):
+ *   out = sum_i p_i v_i / sum_i p_i,  p_i = exp(scale q.k_i),   lse = log sum_i p_i
+ * A sequence without such a key has out = 0 and lse = -infinity.  What lies in cells outside that range is never
+ * used, NaN included.  Sums, running maxima and the products' accumulators are fp32; q enters the matrix instructions
+ * without loss and the p_i to 2^-16 of themselves or better.  Results are the same from run to run. */
+typedef struct qg_attention_desc {
+    qg_kv_cache cache;
+    const int32_t *lens;    /* [batch]: cells in use (limited to max_pages * page); sequence b uses row b of the tables */
+    const int32_t *first;   /* [batch]: first key (a left-padded prompt's padding is before it); NULL: 0 */
+    const void *q;          /* [batch][heads][head_dim] of `type`, batch entries q_stride apart; 16-byte aligned, stride a multiple of 8 */
+    void *out;              /* [batch][heads][head_dim] of `type` */
+    float *lse;             /* [batch][heads], or NULL */
+    int64_t q_stride;
+    int batch, heads, type; /* QG_F32, QG_BF16 or QG_F16 */
+    int window;             /* 0: none */
+    float scale;
+    void *workspace;
+    size_t workspace_bytes;
+} qg_attention_desc;
+int qg_paged_attention(const qg_attention_desc *d /* HOST */, void *stream);
+/* Scratch of qg_paged_attention: parts of outputs, and counters that are prepared once by qg_workspace_init and left
+ * prepared by every call.  Calls that overlap in time must not share one; a buffer as large as the largest
+ * batch asks for serves smaller ones, in any order.  0 if the sizes are not accepted. */
+size_t qg_paged_attention_workspace_bytes(int batch, int heads, int kv_heads, int head_dim);
+
+/* The pages' book of a batch: tables [rows][max_pages] of page ids (-1: none), lens [rows], and for each page of the pool how many
+ * table entries (and other holders) refer to it; 0 is free.  Every call reads one book and writes another.  `out` pointers
+ * may be the book's own (not in qg_pages_fork). */
+typedef struct qg_page_book {
+    const int32_t *tables, *lens, *refs;          /* [rows][max_pages], [rows], [pages] */
+    int32_t *tables_out, *lens_out, *refs_out;
+    int64_t pages;
+    int rows, max_pages, page;
+} qg_page_book;
+/* Memory whose pages move with the book: [layers][pages][page_bytes], 16-byte aligned, page_bytes a multiple of 16. */
+typedef struct qg_page_plane {
+    void *base;
+    int64_t layers, page_bytes;
+} qg_page_plane;
+#define QG_MAX_PLANES 8
+
+/* New lengths (limited to 0 ... max_pages * page) for every row.  First pages past the new lengths are let go of.  Then rows take
+ * what they lack, in order of rows and columns, from the lowest free pages.  A row that grows inside its last page while
+ * others hold that page too gets a copy of it (in all planes) in its place and lets go of it (pages that only such rows held are free
+ * after the call).  If the free pages do not suffice nothing changes (the book is passed on, no page is
+ * copied) and *lacking (DEVICE) says how many are missing; otherwise it is 0. */
+int qg_pages_resize(const qg_page_book *book /* HOST */, const int32_t *new_lens, const qg_page_plane *planes /* HOST */,
+                    int n_planes, int32_t *lacking, void *workspace, size_t workspace_bytes, void *stream);
+/* Row b becomes what row parents[b] was (outside 0 ... rows - 1: empty), sharing its pages; refs follow.  Branches, ends
+ * and reorders sequences; no page is copied.  The outputs must not be the inputs. */
+int qg_pages_fork(const qg_page_book *book /* HOST */, const int32_t *parents, void *stream);
+/* Packs the pool: with n pages in use, those with ids from n on move, in order, to the free ones below n, in all planes,
+ * and tables and refs follow (lens and lens_out are not used).  *live (DEVICE) = n. */
+int qg_pages_compact(const qg_page_book *book /* HOST */, const qg_page_plane *planes /* HOST */, int n_planes, int32_t *live,
+                     void *workspace, size_t workspace_bytes, void *stream);
+/* Copies page pairs[i][0] onto page pairs[i][1] in all planes, for i < count (pairs DEVICE; a pair with an id outside the
+ * pool is passed over).  No page may be both a source and a target, or twice a target. */
+int qg_pages_copy(const qg_page_plane *planes /* HOST */, int n_planes, int64_t pages, const int32_t *pairs, int count, void *stream);
+/* Scratch of qg_pages_resize and qg_pages_compact (16-byte aligned, needs no preparation). */
+size_t qg_pages_workspace_bytes(int rows, int max_pages, int64_t pages);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,6 +17,8 @@ QG_LAYOUT_CANONICAL = 0
 QG_LAYOUT_DEVICE = 1
 QG_LAYOUT_DEVICE_NARROW = 2
 QG_MAX_GROUPED = 16
+QG_F32, QG_BF16, QG_F16, QG_E4M3 = range(4)
+QG_MAX_PLANES = 8
 
 _LIB = None
 
@@ -106,6 +108,25 @@ def lib():
                                        ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_float)]
         L.qg_gemm_autotune_report.restype = i32
         L.qg_gemm_autotune_report.argtypes = [ctypes.POINTER(ctypes.c_float), i32, ctypes.POINTER(i32), ctypes.POINTER(i32)]
+        cp = ctypes.c_char_p                                # a description packed by value
+        L.qg_rms_norm.restype = i32
+        L.qg_rms_norm.argtypes = [cp, vp]
+        L.qg_kv_append.restype = i32
+        L.qg_kv_append.argtypes = [cp, vp]
+        L.qg_paged_attention.restype = i32
+        L.qg_paged_attention.argtypes = [cp, vp]
+        L.qg_paged_attention_workspace_bytes.restype = sz
+        L.qg_paged_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.qg_pages_resize.restype = i32
+        L.qg_pages_resize.argtypes = [cp, vp, cp, i32, vp, vp, sz, vp]
+        L.qg_pages_fork.restype = i32
+        L.qg_pages_fork.argtypes = [cp, vp, vp]
+        L.qg_pages_compact.restype = i32
+        L.qg_pages_compact.argtypes = [cp, cp, i32, vp, vp, sz, vp]
+        L.qg_pages_copy.restype = i32
+        L.qg_pages_copy.argtypes = [cp, i32, i64, vp, i32, vp]
+        L.qg_pages_workspace_bytes.restype = sz
+        L.qg_pages_workspace_bytes.argtypes = [i32, i32, i64]
         _LIB = L
     return _LIB
 
@@ -477,3 +498,266 @@ def qg_gemm_autotune_report():
 
 def qg_set_gemm_tuning(splits: int = 0, shape: int = 0):
     _check(lib().qg_set_gemm_tuning(splits, shape), "qg_set_gemm_tuning")
+
+
+# --- between the products of a token's step --------------------------------------------------------------------
+
+_TYPES = {torch.float32: QG_F32, torch.bfloat16: QG_BF16, torch.float16: QG_F16, torch.float8_e4m3fn: QG_E4M3}
+_E4M3 = torch.float8_e4m3fn
+# descriptions as include/qg.h lays them out (8-byte members first, so that nothing is padded in between)
+_NORM = struct.Struct("6Q4q4if4x").pack
+_CACHE = "5Q2q6i"
+_APPEND = struct.Struct(_CACHE + "7Q5q4i").pack
+_ATTENTION = struct.Struct(_CACHE + "5Qq4if4x2Q").pack
+_BOOK = struct.Struct("6Qq3i4x").pack
+_PLANE = struct.Struct("Qqq").pack
+
+
+def _type(t: torch.Tensor, name: str, types=(torch.float32, torch.bfloat16, torch.float16)) -> int:
+    if t.dtype not in types:
+        raise ValueError(f"{name}: expected one of {', '.join(map(str, types))}, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _gpu(t: torch.Tensor, name: str, shape=None) -> torch.Tensor:
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a tensor on the GPU")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _whole(t: torch.Tensor, dtype, name: str, shape) -> int:
+    _dev(t, dtype, name)
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, name: str, shape) -> int:
+    """Address of a [tokens][heads][head_dim] tensor whose tokens may lie apart (a part of a stacked product's output)."""
+    _gpu(t, name, shape)
+    stride = t.stride()
+    if stride[2] != 1 and shape[2] != 1 or stride[1] != shape[2] and shape[1] != 1:
+        raise ValueError(f"{name}: the heads of a token have to lie together")
+    return t.data_ptr()
+
+
+def _ptr(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def qg_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: Optional[torch.Tensor] = None,
+                dtype: Optional[torch.dtype] = None, group: int = 0, y: Optional[torch.Tensor] = None,
+                h: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None):
+    """(y, h, scales) of rows x [rows][K]: h = x + residual in x's type (None without a residual), y its norm times the
+    weight in `dtype` (x's own if not given); torch.float8_e4m3fn comes with scales [rows][K / group] (group 0: one for a
+    row), other types with None.  x and residual may have rows that lie apart; h may be either."""
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows][K]")
+    rows, K = x.shape
+    kind = _type(_gpu(x, "x"), "x")
+    if dtype is None:
+        dtype = x.dtype if y is None else y.dtype
+    if dtype not in _TYPES:
+        raise ValueError(f"dtype: {dtype} is not supported")
+    if x.stride(1) != 1 and K > 1:
+        raise ValueError("x: expected contiguous rows")
+    wkind = _type(_dev(weight, weight.dtype, "weight"), "weight")
+    if weight.shape != (K,) or group < 0 or (group and K % group):
+        _check(2, "qg_rms_norm")
+    e4m3 = dtype is _E4M3
+    y = _rows(rows, K, dtype, x.device) if y is None else y
+    yp = _whole(y, dtype, "y", (rows, K))
+    hp = rp = rstride = sp = 0
+    if residual is not None:
+        _gpu(residual, "residual", x.shape)
+        if residual.dtype != x.dtype or (residual.stride(1) != 1 and K > 1):
+            raise ValueError("residual: expected x's type and contiguous rows")
+        h = _rows(rows, K, x.dtype, x.device) if h is None else h
+        hp, rp, rstride = _whole(h, x.dtype, "h", (rows, K)), residual.data_ptr(), residual.stride(0)
+    elif h is not None:
+        raise ValueError("h: there is none without a residual")
+    if e4m3:
+        groups = K // group if group else 1
+        scales = _rows(rows, groups, torch.float32, x.device) if scales is None else scales
+        sp = _whole(scales, torch.float32, "scales", (rows, groups))
+    elif scales is not None:
+        raise ValueError("scales: float8_e4m3fn only")
+    rc = (_LIB or lib()).qg_rms_norm(_NORM(x.data_ptr(), rp, weight.data_ptr(), hp, yp, sp, rows, K, x.stride(0), rstride,
+                                           kind, wkind, _TYPES[dtype], group, eps), _stream())
+    if rc != 0:
+        _check(rc, "qg_rms_norm")
+    return y, h, scales
+
+
+def _cache(k, v, tables, k_scale, v_scale):
+    """The packed members of a qg_kv_cache, checked."""
+    shape = k.shape
+    kind = _type(_dev(k, k.dtype, "k"), "k", (torch.bfloat16, torch.float16, _E4M3))
+    if len(shape) != 4:
+        raise ValueError("k: expected [pages][kv_heads][page][head_dim]")
+    vp = _whole(v, k.dtype, "v", shape)
+    ksp = vsp = 0
+    if kind == QG_E4M3:
+        if k_scale is None or v_scale is None:
+            raise ValueError("k_scale, v_scale: a cache in float8_e4m3fn has them")
+        ksp, vsp = _whole(k_scale, torch.float32, "k_scale", shape[:3]), _whole(v_scale, torch.float32, "v_scale", shape[:3])
+    if not tables.is_cuda or tables.dtype != torch.int32 or tables.dim() != 2 or (tables.stride(1) != 1 and tables.shape[1] > 1):
+        raise ValueError("tables: expected an int32 tensor [rows][max_pages] on the GPU, rows contiguous")
+    return (k.data_ptr(), vp, ksp, vsp, tables.data_ptr(), tables.stride(0), shape[0], tables.shape[0], tables.shape[1], shape[1], shape[2],
+            shape[3], kind)
+
+
+def qg_kv_append(k_cache: torch.Tensor, v_cache: torch.Tensor, tables: torch.Tensor, rows: torch.Tensor, positions: torch.Tensor,
+                 k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
+                 interleaved: bool = False, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+                 q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Stores k and v [tokens][kv_heads][head_dim] in the cache's pages at each token's row and position, k and q rotated by
+    cos_sin [positions][rope_dim] (cosines, then sines; None: not at all), and returns the rotated q.  A token of a row
+    or position without a page (row -1, say) is padding."""
+    cache = _cache(k_cache, v_cache, tables, k_scale, v_scale)
+    kv_heads, D = cache[9], cache[11]
+    tokens, heads, qp, qs, qop = k.shape[0], 0, 0, 0, 0
+    kind = _type(k, "k")
+    kp, vp = _heads(k, "k", (tokens, kv_heads, D)), _heads(v, "v", (tokens, kv_heads, D))
+    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        raise ValueError("q, k, v: expected one type")
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else 0
+        qp, qs = _heads(q, "q", (tokens, heads, D)), q.stride(0)
+        if q_out is None:
+            q_out = torch.empty_strided((tokens, heads, D), (heads * D, D, 1), dtype=q.dtype, device=q.device)
+        qop = _whole(q_out, q.dtype, "q_out", (tokens, heads, D))
+    rp, pp = _whole(rows, torch.int32, "rows", (tokens,)), _whole(positions, torch.int32, "positions", (tokens,))
+    cp = rope = angles = 0
+    if cos_sin is not None:
+        if cos_sin.dim() != 2:
+            raise ValueError("cos_sin: expected [positions][rope_dim]")
+        cp, angles, rope = _dev(cos_sin, torch.float32, "cos_sin").data_ptr(), cos_sin.shape[0], cos_sin.shape[1]
+    rc = (_LIB or lib()).qg_kv_append(_APPEND(*cache, rp, pp, qp, kp, vp, qop, cp, tokens, qs, k.stride(0), v.stride(0), angles,
+                                              kind, heads, rope, 1 if interleaved else 0), _stream())
+    if rc != 0:
+        _check(rc, "qg_kv_append")
+    return q_out
+
+
+def qg_paged_attention_workspace_bytes(batch: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().qg_paged_attention_workspace_bytes(batch, heads, kv_heads, head_dim))
+
+
+def qg_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor,
+                       scale: float, first: Optional[torch.Tensor] = None, window: int = 0, k_scale: Optional[torch.Tensor] = None,
+                       v_scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, lse=False,
+                       workspace: Optional[torch.Tensor] = None):
+    """(out, lse) of one new token q [batch][heads][head_dim] of each sequence over its cells [max(first, lens - window), lens)
+    of the cache.  lse [batch][heads] is written if asked for by True or handed in, otherwise None."""
+    cache = _cache(k_cache, v_cache, tables, k_scale, v_scale)
+    if q.dim() != 3:
+        raise ValueError("q: expected [batch][heads][head_dim]")
+    batch, heads, D = q.shape
+    kind = _type(q, "q")
+    qp = _heads(q, "q", (batch, heads, cache[11]))
+    if out is None:
+        out = torch.empty_strided((batch, heads, D), (heads * D, D, 1), dtype=q.dtype, device=q.device)
+    op = _whole(out, q.dtype, "out", (batch, heads, D))
+    lp = _whole(lens, torch.int32, "lens", (batch,))
+    fp = 0 if first is None else _whole(first, torch.int32, "first", (batch,))
+    if lse is True:
+        lse = _rows(batch, heads, torch.float32, q.device)
+    elif lse is False:
+        lse = None
+    ep = 0 if lse is None else _whole(lse, torch.float32, "lse", (batch, heads))
+    L = _LIB or lib()
+    if workspace is None:
+        workspace = new_workspace(L.qg_paged_attention_workspace_bytes(batch, heads, cache[9], D), q.device)
+    rc = L.qg_paged_attention(_ATTENTION(*cache, lp, fp, qp, op, ep, q.stride(0), batch, heads, kind, window, scale,
+                                         workspace.data_ptr(), workspace.numel() * workspace.element_size()), _stream())
+    if rc != 0:
+        _check(rc, "qg_paged_attention")
+    return out, lse
+
+
+def qg_pages_workspace_bytes(rows: int, max_pages: int, pages: int) -> int:
+    return int(lib().qg_pages_workspace_bytes(rows, max_pages, pages))
+
+
+def _planes(planes, pages: int) -> bytes:
+    """Tensors [layers][pages][...] whose pages move with the book, packed as qg_page_plane."""
+    packed = b""
+    for t in planes:
+        if not t.is_cuda or not t.is_contiguous() or t.dim() < 3 or t.shape[1] != pages:
+            raise ValueError("planes: expected contiguous tensors [layers][pages][...] on the GPU")
+        packed += _PLANE(t.data_ptr(), t.shape[0], t.stride(1) * t.element_size())
+    return packed
+
+
+def _book(tables, lens, refs, page, out):
+    """(packed qg_page_book, rows, max_pages, pages, tables_out, lens_out, refs_out)"""
+    if tables.dim() != 2:
+        raise ValueError("tables: expected [rows][max_pages]")
+    rows, columns = tables.shape
+    pages = refs.numel()
+    tp, rp = _dev(tables, torch.int32, "tables").data_ptr(), _whole(refs, torch.int32, "refs", (pages,))
+    lp = 0 if lens is None else _whole(lens, torch.int32, "lens", (rows,))
+    if out is None:
+        device = tables.device
+        out = (_rows(rows, columns, torch.int32, device), None if lens is None else torch.empty_strided((rows,), (1,), dtype=torch.int32, device=device),
+               torch.empty_strided((pages,), (1,), dtype=torch.int32, device=device))
+    t, n, r = out
+    packed = _BOOK(tp, lp, rp, _whole(t, torch.int32, "tables out", (rows, columns)), 0 if lens is None else _whole(n, torch.int32, "lens out", (rows,)),
+                   _whole(r, torch.int32, "refs out", (pages,)), pages, rows, columns, page)
+    return packed, rows, columns, pages, t, n, r
+
+
+def qg_pages_resize(tables: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, page: int, new_lens: torch.Tensor,
+                    planes: Sequence[torch.Tensor] = (), out=None, lacking: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None):
+    """(tables, lens, refs, lacking) after every row got its new length: pages let go of and taken, shared last pages of rows
+    that grow copied in all planes ([layers][pages][...]).  lacking [1]: 0, or how many free pages were missing
+    (then nothing changed).  out: (tables, lens, refs) to write into, the old ones for instance."""
+    book, rows, columns, pages, t, n, r = _book(tables, lens, refs, page, out)
+    np_ = _whole(new_lens, torch.int32, "new_lens", (rows,))
+    lacking = torch.empty_strided((1,), (1,), dtype=torch.int32, device=tables.device) if lacking is None else lacking
+    L = _LIB or lib()
+    if workspace is None:
+        workspace = _bytes(max(256, L.qg_pages_workspace_bytes(rows, columns, pages)), tables.device)
+    rc = L.qg_pages_resize(book, np_, _planes(planes, pages), len(planes), _whole(lacking, torch.int32, "lacking", (1,)),
+                           workspace.data_ptr(), workspace.numel(), _stream())
+    if rc != 0:
+        _check(rc, "qg_pages_resize")
+    return t, n, r, lacking
+
+
+def qg_pages_fork(tables: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, parents: torch.Tensor, out=None):
+    """(tables, lens, refs) with row b the former row parents[b] (-1: empty), pages shared.  out must not be the old ones."""
+    book, rows, _, _, t, n, r = _book(tables, lens, refs, 1, out)
+    rc = (_LIB or lib()).qg_pages_fork(book, _whole(parents, torch.int32, "parents", (rows,)), _stream())
+    if rc != 0:
+        _check(rc, "qg_pages_fork")
+    return t, n, r
+
+
+def qg_pages_compact(tables: torch.Tensor, refs: torch.Tensor, planes: Sequence[torch.Tensor] = (), out=None,
+                     live: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(tables, refs, live) with the pages in use moved to the lower end of the pool in all planes; live [1]: how many
+    there are.  out: (tables, refs) to write into, the old ones for instance."""
+    book, rows, columns, pages, t, _, r = _book(tables, None, refs, 1, None if out is None else (out[0], None, out[1]))
+    live = torch.empty_strided((1,), (1,), dtype=torch.int32, device=tables.device) if live is None else live
+    L = _LIB or lib()
+    if workspace is None:
+        workspace = _bytes(max(256, L.qg_pages_workspace_bytes(rows, columns, pages)), tables.device)
+    rc = L.qg_pages_compact(book, _planes(planes, pages), len(planes), _whole(live, torch.int32, "live", (1,)),
+                            workspace.data_ptr(), workspace.numel(), _stream())
+    if rc != 0:
+        _check(rc, "qg_pages_compact")
+    return t, r, live
+
+
+def qg_pages_copy(planes: Sequence[torch.Tensor], pairs: torch.Tensor):
+    """Copies page pairs[i][0] onto page pairs[i][1] in all planes [layers][pages][...]."""
+    pages = planes[0].shape[1] if len(planes) and planes[0].dim() > 1 else 0
+    if pairs.dim() != 2 or pairs.shape[1] != 2:
+        raise ValueError("pairs: expected [count][2]")
+    _check((_LIB or lib()).qg_pages_copy(_planes(planes, pages), len(planes), pages, _dev(pairs, torch.int32, "pairs").data_ptr(),
+                                         pairs.shape[0], _stream()), "qg_pages_copy")

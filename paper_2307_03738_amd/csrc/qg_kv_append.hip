@@ -1,0 +1,107 @@
+// qg_kv_append: rotates q and k of new tokens and stores k and v in the pages of a cache.
+#include "qg_kv.h"
+
+namespace {
+
+struct AppendArgs {
+    QgKv kv;
+    const int32_t *rows, *positions;
+    const void *q, *k, *v;
+    void *q_out;
+    const float *cos_sin;
+    int64_t q_stride, k_stride, v_stride, cos_sin_rows;
+    int heads, rope_dim, interleaved;
+};
+
+// One wavefront per token and head of q, k or v.
+template <int TYPE, int CACHE>
+__global__ __launch_bounds__(256) void append_heads(AppendArgs a)
+{
+    const int64_t token = blockIdx.x;
+    const int item = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int D = a.kv.head_dim, items = a.heads + 2 * a.kv.kv_heads;
+    if (item >= items) return;
+    const int64_t position = a.positions[token];
+    int64_t page = qg_page_of(a.kv, a.rows[token], position);
+    if (a.rope_dim && position >= a.cos_sin_rows) page = -1;
+    const bool is_q = item < a.heads, is_v = item >= a.heads + a.kv.kv_heads;
+    const int head = is_q ? item : is_v ? item - a.heads - a.kv.kv_heads : item - a.heads;
+    if (page < 0) {
+        if (is_q)
+            for (int i = lane; i < D; i += 64) store_float<TYPE>(a.q_out, (token * a.heads + head) * D + i, 0.0f);
+        return;
+    }
+    const void *src = is_q ? a.q : is_v ? a.v : a.k;
+    const int64_t at = token * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (int64_t)head * D;
+    const int half = a.rope_dim / 2;
+    const float *angle = a.cos_sin + (a.rope_dim ? position * a.rope_dim : 0);
+    float x[4];
+    for (int c = 0; c < 4; ++c) {
+        const int i = lane + 64 * c;
+        x[c] = 0.0f;
+        if (i >= D) continue;
+        x[c] = load_as_float<TYPE>(src, at + i);
+        if (is_v || i >= a.rope_dim) continue;
+        const int j = a.interleaved ? i >> 1 : i < half ? i : i - half;
+        const bool second = a.interleaved ? (i & 1) : i >= half;
+        const float other = load_as_float<TYPE>(src, at + (a.interleaved ? (i ^ 1) : second ? i - half : i + half));
+        const float cosine = angle[j], sine = angle[half + j];
+        x[c] = second ? x[c] * cosine + other * sine : x[c] * cosine - other * sine;
+    }
+    if (is_q) {
+        for (int c = 0; c < 4; ++c)
+            if (lane + 64 * c < D) store_float<TYPE>(a.q_out, (token * a.heads + head) * D + lane + 64 * c, x[c]);
+        return;
+    }
+    const int64_t cell = (page * a.kv.kv_heads + head) * a.kv.page + (position & (a.kv.page - 1));
+    float scale = 1.0f;
+    if constexpr (CACHE == QG_E4M3) {
+        uint32_t most = 0;
+        for (int c = 0; c < 4; ++c) most = max(most, magnitude_bits(x[c]));
+        for (int off = 32; off; off >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, off));
+        scale = e4m3_scale(most);
+        if (lane == 0) (is_v ? a.kv.v_scale : a.kv.k_scale)[cell] = scale;
+    }
+    for (int c = 0; c < 4; ++c)
+        if (lane + 64 * c < D)
+            store_float<CACHE>(is_v ? a.kv.v : a.kv.k, cell * D + lane + 64 * c, CACHE == QG_E4M3 ? limit_e4m3(x[c] / scale) : x[c]);
+}
+
+template <int TYPE>
+int launch_append(int64_t tokens, const AppendArgs &a, hipStream_t st)
+{
+    const dim3 grid((unsigned)tokens, (unsigned)((a.heads + 2 * a.kv.kv_heads + 3) / 4));
+    switch (a.kv.type) {
+    case QG_BF16: hipLaunchKernelGGL((append_heads<TYPE, QG_BF16>), grid, dim3(256), 0, st, a); break;
+    case QG_F16: hipLaunchKernelGGL((append_heads<TYPE, QG_F16>), grid, dim3(256), 0, st, a); break;
+    default: hipLaunchKernelGGL((append_heads<TYPE, QG_E4M3>), grid, dim3(256), 0, st, a); break;
+    }
+    return qg_launch_status();
+}
+
+}  // namespace
+
+extern "C" int qg_kv_append(const qg_append_desc *desc, void *stream)
+{
+    if (!desc) return QG_ERR_NULL;
+    const qg_append_desc &d = *desc;
+    QgKv kv;
+    const int rc = qg_check_cache(d.cache, &kv);
+    if (rc != QG_OK) return rc;
+    if (!qg_float_type(d.type)) return QG_ERR_UNSUPPORTED;
+    const int D = kv.head_dim;
+    if (d.tokens < 0 || d.tokens > 0x7fffffff || d.heads < 0 || d.heads > QG_MAX_HEADS || d.rope_dim < 0 || d.rope_dim > D || d.rope_dim % 2 ||
+        (d.rope_dim && d.cos_sin_rows < 0)) return QG_ERR_SHAPE;
+    if (d.tokens == 0) return QG_OK;
+    if (d.tokens > 1 && ((d.heads && d.q_stride < (int64_t)d.heads * D) || d.k_stride < (int64_t)kv.kv_heads * D || d.v_stride < (int64_t)kv.kv_heads * D))
+        return QG_ERR_SHAPE;
+    if (!d.rows || !d.positions || !d.k || !d.v || (d.heads && (!d.q || !d.q_out)) || (d.rope_dim && !d.cos_sin)) return QG_ERR_NULL;
+    if (!qg_aligned16(d.k) || !qg_aligned16(d.v) || (d.heads && (!qg_aligned16(d.q) || !qg_aligned16(d.q_out))) || !qg_aligned_to(d.cos_sin, 4) ||
+        !qg_aligned_to(d.rows, 4) || !qg_aligned_to(d.positions, 4) ||
+        (d.tokens > 1 && (d.k_stride % 8 || d.v_stride % 8 || (d.heads && d.q_stride % 8)))) return QG_ERR_ALIGN;
+    const AppendArgs a = {kv, d.rows, d.positions, d.q, d.k, d.v, d.q_out, d.cos_sin, d.q_stride, d.k_stride, d.v_stride, d.cos_sin_rows,
+                          d.heads, d.rope_dim, d.interleaved != 0};
+    hipStream_t st = (hipStream_t)stream;
+    return d.type == QG_F32 ? launch_append<QG_F32>(d.tokens, a, st) : d.type == QG_BF16 ? launch_append<QG_BF16>(d.tokens, a, st)
+                                                                                       : launch_append<QG_F16>(d.tokens, a, st);
+}
