@@ -24,7 +24,7 @@ namespace {
 
 constexpr int WAVES = 4;                   // wavefronts of a workgroup
 constexpr int SPAN = 32 * WAVES;           // keys they take together
-constexpr int MAX_WORKERS = 1024;          // workgroups of a launch at most (sizes the counters in the workspace)
+constexpr int MAX_WORKERS = 512;           // workgroups of a launch at most (sizes the counters in the workspace and the maxima in LDS)
 constexpr int COUNTER_BYTES = 4 * MAX_WORKERS;
 constexpr float SLACK = 8.0f;
 
@@ -41,6 +41,7 @@ struct AttentionArgs {
     uint32_t *arrived;                     // [worker]
     float *parts;                          // [2 * worker + ...]: rows x head_dim sums, then rows x (maximum, sum of p)
     int part_floats;
+    uint32_t parts_bytes;
 };
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -48,6 +49,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 union Operand {
     bf16x8 b;
@@ -78,6 +80,14 @@ __device__ inline uint32_t take_part(float &a, float &b)
         b -= __uint_as_float(r & 0xffff0000u);
         return r;
     }
+}
+
+// Parts are written and read past the caches of the chip's dies.
+constexpr int SC1 = 16;
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+__device__ inline rsrc_t buffer_of(const void *p, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000);
 }
 
 __device__ inline float across_quads_max(float v)
@@ -317,10 +327,14 @@ template <int TYPE, int CACHE, int DPAD, bool FULL>
 __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(AttentionArgs a)
 {
     typedef Attend<TYPE, CACHE, DPAD, FULL> A;
-    __shared__ float sums[WAVES][16][A::LDS_ROW];
-    __shared__ float wave_m[WAVES][16], wave_l[WAVES][16];
+    // the wavefronts' sums [wavefront][head][LDS_ROW]; of a head's parts, the maxima [part][head]
+    constexpr int SHARED_FLOATS = WAVES * 16 * A::LDS_ROW > 16 * MAX_WORKERS ? WAVES * 16 * A::LDS_ROW : 16 * MAX_WORKERS;
+    __shared__ float shared[SHARED_FLOATS];
+    __shared__ float wave_m[16][16], wave_l[16][16];
     __shared__ int64_t found_before;
     __shared__ int found_b, scan[WAVES], is_last;
+    __shared__ float head_m[16], head_l[16];
+    const rsrc_t parts = buffer_of(a.parts, a.parts_bytes);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, j = lane >> 4;
     const int D = FULL ? DPAD : a.kv.head_dim;
     const int heads = a.kv.kv_heads * a.blocks;                     // blocks of heads of a sequence
@@ -453,7 +467,7 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
         const float keep = t.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t.m - most);
         const bool whole = from == 0 && to == keys.spans;
         // a worker's first part of a head's keys goes into its slot 0 unless it begins them
-        float *part = a.parts + ((int64_t)2 * worker + (from == 0)) * a.part_floats;
+        const uint32_t part = 4u * (2 * worker + (from == 0)) * a.part_floats;
         for (int half = 0; half < DPAD / A::LDS_DIMS; ++half) {
             if (half) __syncthreads();
             if (i < rows) {
@@ -466,17 +480,17 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
                         floatx4 v;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) v[k] = (DPAD > 128 && half ? t.o[A::DIMS / 2 * (DPAD > 128) + n + k][r] : t.o[n + k][r]) * keep;
-                        *(floatx4 *)&sums[wave][i][d] = v;
+                        *(floatx4 *)&shared[(wave * 16 + i) * A::LDS_ROW + d] = v;
                     }
             }
             __syncthreads();
             const int quads = min(D - half * A::LDS_DIMS, A::LDS_DIMS) / 4;
             for (int x = tid; x < rows * quads; x += 64 * WAVES) {
                 const int row = x / quads, d = 4 * (x - row * quads);
-                floatx4 v = *(const floatx4 *)&sums[0][row][d];
+                floatx4 v = *(const floatx4 *)&shared[row * A::LDS_ROW + d];
                 float sum_l = 0.0f, top = -INFINITY;
 #pragma unroll
-                for (int w = 1; w < WAVES; ++w) v += *(const floatx4 *)&sums[w][row][d];
+                for (int w = 1; w < WAVES; ++w) v += *(const floatx4 *)&shared[(w * 16 + row) * A::LDS_ROW + d];
                 if (whole) {
 #pragma unroll
                     for (int w = 0; w < WAVES; ++w) top = fmaxf(top, wave_m[w][row]);
@@ -486,9 +500,7 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
 #pragma unroll
                     for (int k = 0; k < 4; ++k) store_float<TYPE>(a.out, at_out + k, sum_l == 0.0f ? 0.0f : v[k] / sum_l);
                 } else {
-                    float *to_part = part + row * D + half * A::LDS_DIMS + d;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) __hip_atomic_store(to_part + k, v[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), parts, part + 4 * (row * D + half * A::LDS_DIMS + d), 0, SC1);
                 }
             }
         }
@@ -499,9 +511,7 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
             if (whole) {
                 if (a.lse) a.lse[(int64_t)b * a.heads + head0 + tid] = sum_l == 0.0f ? -INFINITY : top * 0.6931471805599453f + logf(sum_l);
             } else {
-                float *to_part = part + rows * D + 2 * tid;
-                __hip_atomic_store(to_part, top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __hip_atomic_store(to_part + 1, sum_l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(top), __float_as_uint(sum_l)}, parts, part + 4 * (rows * D + 2 * tid), 0, SC1);
             }
         }
         if (!whole) {
@@ -519,21 +529,71 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
             }
             __syncthreads();
             if (is_last) {
-                auto part_of = [&](int k) { return a.parts + ((int64_t)2 * (w0 + k) + (k == 0)) * a.part_floats; };
-                auto read = [&](const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-                for (int x = tid; x < rows * D; x += 64 * WAVES) {
-                    const int row = x / D;
-                    float top = -INFINITY, sum_l = 0.0f, v = 0.0f;
-                    for (int k = 0; k < n; ++k) top = fmaxf(top, read(part_of(k) + rows * D + 2 * row));
-                    for (int k = 0; k < n; ++k) {
-                        const float m = read(part_of(k) + rows * D + 2 * row);
-                        const float keep_k = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-                        sum_l += keep_k * read(part_of(k) + rows * D + 2 * row + 1);
-                        v += keep_k * read(part_of(k) + x);
+                auto part_of = [&](int k) { return 4u * (2 * (w0 + k) + (k == 0)) * a.part_floats; };
+                // maxima and sums of p: 16 lanes for each head, each over every 16th part, then over each other
+                {
+                    const int row = tid & 15, share = tid >> 4;
+                    float top = -INFINITY, sum_l = 0.0f;
+                    if (row < rows)
+                        for (int k = share; k < n; k += 16) {
+                            const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(parts, part_of(k) + 4 * (rows * D + 2 * row), 0, SC1);
+                            const float m = __uint_as_float(x[0]), next = fmaxf(top, m);
+                            shared[k * 16 + row] = m;
+                            if (m != -INFINITY) sum_l = (top == -INFINITY ? 0.0f : sum_l * __builtin_amdgcn_exp2f(top - next)) +
+                                                        __uint_as_float(x[1]) * __builtin_amdgcn_exp2f(m - next);
+                            top = next;
+                        }
+                    wave_m[share][row] = top;
+                    wave_l[share][row] = sum_l;
+                }
+                __syncthreads();
+                if (tid < 16) {
+                    float top = -INFINITY, sum_l = 0.0f;
+                    for (int w = 0; w < 16; ++w) top = fmaxf(top, wave_m[w][tid]);
+                    for (int w = 0; w < 16; ++w) sum_l += wave_m[w][tid] == -INFINITY ? 0.0f : wave_l[w][tid] * __builtin_amdgcn_exp2f(wave_m[w][tid] - top);
+                    head_m[tid] = top;
+                    head_l[tid] = sum_l;
+                    if (a.lse && tid < rows) a.lse[(int64_t)b * a.heads + head0 + tid] = sum_l == 0.0f ? -INFINITY : top * 0.6931471805599453f + logf(sum_l);
+                }
+                __syncthreads();
+                // outputs, four dims a lane; where that leaves lanes over, several share the parts of one
+                const int quads = rows * D / 4;
+                int shares = 1;
+                while (2 * shares * quads <= 64 * WAVES) shares *= 2;
+                for (int x0 = 0; x0 < quads; x0 += 64 * WAVES) {
+                    const int x = shares > 1 ? tid % quads : x0 + tid, share = shares > 1 ? tid / quads : 0;
+                    const bool mine = shares > 1 ? share < shares : x < quads;
+                    const int row = mine ? x / (D / 4) : 0;
+                    floatx4 v = {0, 0, 0, 0};
+                    if (mine) {
+                        const float top = head_m[row];
+                        constexpr int AT_ONCE = 8;
+                        for (int k0 = share; k0 < n; k0 += AT_ONCE * shares) {
+                            u32x4 y[AT_ONCE];
+#pragma unroll
+                            for (int c = 0; c < AT_ONCE; ++c)
+                                if (k0 + c * shares < n) y[c] = __builtin_amdgcn_raw_buffer_load_b128(parts, part_of(k0 + c * shares) + 16 * x, 0, SC1);
+#pragma unroll
+                            for (int c = 0; c < AT_ONCE; ++c)
+                                if (k0 + c * shares < n) {
+                                    const float m = shared[(k0 + c * shares) * 16 + row];
+                                    v += (m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top)) * __builtin_bit_cast(floatx4, y[c]);
+                                }
+                        }
                     }
-                    const int64_t head_out = (int64_t)b * a.heads + head0 + row;
-                    store_float<TYPE>(a.out, head_out * D + (x - row * D), sum_l == 0.0f ? 0.0f : v / sum_l);
-                    if (a.lse && x == row * D) a.lse[head_out] = sum_l == 0.0f ? -INFINITY : top * 0.6931471805599453f + logf(sum_l);
+                    if (shares > 1) {
+                        __syncthreads();                            // the maxima have been read
+                        if (mine) *(floatx4 *)&shared[4 * tid] = v;
+                        __syncthreads();
+                        if (share == 0)
+                            for (int k = 1; k < shares; ++k) v += *(const floatx4 *)&shared[4 * (tid + k * quads)];
+                    }
+                    if (mine && share == 0) {
+                        const float sum_l = head_l[row];
+                        const int64_t at_out = ((int64_t)b * a.heads + head0) * D + 4 * x;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) store_float<TYPE>(a.out, at_out + k, sum_l == 0.0f ? 0.0f : v[k] / sum_l);
+                    }
                 }
             }
         }
@@ -607,7 +667,7 @@ extern "C" int qg_paged_attention(const qg_attention_desc *desc, void *stream)
     const int group = d.heads / kv.kv_heads;
     const AttentionArgs a = {kv, d.lens, d.first, d.q, d.out, d.lse, d.q_stride, d.batch, d.heads, d.window, group, (group + 15) / 16,
                              group < 16 ? group : 16, d.scale, (uint32_t *)d.workspace, (float *)((char *)d.workspace + COUNTER_BYTES),
-                             part_floats(d.heads, kv.kv_heads, D)};
+                             part_floats(d.heads, kv.kv_heads, D), (uint32_t)(2 * workers_for(D) * part_floats(d.heads, kv.kv_heads, D) * 4)};
     hipStream_t st = (hipStream_t)stream;
     return d.type == QG_F32 ? launch_attention<QG_F32>(a, st) : d.type == QG_BF16 ? launch_attention<QG_BF16>(a, st) : launch_attention<QG_F16>(a, st);
 }
