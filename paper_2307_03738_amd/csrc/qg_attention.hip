@@ -139,23 +139,47 @@ struct Attend {
     // First dim of load c of a key's elements by the lanes of quad j (of 8 elements, or 16 bytes of e4m3).
     __device__ static int k_dim(int c, int j) { return E4M3 ? 64 * c + 16 * j : 32 * c + 8 * j; }
 
+    float x[CHUNKS][8];                                            // q on its way into the operands
+
+    // (most sequences' first loads: issued before what depends on the page ids, used after it)
     __device__ void load_q(const AttentionArgs &a, int64_t b, int head, bool real, int j)
     {
         const int D = FULL ? DPAD : a.kv.head_dim;
-        const int64_t at = b * a.q_stride + (int64_t)head * D;
-        float x[CHUNKS][8], most = 0.0f;
+        const char *row = (const char *)a.q + (b * a.q_stride + (int64_t)head * D) * (TYPE == QG_F32 ? 4 : 2);
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             const int d = E4M3 ? k_dim(c / 2, j) + 8 * (c % 2) : k_dim(c, j);
+            const bool some = real && (FULL || d < D);
+            if constexpr (TYPE == QG_F32) {
+                floatx4 v[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+                if (some) {
+                    v[0] = *(const floatx4 *)(row + 4 * d);
+                    v[1] = *(const floatx4 *)(row + 4 * d + 16);
+                }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[c][e] = real && (FULL || d < D) ? load_as_float<TYPE>(a.q, at + d + e) : 0.0f;
-                most = fmaxf(most, fabsf(x[c][e]));
+                for (int e = 0; e < 8; ++e) x[c][e] = v[e / 4][e % 4];
+            } else {
+                u32x4 v = {0, 0, 0, 0};
+                if (some) v = *(const u32x4 *)(row + 2 * d);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t bits = e % 2 ? v[e / 2] >> 16 : v[e / 2] & 0xffffu;
+                    x[c][e] = TYPE == QG_BF16 ? bf16_to_float(bits) : f16_to_float(bits);
+                }
             }
         }
+    }
+
+    __device__ void split_q(const AttentionArgs &a)
+    {
         factor = a.scale * 1.4426950408889634f;
         if constexpr (F16) {
             // the largest element to [2^14, 2^15), so that what f16 cannot hold is below 2^-38 of it
+            float most = 0.0f;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[c][e]));
             most = across_quads_max(most);
             const int up = most > 0.0f && most < INFINITY ? 14 - ilogbf(most) : 0;
 #pragma unroll
@@ -340,45 +364,45 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
     const int heads = a.kv.kv_heads * a.blocks;                     // blocks of heads of a sequence
     const int worker = blockIdx.x;
 
-    // spans of all sequences, and the sequence that this worker's part of them begins in
+    // spans of all sequences, and the sequence that this worker's part of them begins in (the batch 256 at a time)
     int64_t total = 0;
-    int first_spans = 0;                                            // of sequence tid (the first 256)
-    for (int b = tid; b < a.batch; b += 64 * WAVES) {
-        const int n = keys_of(a, b).spans;
-        if (b == tid) first_spans = n;
-        total += n;
+    int mine = 0, up_to_mine = 0;                                   // of the chunk at hand: spans of sequence tid, and with those before it
+    auto scan_chunk = [&](int b0) {
+        mine = up_to_mine = b0 + tid < a.batch ? keys_of(a, b0 + tid).spans : 0;
+        for (int off = 1; off < 64; off <<= 1) {
+            const int x = __shfl_up(up_to_mine, off);
+            if (lane >= off) up_to_mine += x;
+        }
+        if (lane == 63) scan[wave] = up_to_mine;
+        __syncthreads();
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < wave) up_to_mine += scan[w];
+            all += scan[w];
+        }
+        return all;
+    };
+    for (int b0 = 0; b0 < a.batch; b0 += 64 * WAVES) {
+        if (b0) __syncthreads();                                    // scan is free again
+        total += scan_chunk(b0);
     }
-    for (int off = 32; off; off >>= 1) total += __shfl_xor(total, off);
-    __shared__ int64_t wave_total[WAVES];
-    if (lane == 0) wave_total[wave] = total;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < WAVES; ++w) total += wave_total[w];
     total *= heads;
     const int workers = total < gridDim.x ? (int)total : (int)gridDim.x;        // each has a span at least
     if (worker >= workers) return;                                  // the whole workgroup
     const int64_t begin_at = worker_begin(total, worker, workers), end_at = worker_begin(total, worker + 1, workers);
     int64_t before = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 64 * WAVES) {
-        const int b = b0 + tid;
-        const int n = b >= a.batch ? 0 : b0 == 0 ? first_spans : keys_of(a, b).spans;
-        int s = n;
-        for (int off = 1; off < 64; off <<= 1) {
-            const int x = __shfl_up(s, off);
-            if (lane >= off) s += x;
+        int all = 0;
+        if (a.batch > 64 * WAVES) {                                 // (else the only chunk is at hand)
+            __syncthreads();
+            all = scan_chunk(b0);
         }
-        __syncthreads();
-        if (lane == 63) scan[wave] = s;
-        __syncthreads();
-        int64_t up_to = before;
-        for (int w = 0; w < wave; ++w) up_to += scan[w];
-        up_to += s;
-        if (b < a.batch && begin_at < up_to * heads && begin_at >= (up_to - n) * heads) {
-            found_b = b;
-            found_before = (up_to - n) * heads;
+        if (begin_at < (before + up_to_mine) * heads && begin_at >= (before + up_to_mine - mine) * heads) {
+            found_b = b0 + tid;
+            found_before = (before + up_to_mine - mine) * heads;
         }
-        for (int w = 0; w < WAVES; ++w) before += scan[w];
-        if (before * heads > begin_at) break;
+        before += all;
     }
     __syncthreads();
     int b = found_b;
@@ -398,7 +422,6 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
         const int kv_head = hb / a.blocks, head0 = kv_head * a.group + (hb - kv_head * a.blocks) * 16;
         const int rows = min(16, a.group - (hb - kv_head * a.blocks) * 16);
 
-        t.load_q(a, b, head0 + i, i < rows, j);
         t.m = -INFINITY;
         t.l = 0.0f;
 #pragma unroll
@@ -433,8 +456,10 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
         };
         if (tiles) {
             pages_from(0);
+            t.load_q(a, b, head0 + i, i < rows, j);
             fetch_k(0);
             fetch_v(0);
+            t.split_q(a);
         }
         for (int n = 0; n < tiles; ++n) {
             floatx4 s[2];
