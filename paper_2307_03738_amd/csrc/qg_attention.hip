@@ -24,9 +24,11 @@ namespace {
 
 constexpr int WAVES = 4;                   // wavefronts of a workgroup
 constexpr int SPAN = 32 * WAVES;           // keys they take together
-constexpr int MAX_WORKERS = 512;           // workgroups of a launch at most (sizes the counters in the workspace and the maxima in LDS)
+constexpr int MAX_WORKERS = 512;           // workgroups of a launch at most (sizes the counters in the workspace)
 constexpr int COUNTER_BYTES = 4 * MAX_WORKERS;
 constexpr float SLACK = 8.0f;
+// Workgroups that a compute unit holds, by the registers that a head's dims take (three of 64 dims would spill and be no faster)
+constexpr int groups_per_unit(int head_dim) { return head_dim <= 128 ? 2 : 1; }
 
 struct AttentionArgs {
     QgKv kv;
@@ -90,6 +92,18 @@ __device__ inline rsrc_t buffer_of(const void *p, uint32_t bytes)
     return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000);
 }
 
+// Cells are read once, so they need not stay in the caches.
+template <bool ONCE, typename T>
+__device__ inline T load_cells(const char *p)
+{
+    if constexpr (ONCE) {
+        typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
+        return __builtin_bit_cast(T, __builtin_nontemporal_load((const words *)p));
+    } else {
+        return *(const T *)p;
+    }
+}
+
 __device__ inline float across_quads_max(float v)
 {
     v = fmaxf(v, __shfl_xor(v, 16));
@@ -129,25 +143,27 @@ struct Attend {
     static constexpr int LDS_DIMS = DPAD < 128 ? DPAD : 128;       // the wavefronts' sums are added 128 dims at a time
     static constexpr int LDS_ROW = LDS_DIMS + 4;
 
+    // whole lines are read past the caches' replacement order (16-bit cells: 273 us with ordinary loads, so 252); parts of lines, which
+    // several instructions ask for, are not (8-bit values and padded heads lose 10 % by it)
+    static constexpr bool ONCE_K = FULL, ONCE_V = FULL && !E4M3;
+
     u32x4 kr[2][K_LOADS];
     uint32_t vr[8][V_WORDS];
     float ks[8], vs[8];
-    Operand q[Q_PARTS][CHUNKS];
+    // q's operands wait in LDS, where the four wavefronts share them (in registers: up to 96 more)
+    static constexpr int Q_VECTORS = Q_PARTS * CHUNKS * 64;
     floatx4 o[DIMS];
     float m, l, factor;                                            // factor: of a score, for exp2
 
     // First dim of load c of a key's elements by the lanes of quad j (of 8 elements, or 16 bytes of e4m3).
     __device__ static int k_dim(int c, int j) { return E4M3 ? 64 * c + 16 * j : 32 * c + 8 * j; }
 
-    float x[CHUNKS][8];                                            // q on its way into the operands
-
-    // (most sequences' first loads: issued before what depends on the page ids, used after it)
-    __device__ void load_q(const AttentionArgs &a, int64_t b, int head, bool real, int j)
+    // Of q's CHUNKS operands a wavefront makes every fourth and puts its parts into LDS.
+    __device__ void share_q(const AttentionArgs &a, int64_t b, int head, bool real, u32x4 *shared_q, int wave, int lane)
     {
-        const int D = FULL ? DPAD : a.kv.head_dim;
+        const int D = FULL ? DPAD : a.kv.head_dim, j = lane >> 4;
         const char *row = (const char *)a.q + (b * a.q_stride + (int64_t)head * D) * (TYPE == QG_F32 ? 4 : 2);
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
+        auto load = [&](int c, float x[8]) {
             const int d = E4M3 ? k_dim(c / 2, j) + 8 * (c % 2) : k_dim(c, j);
             const bool some = real && (FULL || d < D);
             if constexpr (TYPE == QG_F32) {
@@ -157,43 +173,47 @@ struct Attend {
                     v[1] = *(const floatx4 *)(row + 4 * d + 16);
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[c][e] = v[e / 4][e % 4];
+                for (int e = 0; e < 8; ++e) x[e] = v[e / 4][e % 4];
             } else {
                 u32x4 v = {0, 0, 0, 0};
                 if (some) v = *(const u32x4 *)(row + 2 * d);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t bits = e % 2 ? v[e / 2] >> 16 : v[e / 2] & 0xffffu;
-                    x[c][e] = TYPE == QG_BF16 ? bf16_to_float(bits) : f16_to_float(bits);
+                    x[e] = TYPE == QG_BF16 ? bf16_to_float(bits) : f16_to_float(bits);
                 }
             }
-        }
-    }
-
-    __device__ void split_q(const AttentionArgs &a)
-    {
+        };
         factor = a.scale * 1.4426950408889634f;
+        int up = 0;
         if constexpr (F16) {
             // the largest element to [2^14, 2^15), so that what f16 cannot hold is below 2^-38 of it
-            float most = 0.0f;
+            float most = 0.0f, x[8];
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c)
+            for (int c = 0; c < CHUNKS; ++c) {
+                load(c, x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[c][e]));
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
+            }
             most = across_quads_max(most);
-            const int up = most > 0.0f && most < INFINITY ? 14 - ilogbf(most) : 0;
-#pragma unroll
-            for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[c][e] = ldexpf(x[c][e], up);
+            up = most > 0.0f && most < INFINITY ? 14 - ilogbf(most) : 0;
             factor = ldexpf(factor, -up);
         }
+        for (int c = wave; c < CHUNKS; c += WAVES) {
+            float x[8];
+            load(c, x);
+            if constexpr (F16) {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c)
+                for (int e = 0; e < 8; ++e) x[e] = ldexpf(x[e], up);
+            }
 #pragma unroll
-            for (int p = 0; p < Q_PARTS; ++p)
+            for (int p = 0; p < Q_PARTS; ++p) {
+                u32x4 part;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) q[p][c].r[e] = take_part<F16>(x[c][2 * e], x[c][2 * e + 1]);
+                for (int e = 0; e < 4; ++e) part[e] = take_part<F16>(x[2 * e], x[2 * e + 1]);
+                shared_q[(p * CHUNKS + c) * 64 + lane] = part;
+            }
+        }
     }
 
     __device__ void load_k(const AttentionArgs &a, const char *cell, int j)      // cell: of the lane's first key
@@ -206,13 +226,13 @@ struct Attend {
                 const int d = k_dim(c, j);
                 const char *p = cell + (4 * t * D + d) * SIZE;
                 if constexpr (FULL) {
-                    kr[t][c] = *(const u32x4 *)p;
+                    kr[t][c] = load_cells<ONCE_K, u32x4>(p);
                 } else if constexpr (E4M3) {
                     const uint2 none = {0, 0};
-                    const uint2 x = d < D ? *(const uint2 *)p : none, y = d + 8 < D ? *(const uint2 *)(p + 8) : none;
+                    const uint2 x = d < D ? load_cells<false, uint2>(p) : none, y = d + 8 < D ? load_cells<false, uint2>(p + 8) : none;
                     kr[t][c] = u32x4{x.x, x.y, y.x, y.y};
                 } else {
-                    kr[t][c] = d < D ? *(const u32x4 *)p : u32x4{0, 0, 0, 0};
+                    kr[t][c] = d < D ? load_cells<false, u32x4>(p) : u32x4{0, 0, 0, 0};
                 }
             }
     }
@@ -228,7 +248,7 @@ struct Attend {
             for (int h = 0; h < PIECES; ++h) {
                 const int d = 128 * h + PIECE * i;
                 raw x = raw{};
-                if (FULL || d < D) x = *(const raw *)(cell + (e * D + d) * SIZE);
+                if (FULL || d < D) x = load_cells<ONCE_V, raw>(cell + (e * D + d) * SIZE);
                 __builtin_memcpy(&vr[e][h * W], &x, sizeof x);
             }
     }
@@ -250,13 +270,21 @@ struct Attend {
         return __builtin_bit_cast(uint32_t, v);
     }
 
-    __device__ void scores(floatx4 s[2])
+    __device__ void scores(floatx4 s[2], const u32x4 *shared_q, int lane)
     {
+        asm volatile("" : "+v"(lane));                              // read anew for every tile, not kept in registers
+        s[0] = s[1] = floatx4{0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[t] = floatx4{0, 0, 0, 0};
+        for (int c = 0; c < CHUNKS; ++c) {
+            Operand part[Q_PARTS];
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
+            for (int p = 0; p < Q_PARTS; ++p) {
+                const u32x4 v = shared_q[(p * CHUNKS + c) * 64 + lane];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) part[p].r[r] = v[r];
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
                 Operand k;
                 if constexpr (E4M3) {
 #pragma unroll
@@ -266,7 +294,7 @@ struct Attend {
                     for (int r = 0; r < 4; ++r) k.r[r] = kr[t][c][r];
                 }
 #pragma unroll
-                for (int p = Q_PARTS - 1; p >= 0; --p) s[t] = mma<F16>(k, q[p][c], s[t]);
+                for (int p = Q_PARTS - 1; p >= 0; --p) s[t] = mma<F16>(k, part[p], s[t]);
             }
         }
     }
@@ -340,23 +368,56 @@ struct Attend {
     }
 };
 
-// Range of the flattened list of (sequence, key head, block of heads, span) that a worker takes.
-__device__ inline int64_t worker_begin(int64_t total, int worker, int workers) { return total * worker / workers; }
-__device__ inline int worker_of(int64_t total, int64_t at, int workers)
+// Sum of the values of the lanes up to this one.
+__device__ inline int sum_up_to_lane(int v)
 {
-    return (int)(((at + 1) * workers - 1) / total);                 // the last worker that begins at or before it
+#define QG_UP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+    QG_UP(0x111, 0xf) QG_UP(0x112, 0xf) QG_UP(0x114, 0xf) QG_UP(0x118, 0xf)          // row_shr 1, 2, 4, 8
+    QG_UP(0x142, 0xa) QG_UP(0x143, 0xc)                                            // row_bcast 15, 31
+#undef QG_UP
+    return v;
 }
 
+// n / d rounded up, for n below 2^16 and d below 2^8.
+__device__ inline uint32_t divided(uint32_t n, uint32_t d) { return d == 1 ? n : __umulhi(n + d - 1, 0xffffffffu / d + 1); }
+
+constexpr int FEW = 24;                    // spans for each worker up to which pieces are looked at
+
+// n / d, in 32 bits where they do (a division in 64 bits is a hundred instructions and more, all of them one after the other).
+__device__ inline int64_t quotient(int64_t n, int64_t d)
+{
+    return ((uint64_t)n | (uint64_t)d) >> 32 ? n / d : (int64_t)((uint32_t)n / (uint32_t)d);
+}
+
+// The list of units in as many runs as there are workers, the first `larger` of them a unit longer than the others.
+struct Runs {
+    int64_t size;
+    int larger;
+    __device__ Runs(int64_t total, int workers)
+    {
+        size = total == workers ? 1 : quotient(total, workers);
+        larger = (int)(total - size * workers);
+    }
+    __device__ int64_t begin(int worker) const { return size * worker + min(worker, larger); }
+    __device__ int of(int64_t unit) const
+    {
+        if (size == 1 && larger == 0) return (int)unit;
+        const int64_t cut = (size + 1) * larger;
+        return unit < cut ? (int)quotient(unit, size + 1) : larger + (int)quotient(unit - cut, size);
+    }
+};
+
 template <int TYPE, int CACHE, int DPAD, bool FULL>
-__global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(AttentionArgs a)
+__global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(AttentionArgs a)
 {
     typedef Attend<TYPE, CACHE, DPAD, FULL> A;
     // the wavefronts' sums [wavefront][head][LDS_ROW]; of a head's parts, the maxima [part][head]
-    constexpr int SHARED_FLOATS = WAVES * 16 * A::LDS_ROW > 16 * MAX_WORKERS ? WAVES * 16 * A::LDS_ROW : 16 * MAX_WORKERS;
+    constexpr int SHARED_FLOATS = WAVES * 16 * A::LDS_ROW;
     __shared__ float shared[SHARED_FLOATS];
+    __shared__ u32x4 shared_q[A::Q_VECTORS];
     __shared__ float wave_m[16][16], wave_l[16][16];
-    __shared__ int64_t found_before;
-    __shared__ int found_b, scan[WAVES], is_last;
+    __shared__ int is_last, found_b, wave_sums[2][WAVES];
+    __shared__ int64_t found_at;
     __shared__ float head_m[16], head_l[16];
     const rsrc_t parts = buffer_of(a.parts, a.parts_bytes);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, j = lane >> 4;
@@ -364,68 +425,94 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
     const int heads = a.kv.kv_heads * a.blocks;                     // blocks of heads of a sequence
     const int worker = blockIdx.x;
 
-    // spans of all sequences, and the sequence that this worker's part of them begins in (the batch 256 at a time)
-    int64_t total = 0;
-    int mine = 0, up_to_mine = 0;                                   // of the chunk at hand: spans of sequence tid, and with those before it
-    auto scan_chunk = [&](int b0) {
-        mine = up_to_mine = b0 + tid < a.batch ? keys_of(a, b0 + tid).spans : 0;
-        for (int off = 1; off < 64; off <<= 1) {
-            const int x = __shfl_up(up_to_mine, off);
-            if (lane >= off) up_to_mine += x;
-        }
-        if (lane == 63) scan[wave] = up_to_mine;
+    // The work is a list of units: sequence by sequence, block of heads by block of heads.  The lengths are gone over 256 sequences at a
+    // time, a lane each; unless the batch is larger, once.
+    int mine = 0, up_to_mine = 0, chunk = 0;                        // units of sequence tid of the chunk, of it and those before it, of the chunk
+    auto scan = [&](int n, int *of_waves) {
+        mine = n;
+        up_to_mine = sum_up_to_lane(n);
+        if (lane == 63) of_waves[wave] = up_to_mine;
         __syncthreads();
-        int all = 0;
+        chunk = 0;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            if (w < wave) up_to_mine += scan[w];
-            all += scan[w];
+            if (w < wave) up_to_mine += of_waves[w];
+            chunk += of_waves[w];
         }
-        return all;
     };
-    for (int b0 = 0; b0 < a.batch; b0 += 64 * WAVES) {
-        if (b0) __syncthreads();                                    // scan is free again
-        total += scan_chunk(b0);
+    auto spans_of = [&](int b) { return b < a.batch ? keys_of(a, b).spans : 0; };
+    scan(spans_of(tid), wave_sums[0]);
+    int64_t total = chunk;
+    for (int b0 = 256; b0 < a.batch; b0 += 256) {
+        __syncthreads();
+        scan(spans_of(b0 + tid), wave_sums[0]);
+        total += chunk;
     }
     total *= heads;
-    const int workers = total < gridDim.x ? (int)total : (int)gridDim.x;        // each has a span at least
-    if (worker >= workers) return;                                  // the whole workgroup
-    const int64_t begin_at = worker_begin(total, worker, workers), end_at = worker_begin(total, worker + 1, workers);
-    int64_t before = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 64 * WAVES) {
-        int all = 0;
-        if (a.batch > 64 * WAVES) {                                 // (else the only chunk is at hand)
+
+    // Two ways to cut it.  In equal runs of spans (piece = 0): a worker's run may end one head's keys and begin another's, and every such
+    // beginning (first page ids, first keys, adding up) costs 5 us, as much as some spans.  Or, where there is little to do, a unit is a
+    // piece of at most `piece` spans of one head's keys and every worker takes one: the longest take a little more, but each begins
+    // once.  (16 sequences of up to 2000 tokens, 8 key heads: 22.6 -> 21.1 us; 32 of up to 4093 in 8 bits: 34.6 -> 32.4)
+    int piece = 0;
+    const int64_t least = total <= gridDim.x ? 1 : quotient(total + gridDim.x - 1, gridDim.x);
+    if (a.batch <= 256 && least <= FEW) {
+        const uint32_t exact = (uint32_t)least, more = exact + 1 + exact / 4;
+        const int before_scan = mine;
+        scan((int)(divided(mine, exact) | divided(mine, more) << 16), wave_sums[1]);
+        const int low = chunk & 0xffff, high = chunk >> 16;
+        piece = low * heads <= (int)gridDim.x ? exact : high * heads <= (int)gridDim.x ? more : 0;
+        if (piece) {
+            const int shift = piece == (int)exact ? 0 : 16;
+            mine = mine >> shift & 0xffff;
+            up_to_mine = up_to_mine >> shift & 0xffff;
+            chunk = chunk >> shift & 0xffff;
+            total = (int64_t)chunk * heads;
+        } else {
             __syncthreads();
-            all = scan_chunk(b0);
+            scan(before_scan, wave_sums[0]);
+        }
+    }
+    auto units_of = [&](int spans) { return piece ? (int)divided(spans, piece) : spans; };
+    const int workers = total < gridDim.x ? (int)total : (int)gridDim.x;        // each has a unit at least
+    if (worker >= workers) return;                                  // the whole workgroup
+    const Runs runs(total, workers);
+    const int64_t begin_at = runs.begin(worker), end_at = runs.begin(worker + 1);
+
+    // the sequence that this worker's units begin in, and where that sequence's begin in the list
+    int64_t before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 256) {
+        if (a.batch > 256) {                                        // (else the only chunk is at hand)
+            __syncthreads();
+            scan(spans_of(b0 + tid), wave_sums[0]);
         }
         if (begin_at < (before + up_to_mine) * heads && begin_at >= (before + up_to_mine - mine) * heads) {
             found_b = b0 + tid;
-            found_before = (before + up_to_mine - mine) * heads;
+            found_at = (before + up_to_mine - mine) * heads;
         }
-        before += all;
+        before += chunk;
     }
     __syncthreads();
     int b = found_b;
-    int64_t sequence_at = found_before;                             // where sequence b's spans begin in the list
+    int64_t sequence_at = found_at;
+    b = __builtin_amdgcn_readfirstlane(b);
     Keys keys = keys_of(a, b);
 
     A t;
     for (int64_t at = begin_at; at < end_at;) {
-        while (at - sequence_at >= (int64_t)keys.spans * heads) {
-            sequence_at += (int64_t)keys.spans * heads;
+        int units = units_of(keys.spans);
+        while (at - sequence_at >= (int64_t)units * heads) {
+            sequence_at += (int64_t)units * heads;
             keys = keys_of(a, ++b);
+            units = units_of(keys.spans);
         }
-        const int hb = (int)((at - sequence_at) / keys.spans);      // key head and block of heads
-        const int64_t segment_at = sequence_at + (int64_t)hb * keys.spans;
-        const int from = (int)(at - segment_at);
-        const int to = (int)(end_at - segment_at < keys.spans ? end_at - segment_at : keys.spans);
+        const int hb = (int)quotient(at - sequence_at, units);           // key head and block of heads
+        const int64_t segment_at = sequence_at + (int64_t)hb * units;
+        const int unit = (int)(at - segment_at), past = (int)(end_at - segment_at < units ? end_at - segment_at : units);
+        const int from = piece ? (int)((uint32_t)(keys.spans * unit) / (uint32_t)units) : unit;
+        const int to = piece ? (int)((uint32_t)(keys.spans * past) / (uint32_t)units) : past;
         const int kv_head = hb / a.blocks, head0 = kv_head * a.group + (hb - kv_head * a.blocks) * 16;
         const int rows = min(16, a.group - (hb - kv_head * a.blocks) * 16);
-
-        t.m = -INFINITY;
-        t.l = 0.0f;
-#pragma unroll
-        for (int n = 0; n < A::DIMS; ++n) t.o[n] = floatx4{0, 0, 0, 0};
 
         // tiles of 32 keys: first, first + WAVES, ...
         const int first = from * WAVES + wave, end_key = min(keys.len, keys.base + to * SPAN);
@@ -447,26 +534,31 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
         };
         auto fetch_k = [&](int n) {
             t.load_k(a, (const char *)a.kv.k + cell_of(n, i >> 3, 8 * (i >> 2) + (i & 3)) * (D * A::SIZE), j);
-            if constexpr (A::E4M3) t.load_scales(t.ks, a.kv.k_scale + cell_of(n, j >> 1, 8 * j));
+            // (loads arrive in the order of their requests: scales are asked for before the values, which are used after them)
+            if constexpr (A::E4M3) {
+                const int64_t cell = cell_of(n, j >> 1, 8 * j);
+                t.load_scales(t.ks, a.kv.k_scale + cell);
+                t.load_scales(t.vs, a.kv.v_scale + cell);
+            }
         };
-        auto fetch_v = [&](int n) {
-            const int64_t cell = cell_of(n, j >> 1, 8 * j);
-            t.load_v(a, (const char *)a.kv.v + cell * (D * A::SIZE), i);
-            if constexpr (A::E4M3) t.load_scales(t.vs, a.kv.v_scale + cell);
-        };
+        auto fetch_v = [&](int n) { t.load_v(a, (const char *)a.kv.v + cell_of(n, j >> 1, 8 * j) * (D * A::SIZE), i); };
+        if (tiles) pages_from(0);
+        t.share_q(a, b, head0 + i, i < rows, shared_q, wave, lane);
         if (tiles) {
-            pages_from(0);
-            t.load_q(a, b, head0 + i, i < rows, j);
             fetch_k(0);
             fetch_v(0);
-            t.split_q(a);
         }
+        __syncthreads();
+        t.m = -INFINITY;
+        t.l = 0.0f;
+#pragma unroll
+        for (int n = 0; n < A::DIMS; ++n) t.o[n] = floatx4{0, 0, 0, 0};
         for (int n = 0; n < tiles; ++n) {
             floatx4 s[2];
             float p[8];
             const int tile_key = keys.base + 32 * (first + WAVES * n), key = tile_key + 8 * j;
             const bool whole = tile_key >= keys.begin && tile_key + 32 <= keys.len;
-            t.scores(s);
+            t.scores(s, shared_q, lane);
             if (whole) t.template soften<false>(s, p, key, keys.begin, keys.len);
             else t.template soften<true>(s, p, key, keys.begin, keys.len);
             if (n + 1 < tiles) {
@@ -545,7 +637,7 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
             // that of the worker that begins the head's keys: a worker begins at most one that it does not end.
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
-            const int w0 = worker_of(total, segment_at, workers), w1 = worker_of(total, segment_at + keys.spans - 1, workers);
+            const int w0 = runs.of(segment_at), w1 = runs.of(segment_at + units - 1);
             const int n = w1 - w0 + 1;
             if (tid == 0) {
                 const uint32_t was = __hip_atomic_fetch_add(a.arrived + w0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -555,6 +647,19 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
             __syncthreads();
             if (is_last) {
                 auto part_of = [&](int k) { return 4u * (2 * (w0 + k) + (k == 0)) * a.part_floats; };
+                // outputs, four dims a lane; where that leaves lanes over, several share the parts of one
+                const int quads = rows * D / 4;
+                int shares = 1;
+                while (2 * shares * quads <= 64 * WAVES) shares *= 2;
+                const int share = shares > 1 ? tid / quads : 0;
+                constexpr int AT_ONCE = 8;
+                u32x4 y[AT_ONCE];
+                auto request = [&](int k0, int x) {
+#pragma unroll
+                    for (int c = 0; c < AT_ONCE; ++c)
+                        if (k0 + c * shares < n) y[c] = __builtin_amdgcn_raw_buffer_load_b128(parts, part_of(k0 + c * shares) + 16 * x, 0, SC1);
+                };
+                if (share < shares) request(share, shares > 1 ? tid % quads : min(tid, quads - 1));       // on its way while the maxima are looked at
                 // maxima and sums of p: 16 lanes for each head, each over every 16th part, then over each other
                 {
                     const int row = tid & 15, share = tid >> 4;
@@ -563,7 +668,7 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
                         for (int k = share; k < n; k += 16) {
                             const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(parts, part_of(k) + 4 * (rows * D + 2 * row), 0, SC1);
                             const float m = __uint_as_float(x[0]), next = fmaxf(top, m);
-                            shared[k * 16 + row] = m;
+                            if (k * rows + row < SHARED_FLOATS) shared[k * rows + row] = m;
                             if (m != -INFINITY) sum_l = (top == -INFINITY ? 0.0f : sum_l * __builtin_amdgcn_exp2f(top - next)) +
                                                         __uint_as_float(x[1]) * __builtin_amdgcn_exp2f(m - next);
                             top = next;
@@ -581,27 +686,21 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
                     if (a.lse && tid < rows) a.lse[(int64_t)b * a.heads + head0 + tid] = sum_l == 0.0f ? -INFINITY : top * 0.6931471805599453f + logf(sum_l);
                 }
                 __syncthreads();
-                // outputs, four dims a lane; where that leaves lanes over, several share the parts of one
-                const int quads = rows * D / 4;
-                int shares = 1;
-                while (2 * shares * quads <= 64 * WAVES) shares *= 2;
                 for (int x0 = 0; x0 < quads; x0 += 64 * WAVES) {
-                    const int x = shares > 1 ? tid % quads : x0 + tid, share = shares > 1 ? tid / quads : 0;
+                    const int x = shares > 1 ? tid % quads : x0 + tid;
                     const bool mine = shares > 1 ? share < shares : x < quads;
                     const int row = mine ? x / (D / 4) : 0;
                     floatx4 v = {0, 0, 0, 0};
                     if (mine) {
                         const float top = head_m[row];
-                        constexpr int AT_ONCE = 8;
                         for (int k0 = share; k0 < n; k0 += AT_ONCE * shares) {
-                            u32x4 y[AT_ONCE];
-#pragma unroll
-                            for (int c = 0; c < AT_ONCE; ++c)
-                                if (k0 + c * shares < n) y[c] = __builtin_amdgcn_raw_buffer_load_b128(parts, part_of(k0 + c * shares) + 16 * x, 0, SC1);
+                            if (x0 || k0 != share) request(k0, x);
 #pragma unroll
                             for (int c = 0; c < AT_ONCE; ++c)
                                 if (k0 + c * shares < n) {
-                                    const float m = shared[(k0 + c * shares) * 16 + row];
+                                    const int at_m = (k0 + c * shares) * rows + row;
+                                    const float m = at_m < SHARED_FLOATS ? shared[at_m] : __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+                                                                                              parts, part_of(k0 + c * shares) + 4 * (rows * D + 2 * row), 0, SC1));
                                     v += (m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top)) * __builtin_bit_cast(floatx4, y[c]);
                                 }
                         }
@@ -623,13 +722,13 @@ __global__ __launch_bounds__(64 * WAVES, DPAD == 256 ? 1 : 2) void attend(Attent
             }
         }
         __syncthreads();
-        at = segment_at + to;
+        at = segment_at + past;
     }
 }
 
 int workers_for(int head_dim)
 {
-    const int n = qg_compute_units() * (head_dim > 128 ? 1 : 2);
+    const int n = qg_compute_units() * groups_per_unit(head_dim);
     return n < MAX_WORKERS ? n : MAX_WORKERS;
 }
 
