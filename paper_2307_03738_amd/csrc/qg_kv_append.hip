@@ -13,7 +13,7 @@ struct AppendArgs {
     int heads, rope_dim, interleaved;
 };
 
-// One wavefront per token and head of q, k or v.
+// Heads whose rotation does not come in eights (the kernel below takes the others): one wavefront per token and head of q, k or v.
 template <int TYPE, int CACHE>
 __global__ __launch_bounds__(256) void append_heads(AppendArgs a)
 {
@@ -67,16 +67,101 @@ __global__ __launch_bounds__(256) void append_heads(AppendArgs a)
             store_float<CACHE>(is_v ? a.kv.v : a.kv.k, cell * D + lane + 64 * c, CACHE == QG_E4M3 ? limit_e4m3(x[c] / scale) : x[c]);
 }
 
+// A team of 1, 2, 4 ... 32 lanes, eight neighbouring elements each, takes heads of q, k and v of one token in turn and keeps the position's
+// cosines and sines in registers.  Memory bounds it: every element crosses once, the pair's other half a second time from the caches.
+template <int TYPE, int CACHE>
+__global__ __launch_bounds__(256) void append_eights(AppendArgs a, int team_shift)
+{
+    const int64_t token = blockIdx.x;
+    const int team = 1 << team_shift, teams = 256 >> team_shift, i = 8 * (threadIdx.x & (team - 1));
+    const int D = a.kv.head_dim, items = a.heads + 2 * a.kv.kv_heads, half = a.rope_dim / 2;
+    const int64_t position = a.positions[token];
+    int64_t page = qg_page_of(a.kv, a.rows[token], position);
+    if (a.rope_dim && position >= a.cos_sin_rows) page = -1;
+    const bool real = i < D, turned = i < a.rope_dim, second = i >= half;
+    float cosine[8], sine[8];
+    if (turned && page >= 0) {
+        const float *angle = a.cos_sin + position * a.rope_dim;
+        if (a.interleaved) {                                        // four pairs
+            const float4 c = *(const float4 *)(angle + i / 2), s = *(const float4 *)(angle + half + i / 2);
+            cosine[0] = c.x; cosine[1] = c.y; cosine[2] = c.z; cosine[3] = c.w;
+            sine[0] = s.x; sine[1] = s.y; sine[2] = s.z; sine[3] = s.w;
+        } else {
+            load_eight<QG_F32>(angle, second ? i - half : i, cosine);
+            load_eight<QG_F32>(angle, second ? i : i + half, sine);
+            if (!second) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sine[e] = -sine[e];
+            }
+        }
+    }
+    const int64_t cell0 = page * a.kv.kv_heads * a.kv.page + (position & (a.kv.page - 1));
+    // (all lanes of a wavefront go round as often: the largest of a team is found across lanes)
+    for (int item0 = blockIdx.y * teams; item0 < items; item0 += gridDim.y * teams) {
+        const int item = item0 + (threadIdx.x >> team_shift);
+        const bool mine = real && item < items, is_q = item < a.heads, is_v = item >= a.heads + a.kv.kv_heads;
+        const int head = is_q ? item : is_v ? item - a.heads - a.kv.kv_heads : item - a.heads;
+        const void *src = is_q ? a.q : is_v ? a.v : a.k;
+        const int64_t at = token * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (int64_t)head * D;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+        if (mine && page >= 0) {
+            load_eight<TYPE>(src, at + i, x);
+            if (turned && !is_v) {
+                if (a.interleaved) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float u = x[2 * e], w = x[2 * e + 1];
+                        x[2 * e] = u * cosine[e] - w * sine[e];
+                        x[2 * e + 1] = w * cosine[e] + u * sine[e];
+                    }
+                } else {
+                    float other[8];
+                    load_eight<TYPE>(src, at + (second ? i - half : i + half), other);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = x[e] * cosine[e] + other[e] * sine[e];
+                }
+            }
+        }
+        if (mine && is_q) store_eight<TYPE>(a.q_out, (token * a.heads + head) * D + i, x);
+        if (page < 0) continue;                                     // (of the whole workgroup: its token)
+        const int64_t cell = cell0 + (int64_t)head * a.kv.page;
+        if constexpr (CACHE == QG_E4M3) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, magnitude_bits(x[e]));
+            const float scale = e4m3_scale(most_of(most, team));
+            if (mine && !is_q && i == 0) (is_v ? a.kv.v_scale : a.kv.k_scale)[cell] = scale;
+            scale_eight(x, scale);
+        }
+        if (mine && !is_q) store_eight<CACHE>(is_v ? a.kv.v : a.kv.k, cell * D + i, x);
+    }
+}
+
+template <int TYPE, int CACHE>
+int launch_heads(int64_t tokens, const AppendArgs &a, hipStream_t st)
+{
+    const int items = a.heads + 2 * a.kv.kv_heads, D = a.kv.head_dim;
+    if (a.rope_dim % (a.interleaved ? 8 : 16) == 0 && qg_aligned16(a.cos_sin)) {
+        int shift = 0;
+        while ((8 << shift) < D) ++shift;
+        // a workgroup takes all heads of a token (its angles are loaded once), or, where tokens are few, as many as it has teams
+        const int teams = 256 >> shift, most = (items + teams - 1) / teams;
+        const int64_t want = 4 * (int64_t)qg_compute_units() / tokens;
+        const dim3 grid((unsigned)tokens, (unsigned)(want < 1 ? 1 : want < most ? want : most));
+        hipLaunchKernelGGL((append_eights<TYPE, CACHE>), grid, dim3(256), 0, st, a, shift);
+    } else {
+        hipLaunchKernelGGL((append_heads<TYPE, CACHE>), dim3((unsigned)tokens, (unsigned)((items + 3) / 4)), dim3(256), 0, st, a);
+    }
+    return qg_launch_status();
+}
+
 template <int TYPE>
 int launch_append(int64_t tokens, const AppendArgs &a, hipStream_t st)
 {
-    const dim3 grid((unsigned)tokens, (unsigned)((a.heads + 2 * a.kv.kv_heads + 3) / 4));
-    switch (a.kv.type) {
-    case QG_BF16: hipLaunchKernelGGL((append_heads<TYPE, QG_BF16>), grid, dim3(256), 0, st, a); break;
-    case QG_F16: hipLaunchKernelGGL((append_heads<TYPE, QG_F16>), grid, dim3(256), 0, st, a); break;
-    default: hipLaunchKernelGGL((append_heads<TYPE, QG_E4M3>), grid, dim3(256), 0, st, a); break;
-    }
-    return qg_launch_status();
+    return a.kv.type == QG_BF16 ? launch_heads<TYPE, QG_BF16>(tokens, a, st) : a.kv.type == QG_F16 ? launch_heads<TYPE, QG_F16>(tokens, a, st)
+                                                                                                  : launch_heads<TYPE, QG_E4M3>(tokens, a, st);
 }
 
 }  // namespace

@@ -70,47 +70,6 @@ __global__ __launch_bounds__(256) void norm_rows(NormArgs a, int weight_type)
     }
 }
 
-// Eight neighbouring elements as floats, and back.
-template <int TYPE>
-__device__ inline void load_eight(const void *p, int64_t i, float *v)
-{
-    if constexpr (TYPE == QG_F32) {
-        const float4 a = ((const float4 *)((const float *)p + i))[0], b = ((const float4 *)((const float *)p + i))[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-        const uint4 a = *(const uint4 *)((const uint16_t *)p + i);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t bits = e % 2 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu;
-            v[e] = TYPE == QG_BF16 ? bf16_to_float(bits) : f16_to_float(bits);
-        }
-    }
-}
-
-template <int TYPE>
-__device__ inline void store_eight(void *p, int64_t i, const float *v)
-{
-    if constexpr (TYPE == QG_F32) {
-        ((float4 *)((float *)p + i))[0] = make_float4(v[0], v[1], v[2], v[3]);
-        ((float4 *)((float *)p + i))[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else if constexpr (TYPE == QG_E4M3) {
-        uint32_t w[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) w[e] = floats_to_e4m3x2(v[4 * e], v[4 * e + 1]) | floats_to_e4m3x2(v[4 * e + 2], v[4 * e + 3]) << 16;
-        *(uint2 *)((uint8_t *)p + i) = make_uint2(w[0], w[1]);
-    } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            w[e] = TYPE == QG_BF16 ? float_to_bf16(v[2 * e]) | float_to_bf16(v[2 * e + 1]) << 16 : float_to_f16(v[2 * e]) | float_to_f16(v[2 * e + 1]) << 16;
-        *(uint4 *)((uint16_t *)p + i) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-}
-
-template <int CTRL, int ROWS>
-__device__ inline uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
-
 // Sum of a wavefront, in its last lane.
 __device__ inline float sum_of_wave(float v)
 {
@@ -118,25 +77,6 @@ __device__ inline float sum_of_wave(float v)
     QG_UP(0x111, 0xf) QG_UP(0x112, 0xf) QG_UP(0x114, 0xf) QG_UP(0x118, 0xf)          // row_shr 1, 2, 4, 8
     QG_UP(0x142, 0xa) QG_UP(0x143, 0xc)                                            // row_bcast 15, 31
 #undef QG_UP
-    return v;
-}
-
-// Largest of `lanes` (1, 2, 4 ... 64) neighbouring lanes, in all of them: exchanges inside a row of 16 lanes on the vector ALU (pairs, quads,
-// mirrored halves and rows), rows by lane exchanges.
-__device__ inline uint32_t most_of(uint32_t v, int lanes)
-{
-    if (lanes >= 2) v = max(v, dpp<0xb1, 0xf>(v));
-    if (lanes >= 4) v = max(v, dpp<0x4e, 0xf>(v));
-    if (lanes >= 8) v = max(v, dpp<0x141, 0xf>(v));
-    if (lanes >= 16) v = max(v, dpp<0x140, 0xf>(v));
-    if (lanes >= 32) {
-        const auto x = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-        v = max(x[0], x[1]);
-    }
-    if (lanes >= 64) {
-        const auto x = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-        v = max(x[0], x[1]);
-    }
     return v;
 }
 
@@ -234,16 +174,7 @@ __global__ __launch_bounds__(1024, 4) void norm_rows8(NormArgs a, int weight_typ
                     top = most_of(most[c], a.group / 8);
                 const float scale = e4m3_scale(top);
                 if (a.group != K && at[c] < K && row < rows && at[c] % a.group == 0) a.scales[row * (K / a.group) + at[c] / a.group] = scale;
-                // y / scale by its reciprocal: off by a rounding, which moves a code only where y / scale is that close to the middle of
-                // two; tiny scales, whose reciprocal overflows, divide, and NaN goes that way too
-                const float inverse = __builtin_amdgcn_rcpf(scale);
-                if (__any(!(scale >= 1e-37f))) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) h[c][e] = limit_e4m3(h[c][e] / scale);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) h[c][e] = __builtin_amdgcn_fmed3f(h[c][e] * inverse, -QG_E4M3_MOST, QG_E4M3_MOST);
-                }
+                scale_eight(h[c], scale);
             }
         }
         if (row < rows) {
