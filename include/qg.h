@@ -399,7 +399,7 @@ size_t qg_paged_attention_workspace_bytes(int batch, int heads, int kv_heads, in
 
 /* The pages' book of a batch: tables [rows][max_pages] of page ids (-1: none), lens [rows], and for each page of the pool how many
  * table entries (and other holders) refer to it; 0 is free.  Every call reads one book and writes another.  `out` pointers
- * may be the book's own (not in qg_pages_fork). */
+ * may be the book's own (tables and lens both or neither; not in qg_pages_fork). */
 typedef struct qg_page_book {
     const int32_t *tables, *lens, *refs;          /* [rows][max_pages], [rows], [pages] */
     int32_t *tables_out, *lens_out, *refs_out;

@@ -48,17 +48,19 @@ __device__ inline int before_me(int v, int *part, int *all)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int s = v;
-    for (int off = 1; off < 64; off <<= 1) {
-        const int o = __shfl_up(s, off);
-        if (lane >= off) s += o;
-    }
+#define QG_UP(CTRL, ROWS) s += __builtin_amdgcn_update_dpp(0, s, CTRL, ROWS, 0xf, false);
+    QG_UP(0x111, 0xf) QG_UP(0x112, 0xf) QG_UP(0x114, 0xf) QG_UP(0x118, 0xf)          // row_shr 1, 2, 4, 8
+    QG_UP(0x142, 0xa) QG_UP(0x143, 0xc)                                            // row_bcast 15, 31
+#undef QG_UP
     __syncthreads();                    // part is free again
     if (lane == 63) part[wave] = s;
     __syncthreads();
     int base = 0, total = 0;
+#pragma unroll
     for (int w = 0; w < BOOK_LANES / 64; ++w) {
-        if (w < wave) base += part[w];
-        total += part[w];
+        const int x = part[w];
+        if (w < wave) base += x;
+        total += x;
     }
     *all = total;
     return base + s - v;
@@ -71,94 +73,203 @@ __device__ inline int pages_for(int len, int page, int most)
     return min((int)(((int64_t)max(len, 0) + page - 1) / page), most);
 }
 
-struct ResizeSpace {
-    int32_t *refs, *free, *start, *pairs, *count;
+// What a row's new length changes: pages [has, had) go, pages [had, has) come, and a row that grows inside its last page may need a copy of it.
+struct Change {
+    int had, has, len;
+    bool inside;
+    __device__ int gone() const { return max(had - has, 0); }
+    __device__ int more() const { return max(has - had, 0); }
 };
 
-// One workgroup keeps the whole book.
+__device__ inline Change change_of(const Book &b, const int32_t *new_lens, int row)
+{
+    const int limit = b.max_pages * b.page, old = min(max(b.lens[row], 0), limit), len = min(max(new_lens[row], 0), limit);
+    Change c;
+    c.had = pages_for(old, b.page, b.max_pages);
+    c.has = pages_for(len, b.page, b.max_pages);
+    c.len = len;
+    c.inside = len > old && old % b.page != 0;
+    return c;
+}
+
+struct ResizeSpace {
+    int32_t *free, *pairs, *count;
+};
+
+// The row that unit e belongs to, where row r's units begin at at[r] (at[rows] is past e).
+__device__ inline int row_of(const int *at, int rows, int e)
+{
+    int low = 0, high = rows;
+    while (high - low > 1) {
+        const int mid = (low + high) / 2;
+        if (at[mid] <= e) low = mid;
+        else high = mid;
+    }
+    return low;
+}
+
+constexpr int FREE_IN_LDS = 4096;
+
+// Workgroup 0 keeps the book: pages that go and pages that come are dealt out over its lanes one by one, whatever their rows, so its time
+// follows what changes (and the references, which it passes on and searches for free pages from the lowest id on).  The other
+// workgroups pass on the table entries that do not change.  (One workgroup for all of it, an entry a lane: 33 us for 64 rows of 256 entries and
+// 8192 pages.)
 __global__ __launch_bounds__(BOOK_LANES) void resize_book(Book b, const int32_t *new_lens, ResizeSpace w, int32_t *lacking)
 {
-    __shared__ int part[BOOK_LANES / 64], copies;
     const int tid = threadIdx.x;
-    const int64_t entries = (int64_t)b.rows * b.max_pages;
-    const int limit = b.max_pages * b.page;
-    if (tid == 0) copies = 0;
-    for (int64_t p = tid; p < b.pages; p += BOOK_LANES) w.refs[p] = b.refs[p];
-    __syncthreads();
-    // references of the dropped pages
-    for (int64_t e = tid; e < entries; e += BOOK_LANES) {
+    if (blockIdx.x > 0) {
+        const int64_t entries = (int64_t)b.rows * b.max_pages;
+        const int64_t e = (int64_t)(blockIdx.x - 1) * BOOK_LANES + tid;
+        if (e >= entries) return;
         const int row = (int)(e / b.max_pages), column = (int)(e - (int64_t)row * b.max_pages);
-        const int had = pages_for(b.lens[row], b.page, b.max_pages), has = pages_for(new_lens[row], b.page, b.max_pages);
         const int32_t id = b.tables[e];
-        if (column >= has && column < had && id >= 0 && id < b.pages) atomicSub(&w.refs[id], 1);
+        const Change c = change_of(b, new_lens, row);
+        const bool changes = (column >= min(c.had, c.has) && column < max(c.had, c.has)) || (c.inside && column == c.had - 1);
+        if (!changes) b.tables_out[e] = id;
+        return;
     }
+    __shared__ int part[BOOK_LANES / 64], copies, at[BOOK_LANES + 1], low_free[FREE_IN_LDS];
+    __shared__ int16_t copied[BOOK_LANES];
+    if (tid == 0) copies = 0;
+    if (b.refs != b.refs_out) {
+        // (the references may be at any 4-byte address)
+        constexpr int AHEAD = 8;
+        for (int64_t p0 = 0; p0 < b.pages; p0 += AHEAD * BOOK_LANES) {
+            int32_t v[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) v[k] = p0 + k * BOOK_LANES + tid < b.pages ? b.refs[p0 + k * BOOK_LANES + tid] : 0;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (p0 + k * BOOK_LANES + tid < b.pages) b.refs_out[p0 + k * BOOK_LANES + tid] = v[k];
+        }
+    }
+    // pages that go, rows 1024 at a time: f(entry, page id) for each
+    auto for_gone = [&](auto f) {
+        for (int row0 = 0; row0 < b.rows; row0 += BOOK_LANES) {
+            const int rows = min(b.rows - row0, BOOK_LANES);
+            Change c = {};
+            if (tid < rows) c = change_of(b, new_lens, row0 + tid);
+            int all;
+            const int before = before_me(c.gone(), part, &all);
+            at[tid] = before;
+            __syncthreads();
+            for (int e = tid; e < all; e += BOOK_LANES) {
+                const int r = row_of(at, rows, e);
+                const Change of = change_of(b, new_lens, row0 + r);
+                const int64_t entry = (int64_t)(row0 + r) * b.max_pages + of.has + e - at[r];
+                f(entry, b.tables[entry]);
+            }
+            __syncthreads();
+        }
+    };
     __syncthreads();
-    // pages that each row needs, and where its share of the free ones begins
-    int need = 0;
-    for (int first = 0; first < b.rows; first += BOOK_LANES) {
-        const int row = first + tid;
-        int want = 0;
+    for_gone([&](int64_t, int32_t id) {
+        if (id >= 0 && id < b.pages) atomicSub(&b.refs_out[id], 1);
+    });
+    // pages that come: those of rows from row0 on begin at `base` in the list of free pages
+    auto wants = [&](int row0, int *before) {
+        const int row = row0 + tid;
+        int n = 0, copy = 0;
         if (row < b.rows) {
-            const int old = min(max(b.lens[row], 0), limit), len = min(max(new_lens[row], 0), limit);
-            const int had = pages_for(old, b.page, b.max_pages), has = pages_for(len, b.page, b.max_pages);
-            want = max(has - had, 0);
-            if (len > old && old % b.page) {
-                const int32_t id = b.tables[(int64_t)row * b.max_pages + had - 1];
-                if (id >= 0 && id < b.pages && seen(&w.refs[id]) > 1) want |= 1 << 30;
+            const Change c = change_of(b, new_lens, row);
+            n = c.more();
+            if (c.inside) {
+                const int32_t id = b.tables[(int64_t)row * b.max_pages + c.had - 1];
+                copy = id >= 0 && id < b.pages && seen(&b.refs_out[id]) > 1;
             }
         }
-        const int n = (want & ~(1 << 30)) + (want >> 30);
         int all;
-        const int before = before_me(n, part, &all);
-        if (row < b.rows) w.start[row] = (need + before) | (want & (1 << 30));
-        need += all;
-    }
-    // the lowest free pages
+        *before = before_me(n + copy, part, &all);
+        copied[tid] = (int16_t)copy;
+        return all;
+    };
+    int need = 0, before = 0;
+    for (int row0 = 0; row0 < b.rows; row0 += BOOK_LANES) need += wants(row0, &before);
+    // the lowest free pages, eight neighbouring ones a lane
     int found = 0;
-    for (int64_t first = 0; first < b.pages && found < need; first += BOOK_LANES) {
-        const int64_t p = first + tid;
-        const int is_free = p < b.pages && seen(&w.refs[p]) == 0;
+    for (int64_t p0 = 0; p0 < b.pages && found < need; p0 += 8 * BOOK_LANES) {
+        const int64_t p = p0 + 8 * tid;
+        int32_t v[8];
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = p + k < b.pages ? seen(&b.refs_out[p + k]) : 1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) n += v[k] == 0;
         int all;
-        const int at = found + before_me(is_free, part, &all);
-        if (is_free && at < need) w.free[at] = (int32_t)p;
+        int to = found + before_me(n, part, &all);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (v[k] == 0) {
+                if (to < need) {
+                    if (to < FREE_IN_LDS) low_free[to] = (int32_t)(p + k);
+                    else w.free[to] = (int32_t)(p + k);
+                }
+                ++to;
+            }
         found += all;
     }
     const bool enough = found >= need;
     if (tid == 0) *lacking = enough ? 0 : need - found;
-    __syncthreads();
-    for (int64_t p = tid; p < b.pages; p += BOOK_LANES) {
-        const int32_t v = enough ? seen(&w.refs[p]) : b.refs[p];
-        b.refs_out[p] = v;
-    }
-    __syncthreads();
-    // what is copied or shared: refs_out is only touched by atomics from here on
-    for (int64_t e = tid; e < entries; e += BOOK_LANES) {
-        const int row = (int)(e / b.max_pages), column = (int)(e - (int64_t)row * b.max_pages);
-        const int old = min(max(b.lens[row], 0), limit), len = min(max(new_lens[row], 0), limit);
-        const int had = pages_for(old, b.page, b.max_pages), has = pages_for(len, b.page, b.max_pages);
-        int32_t id = b.tables[e];
-        if (enough) {
-            const int start = w.start[row], copied = start >> 30;
-            const int from = start & ~(1 << 30);
-            if (column >= has && column < had) id = -1;
-            if (copied && column == had - 1) {
-                const int32_t fresh = w.free[from];
-                const int k = atomicAdd(&copies, 1);
-                w.pairs[2 * k] = id;
-                w.pairs[2 * k + 1] = fresh;
-                atomicSub(&b.refs_out[id], 1);
-                atomicAdd(&b.refs_out[fresh], 1);
-                id = fresh;
-            } else if (column >= had && column < has) {
-                id = w.free[from + copied + column - had];
-                atomicAdd(&b.refs_out[id], 1);
+    if (!enough) {
+        // as it was
+        for_gone([&](int64_t entry, int32_t id) {
+            if (id >= 0 && id < b.pages) atomicAdd(&b.refs_out[id], 1);
+            b.tables_out[entry] = id;
+        });
+        for (int row = tid; row < b.rows; row += BOOK_LANES) {
+            const Change c = change_of(b, new_lens, row);
+            const int64_t first = (int64_t)row * b.max_pages;
+            if (b.tables != b.tables_out) {
+                if (c.inside) b.tables_out[first + c.had - 1] = b.tables[first + c.had - 1];
+                for (int column = c.had; column < c.has; ++column) b.tables_out[first + column] = b.tables[first + column];
             }
         }
-        b.tables_out[e] = id;
+        if (b.lens != b.lens_out)
+            for (int row = tid; row < b.rows; row += BOOK_LANES) b.lens_out[row] = b.lens[row];
+        if (tid == 0) *w.count = 0;
+        return;
     }
-    __syncthreads();
-    if (tid == 0) *w.count = enough ? copies : 0;
-    for (int row = tid; row < b.rows; row += BOOK_LANES) b.lens_out[row] = enough ? min(max(new_lens[row], 0), limit) : b.lens[row];
+    int base = 0;
+    for (int row0 = 0; row0 < b.rows; row0 += BOOK_LANES) {
+        const int rows = min(b.rows - row0, BOOK_LANES);
+        int all;
+        if (b.rows > BOOK_LANES) {
+            // (the same answer as before: references of pages that are copied go down below, after all rows)
+            all = wants(row0, &before);
+        } else {
+            all = need;
+        }
+        at[tid] = before;
+        __syncthreads();
+        for (int e = tid; e < all; e += BOOK_LANES) {
+            const int r = row_of(at, rows, e), row = row0 + r;
+            const Change c = change_of(b, new_lens, row);
+            const int32_t fresh = base + e < FREE_IN_LDS ? low_free[base + e] : w.free[base + e];
+            const int k = e - at[r];
+            const int64_t first = (int64_t)row * b.max_pages;
+            if (copied[r] && k == 0) {
+                const int i = atomicAdd(&copies, 1);
+                w.pairs[2 * i] = b.tables[first + c.had - 1];
+                w.pairs[2 * i + 1] = fresh;
+                b.tables_out[first + c.had - 1] = fresh;
+            } else {
+                b.tables_out[first + c.had + k - copied[r]] = fresh;
+            }
+            b.refs_out[fresh] = 1;
+        }
+        if (b.tables != b.tables_out && tid < rows) {
+            const Change c = change_of(b, new_lens, row0 + tid);
+            const int64_t entry = (int64_t)(row0 + tid) * b.max_pages + c.had - 1;
+            if (c.inside && !copied[tid]) b.tables_out[entry] = b.tables[entry];
+        }
+        base += all;
+        __syncthreads();
+    }
+    // what the copies were taken of
+    for (int i = tid; i < copies; i += BOOK_LANES) atomicSub(&b.refs_out[w.pairs[2 * i]], 1);
+    for_gone([&](int64_t entry, int32_t) { b.tables_out[entry] = -1; });
+    for (int row = tid; row < b.rows; row += BOOK_LANES) b.lens_out[row] = change_of(b, new_lens, row).len;
+    if (tid == 0) *w.count = copies;
 }
 
 __global__ __launch_bounds__(256) void fork_refs(Book b)
@@ -187,38 +298,55 @@ struct CompactSpace {
     int32_t *map, *moved, *pairs, *count;
 };
 
+// One workgroup, eight neighbouring pages a lane: counts the pages in use, numbers the sources and targets (both in one sum: up to 8192
+// of each a turn), and leaves the new references and the map from old ids to new ones.  (A page a lane: 38 us for 16384 pages.)
 __global__ __launch_bounds__(BOOK_LANES) void compact_book(Book b, CompactSpace w, int32_t *live_out)
 {
     __shared__ int part[BOOK_LANES / 64];
     const int tid = threadIdx.x;
     int mine = 0, live;
-    for (int64_t p = tid; p < b.pages; p += BOOK_LANES) mine += b.refs[p] > 0;
+    int32_t v[8] = {};
+    auto load = [&](int64_t p) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = p + k < b.pages ? b.refs[p + k] : 0;
+    };
+    for (int64_t p = 8 * tid; p < b.pages; p += 8 * BOOK_LANES) {
+        load(p);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) mine += v[k] > 0;
+    }
     before_me(mine, part, &live);
     int sources = 0, targets = 0;
-    for (int64_t first = 0; first < b.pages; first += BOOK_LANES) {
-        const int64_t p = first + tid;
-        const int32_t r = p < b.pages ? b.refs[p] : 0;
-        const int target = p < live && r <= 0, source = p >= live && r > 0;
-        int all_t, all_s;
-        const int t = targets + before_me(target, part, &all_t), s = sources + before_me(source, part, &all_s);
-        if (target) w.pairs[2 * t + 1] = (int32_t)p;
-        if (source) {
-            w.pairs[2 * s] = (int32_t)p;
-            w.moved[s] = r;
-        }
-        targets += all_t;
-        sources += all_s;
-    }
-    __syncthreads();
-    for (int64_t p = tid; p < b.pages; p += BOOK_LANES) {
-        w.map[p] = (int32_t)p;
-        const int32_t r = b.refs[p];
-        b.refs_out[p] = p < live ? r : 0;
+    for (int64_t p0 = 0; p0 < b.pages; p0 += 8 * BOOK_LANES) {
+        const int64_t p = p0 + 8 * tid;
+        if (b.pages > 8 * BOOK_LANES) load(p);
+        int n = 0, all;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) n += p + k < live ? v[k] <= 0 : v[k] > 0 ? 1 << 16 : 0;
+        const int first = before_me(n, part, &all);
+        int t = targets + (first & 0xffff), s = sources + (first >> 16);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (p + k < live) {
+                if (v[k] <= 0) w.pairs[2 * t++ + 1] = (int32_t)(p + k);
+            } else if (v[k] > 0) {
+                w.moved[s] = v[k];
+                w.pairs[2 * s++] = (int32_t)(p + k);
+            }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (p + k < b.pages) {
+                w.map[p + k] = (int32_t)(p + k);
+                b.refs_out[p + k] = p + k < live ? v[k] : 0;
+            }
+        targets += all & 0xffff;
+        sources += all >> 16;
     }
     __syncthreads();
     for (int i = tid; i < sources; i += BOOK_LANES) {
-        w.map[w.pairs[2 * i]] = w.pairs[2 * i + 1];
-        b.refs_out[w.pairs[2 * i + 1]] = w.moved[i];
+        const int32_t from = w.pairs[2 * i], to = w.pairs[2 * i + 1];
+        w.map[from] = to;
+        b.refs_out[to] = w.moved[i];
     }
     if (tid == 0) {
         *w.count = sources;
@@ -316,13 +444,15 @@ extern "C" int qg_pages_resize(const qg_page_book *book, const int32_t *new_lens
     if (rc != QG_OK) return rc;
     if ((rc = check_planes(planes, n_planes, &p)) != QG_OK) return rc;
     if ((b.rows && !new_lens) || !lacking) return QG_ERR_NULL;
+    if ((b.tables == b.tables_out) != (b.lens == b.lens_out)) return QG_ERR_UNSUPPORTED;        // (one is read while the other is written)
     if (((uintptr_t)new_lens & 3) || ((uintptr_t)lacking & 3) || !qg_aligned16(workspace)) return QG_ERR_ALIGN;
     if (!workspace || workspace_bytes < qg_pages_workspace_bytes(b.rows, b.max_pages, b.pages)) return QG_ERR_WORKSPACE;
     set_layers(&p, b.pages);
     int32_t *w = (int32_t *)workspace;
-    const ResizeSpace space = {w + 64, w + 64 + b.pages, w + 64 + 2 * b.pages, w + 64 + 2 * b.pages + b.rows, w};
+    const ResizeSpace space = {w + 64, w + 64 + b.pages, w};
     hipStream_t st = (hipStream_t)stream;
-    hipLaunchKernelGGL(resize_book, dim3(1), dim3(BOOK_LANES), 0, st, b, new_lens, space, lacking);
+    const int64_t passed_on = b.tables == b.tables_out ? 0 : ((int64_t)b.rows * b.max_pages + BOOK_LANES - 1) / BOOK_LANES;
+    hipLaunchKernelGGL(resize_book, dim3((unsigned)(1 + passed_on)), dim3(BOOK_LANES), 0, st, b, new_lens, space, lacking);
     if ((rc = qg_launch_status()) != QG_OK) return rc;
     return launch_copies(p, space.pairs, space.count, b.rows, b.pages, st);
 }
