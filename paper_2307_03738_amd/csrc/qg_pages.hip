@@ -13,11 +13,23 @@ struct Planes {
     } p[QG_MAX_PLANES];
 };
 
-constexpr int COPY_UNIT = 4096;         // bytes: 256 lanes of 16
+constexpr int COPY_UNIT = 8192;         // bytes: 256 lanes of 2 x 16
 
-// Copies pages[i][0] onto pages[i][1] for i below the count; a workgroup takes units of 4 KB, all over the list.
-__global__ __launch_bounds__(256) void copy_pages(Planes planes, const int32_t *pairs, const int32_t *count, int most, int64_t pages)
+// Table entries that follow their pages' move (entries 0: none).
+struct Renumber {
+    const int32_t *tables, *map;
+    int32_t *tables_out;
+    int64_t entries;
+};
+
+// Copies pages[i][0] onto pages[i][1] for i below the count; a workgroup takes units of 8 KB, all over the list.  (5.3 TB/s read and written on
+// 720 MB, the rate of a large copy.)
+__global__ __launch_bounds__(256) void copy_pages(Planes planes, const int32_t *pairs, const int32_t *count, int most, int64_t pages, Renumber ids)
 {
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < ids.entries; e += (int64_t)gridDim.x * 256) {
+        const int32_t id = ids.tables[e];
+        ids.tables_out[e] = id >= 0 && id < pages ? ids.map[id] : id;
+    }
     const int64_t units = (int64_t)(count ? min(*count, most) : most) * planes.units;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int64_t pair = u / planes.units;
@@ -27,10 +39,13 @@ __global__ __launch_bounds__(256) void copy_pages(Planes planes, const int32_t *
         int k = 0;
         while (at >= planes.p[k].units) at -= planes.p[k++].units;
         const unsigned layer = at / planes.p[k].layer_units;
-        const int64_t offset = (int64_t)(at - layer * planes.p[k].layer_units) * COPY_UNIT + threadIdx.x * 16;
+        const int64_t bytes = planes.p[k].page_bytes, offset = (int64_t)(at - layer * planes.p[k].layer_units) * COPY_UNIT + threadIdx.x * 16;
         char *base = planes.p[k].base + layer * planes.p[k].layer_stride + offset;
-        if (offset < planes.p[k].page_bytes)
-            *(uint4 *)(base + to * planes.p[k].page_bytes) = *(const uint4 *)(base + from * planes.p[k].page_bytes);
+        uint4 x = {}, y = {};
+        if (offset < bytes) x = *(const uint4 *)(base + from * bytes);
+        if (offset + 4096 < bytes) y = *(const uint4 *)(base + from * bytes + 4096);
+        if (offset < bytes) *(uint4 *)(base + to * bytes) = x;
+        if (offset + 4096 < bytes) *(uint4 *)(base + to * bytes + 4096) = y;
     }
 }
 
@@ -72,6 +87,12 @@ __device__ inline int pages_for(int len, int page, int most)
 {
     return min((int)(((int64_t)max(len, 0) + page - 1) / page), most);
 }
+
+// Turns of 8192 pages: a wavefront takes 512 neighbouring ones, 64 at a time, and numbers them by the votes of its lanes, so that every
+// load and store is of neighbouring words.
+constexpr int TURN = 8 * BOOK_LANES;
+__device__ inline int64_t page_of_lane(int64_t p0, int k) { return p0 + (threadIdx.x >> 6) * 512 + k * 64 + (threadIdx.x & 63); }
+__device__ inline int votes_before(uint64_t votes) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(votes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)votes, 0)); }
 
 // What a row's new length changes: pages [has, had) go, pages [had, has) come, and a row that grows inside its last page may need a copy of it.
 struct Change {
@@ -130,6 +151,7 @@ __global__ __launch_bounds__(BOOK_LANES) void resize_book(Book b, const int32_t 
     }
     __shared__ int part[BOOK_LANES / 64], copies, at[BOOK_LANES + 1], low_free[FREE_IN_LDS];
     __shared__ int16_t copied[BOOK_LANES];
+    __shared__ int had[BOOK_LANES], has[BOOK_LANES];               // of the 1024 rows at hand
     if (tid == 0) copies = 0;
     if (b.refs != b.refs_out) {
         // (the references may be at any 4-byte address)
@@ -151,12 +173,13 @@ __global__ __launch_bounds__(BOOK_LANES) void resize_book(Book b, const int32_t 
             if (tid < rows) c = change_of(b, new_lens, row0 + tid);
             int all;
             const int before = before_me(c.gone(), part, &all);
+            if (all == 0) continue;                                 // (of the whole workgroup)
             at[tid] = before;
+            has[tid] = c.has;
             __syncthreads();
             for (int e = tid; e < all; e += BOOK_LANES) {
                 const int r = row_of(at, rows, e);
-                const Change of = change_of(b, new_lens, row0 + r);
-                const int64_t entry = (int64_t)(row0 + r) * b.max_pages + of.has + e - at[r];
+                const int64_t entry = (int64_t)(row0 + r) * b.max_pages + has[r] + e - at[r];
                 f(entry, b.tables[entry]);
             }
             __syncthreads();
@@ -173,6 +196,7 @@ __global__ __launch_bounds__(BOOK_LANES) void resize_book(Book b, const int32_t 
         if (row < b.rows) {
             const Change c = change_of(b, new_lens, row);
             n = c.more();
+            had[tid] = c.had;
             if (c.inside) {
                 const int32_t id = b.tables[(int64_t)row * b.max_pages + c.had - 1];
                 copy = id >= 0 && id < b.pages && seen(&b.refs_out[id]) > 1;
@@ -185,27 +209,29 @@ __global__ __launch_bounds__(BOOK_LANES) void resize_book(Book b, const int32_t 
     };
     int need = 0, before = 0;
     for (int row0 = 0; row0 < b.rows; row0 += BOOK_LANES) need += wants(row0, &before);
-    // the lowest free pages, eight neighbouring ones a lane
+    // the lowest free pages
     int found = 0;
-    for (int64_t p0 = 0; p0 < b.pages && found < need; p0 += 8 * BOOK_LANES) {
-        const int64_t p = p0 + 8 * tid;
+    for (int64_t p0 = 0; p0 < b.pages && found < need; p0 += TURN) {
+        uint64_t is_free[8];
+        int n = 0, all;
         int32_t v[8];
-        int n = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = p + k < b.pages ? seen(&b.refs_out[p + k]) : 1;
+        for (int k = 0; k < 8; ++k) v[k] = page_of_lane(p0, k) < b.pages ? seen(&b.refs_out[page_of_lane(p0, k)]) : 1;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) n += v[k] == 0;
-        int all;
-        int to = found + before_me(n, part, &all);
+        for (int k = 0; k < 8; ++k) {
+            is_free[k] = __ballot(v[k] == 0);
+            n += __popcll(is_free[k]);
+        }
+        int to = found + __shfl(before_me((tid & 63) == 63 ? n : 0, part, &all), 63);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (v[k] == 0) {
-                if (to < need) {
-                    if (to < FREE_IN_LDS) low_free[to] = (int32_t)(p + k);
-                    else w.free[to] = (int32_t)(p + k);
-                }
-                ++to;
+        for (int k = 0; k < 8; ++k) {
+            const int i = to + votes_before(is_free[k]);
+            if (v[k] == 0 && i < need) {
+                if (i < FREE_IN_LDS) low_free[i] = (int32_t)page_of_lane(p0, k);
+                else w.free[i] = (int32_t)page_of_lane(p0, k);
             }
+            to += __popcll(is_free[k]);
+        }
         found += all;
     }
     const bool enough = found >= need;
@@ -243,17 +269,16 @@ __global__ __launch_bounds__(BOOK_LANES) void resize_book(Book b, const int32_t 
         __syncthreads();
         for (int e = tid; e < all; e += BOOK_LANES) {
             const int r = row_of(at, rows, e), row = row0 + r;
-            const Change c = change_of(b, new_lens, row);
             const int32_t fresh = base + e < FREE_IN_LDS ? low_free[base + e] : w.free[base + e];
             const int k = e - at[r];
-            const int64_t first = (int64_t)row * b.max_pages;
+            const int64_t first = (int64_t)row * b.max_pages + had[r];
             if (copied[r] && k == 0) {
                 const int i = atomicAdd(&copies, 1);
-                w.pairs[2 * i] = b.tables[first + c.had - 1];
+                w.pairs[2 * i] = b.tables[first - 1];
                 w.pairs[2 * i + 1] = fresh;
-                b.tables_out[first + c.had - 1] = fresh;
+                b.tables_out[first - 1] = fresh;
             } else {
-                b.tables_out[first + c.had + k - copied[r]] = fresh;
+                b.tables_out[first + k - copied[r]] = fresh;
             }
             b.refs_out[fresh] = 1;
         }
@@ -298,69 +323,68 @@ struct CompactSpace {
     int32_t *map, *moved, *pairs, *count;
 };
 
-// One workgroup, eight neighbouring pages a lane: counts the pages in use, numbers the sources and targets (both in one sum: up to 8192
-// of each a turn), and leaves the new references and the map from old ids to new ones.  (A page a lane: 38 us for 16384 pages.)
+// One workgroup: counts the pages in use, numbers the sources and the targets (both in one sum), and leaves the new references and the
+// map from old ids to new ones.  (A page a lane and two scans a turn: 38 us for 16384 pages.)
 __global__ __launch_bounds__(BOOK_LANES) void compact_book(Book b, CompactSpace w, int32_t *live_out)
 {
     __shared__ int part[BOOK_LANES / 64];
     const int tid = threadIdx.x;
     int mine = 0, live;
-    int32_t v[8] = {};
-    auto load = [&](int64_t p) {
+    int32_t v[8];
+    auto load = [&](int64_t p0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = p + k < b.pages ? b.refs[p + k] : 0;
+        for (int k = 0; k < 8; ++k) v[k] = page_of_lane(p0, k) < b.pages ? b.refs[page_of_lane(p0, k)] : 0;
     };
-    for (int64_t p = 8 * tid; p < b.pages; p += 8 * BOOK_LANES) {
-        load(p);
+    for (int64_t p0 = 0; p0 < b.pages; p0 += TURN) {
+        load(p0);
 #pragma unroll
         for (int k = 0; k < 8; ++k) mine += v[k] > 0;
     }
     before_me(mine, part, &live);
     int sources = 0, targets = 0;
-    for (int64_t p0 = 0; p0 < b.pages; p0 += 8 * BOOK_LANES) {
-        const int64_t p = p0 + 8 * tid;
-        if (b.pages > 8 * BOOK_LANES) load(p);
-        int n = 0, all;
+    for (int64_t p0 = 0; p0 < b.pages; p0 += TURN) {
+        if (b.pages > TURN) load(p0);
+        int n = 0, all;                                             // of the wavefront, in its last lane: targets, sources << 16
+        uint64_t target[8], source[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) n += p + k < live ? v[k] <= 0 : v[k] > 0 ? 1 << 16 : 0;
-        const int first = before_me(n, part, &all);
+        for (int k = 0; k < 8; ++k) {
+            const int64_t p = page_of_lane(p0, k);
+            target[k] = __ballot(p < live && v[k] <= 0);
+            source[k] = __ballot(p >= live && v[k] > 0);
+            n += __popcll(target[k]) | __popcll(source[k]) << 16;
+        }
+        const int first = __shfl(before_me((tid & 63) == 63 ? n : 0, part, &all), 63);
         int t = targets + (first & 0xffff), s = sources + (first >> 16);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (p + k < live) {
-                if (v[k] <= 0) w.pairs[2 * t++ + 1] = (int32_t)(p + k);
-            } else if (v[k] > 0) {
-                w.moved[s] = v[k];
-                w.pairs[2 * s++] = (int32_t)(p + k);
+        for (int k = 0; k < 8; ++k) {
+            const int64_t p = page_of_lane(p0, k);
+            if (p < live && v[k] <= 0) w.pairs[2 * (t + votes_before(target[k])) + 1] = (int32_t)p;
+            if (p >= live && v[k] > 0) {
+                const int i = s + votes_before(source[k]);
+                w.moved[i] = v[k];
+                w.pairs[2 * i] = (int32_t)p;
             }
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (p + k < b.pages) {
-                w.map[p + k] = (int32_t)(p + k);
-                b.refs_out[p + k] = p + k < live ? v[k] : 0;
+            if (p < b.pages) {
+                w.map[p] = (int32_t)p;
+                b.refs_out[p] = p < live ? v[k] : 0;
             }
+            t += __popcll(target[k]);
+            s += __popcll(source[k]);
+        }
         targets += all & 0xffff;
         sources += all >> 16;
     }
     __syncthreads();
+#pragma unroll 4
     for (int i = tid; i < sources; i += BOOK_LANES) {
-        const int32_t from = w.pairs[2 * i], to = w.pairs[2 * i + 1];
+        const int32_t from = w.pairs[2 * i], to = w.pairs[2 * i + 1], refs = w.moved[i];
         w.map[from] = to;
-        b.refs_out[to] = w.moved[i];
+        b.refs_out[to] = refs;
     }
     if (tid == 0) {
         *w.count = sources;
         *live_out = live;
     }
-}
-
-__global__ __launch_bounds__(256) void compact_tables(Book b, const int32_t *map)
-{
-    const int64_t entries = (int64_t)b.rows * b.max_pages;
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= entries) return;
-    const int32_t id = b.tables[e];
-    b.tables_out[e] = id >= 0 && id < b.pages ? map[id] : id;
 }
 
 int check_planes(const qg_page_plane *planes, int n, Planes *out)
@@ -392,11 +416,12 @@ void set_layers(Planes *p, int64_t pages)
     for (int i = 0; i < p->n; ++i) p->p[i].layer_stride = pages * p->p[i].page_bytes;
 }
 
-int launch_copies(const Planes &planes, const int32_t *pairs, const int32_t *count, int most, int64_t pages, hipStream_t st)
+int launch_copies(const Planes &planes, const int32_t *pairs, const int32_t *count, int most, int64_t pages, const Renumber &ids, hipStream_t st)
 {
-    if (planes.n == 0 || most == 0) return QG_OK;
-    const int64_t units = (int64_t)most * planes.units, blocks = 16 * (int64_t)qg_compute_units();
-    hipLaunchKernelGGL(copy_pages, dim3((unsigned)(units < blocks ? units : blocks)), dim3(256), 0, st, planes, pairs, count, most, pages);
+    if ((planes.n == 0 || most == 0) && ids.entries == 0) return QG_OK;
+    const int64_t copies = (int64_t)most * planes.units, lanes = (ids.entries + 255) / 256, units = copies > lanes ? copies : lanes;
+    const int64_t blocks = 8 * (int64_t)qg_compute_units();
+    hipLaunchKernelGGL(copy_pages, dim3((unsigned)(units < blocks ? units : blocks)), dim3(256), 0, st, planes, pairs, count, most, pages, ids);
     return qg_launch_status();
 }
 
@@ -432,7 +457,7 @@ extern "C" int qg_pages_copy(const qg_page_plane *planes, int n_planes, int64_t 
     if (!pairs) return QG_ERR_NULL;
     if ((uintptr_t)pairs & 3) return QG_ERR_ALIGN;
     set_layers(&p, pages);
-    return launch_copies(p, pairs, nullptr, count, pages, (hipStream_t)stream);
+    return launch_copies(p, pairs, nullptr, count, pages, Renumber{}, (hipStream_t)stream);
 }
 
 extern "C" int qg_pages_resize(const qg_page_book *book, const int32_t *new_lens, const qg_page_plane *planes, int n_planes, int32_t *lacking,
@@ -454,7 +479,7 @@ extern "C" int qg_pages_resize(const qg_page_book *book, const int32_t *new_lens
     const int64_t passed_on = b.tables == b.tables_out ? 0 : ((int64_t)b.rows * b.max_pages + BOOK_LANES - 1) / BOOK_LANES;
     hipLaunchKernelGGL(resize_book, dim3((unsigned)(1 + passed_on)), dim3(BOOK_LANES), 0, st, b, new_lens, space, lacking);
     if ((rc = qg_launch_status()) != QG_OK) return rc;
-    return launch_copies(p, space.pairs, space.count, b.rows, b.pages, st);
+    return launch_copies(p, space.pairs, space.count, b.rows, b.pages, Renumber{}, st);
 }
 
 extern "C" int qg_pages_fork(const qg_page_book *book, const int32_t *parents, void *stream)
@@ -487,9 +512,7 @@ extern "C" int qg_pages_compact(const qg_page_book *book, const qg_page_plane *p
     const CompactSpace space = {w + 64, w + 64 + b.pages, w + 64 + 2 * b.pages, w};
     hipStream_t st = (hipStream_t)stream;
     hipLaunchKernelGGL(compact_book, dim3(1), dim3(BOOK_LANES), 0, st, b, space, live);
-    if (b.rows)
-        hipLaunchKernelGGL(compact_tables, dim3((unsigned)(((int64_t)b.rows * b.max_pages + 255) / 256)), dim3(256), 0, st, b, space.map);
     if ((rc = qg_launch_status()) != QG_OK) return rc;
     const int most = (int)(b.pages / 2 < 0x7fffffff ? b.pages / 2 : 0x7fffffff);
-    return launch_copies(p, space.pairs, space.count, most, b.pages, st);
+    return launch_copies(p, space.pairs, space.count, most, b.pages, Renumber{b.tables, space.map, b.tables_out, (int64_t)b.rows * b.max_pages}, st);
 }
