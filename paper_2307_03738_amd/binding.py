@@ -513,38 +513,35 @@ _BOOK = struct.Struct("6Qq3i4x").pack
 _PLANE = struct.Struct("Qqq").pack
 
 
-def _type(t: torch.Tensor, name: str, types=(torch.float32, torch.bfloat16, torch.float16)) -> int:
-    if t.dtype not in types:
+# A call of a few microseconds on the GPU must not take longer to describe: outputs that are made here are not looked at again, and
+# what every call asks of its tensors is asked once (norm of one row: 9.9 -> 8.3 us a call, 2.4 of them the launch).
+_FLOATS = {t: k for t, k in _TYPES.items() if k != QG_E4M3}
+_CELLS = {t: k for t, k in _TYPES.items() if k != QG_F32}
+
+
+def _type(t: torch.Tensor, name: str, types=_FLOATS) -> int:
+    kind = types.get(t.dtype)
+    if kind is None:
         raise ValueError(f"{name}: expected one of {', '.join(map(str, types))}, got {t.dtype}")
-    return _TYPES[t.dtype]
-
-
-def _gpu(t: torch.Tensor, name: str, shape=None) -> torch.Tensor:
     if not t.is_cuda:
         raise ValueError(f"{name}: expected a tensor on the GPU")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t
+    return kind
 
 
 def _whole(t: torch.Tensor, dtype, name: str, shape) -> int:
-    _dev(t, dtype, name)
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the GPU")
     return t.data_ptr()
 
 
-def _heads(t: torch.Tensor, name: str, shape) -> int:
-    """Address of a [tokens][heads][head_dim] tensor whose tokens may lie apart (a part of a stacked product's output)."""
-    _gpu(t, name, shape)
-    stride = t.stride()
-    if stride[2] != 1 and shape[2] != 1 or stride[1] != shape[2] and shape[1] != 1:
+def _heads(t: torch.Tensor, dtype, name: str, shape):
+    """Address and stride of a [tokens][heads][head_dim] tensor whose tokens may lie apart (a part of a stacked product's output)."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
+        raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the GPU")
+    token, head, element = t.stride()
+    if element != 1 or (head != shape[2] and shape[1] != 1):
         raise ValueError(f"{name}: the heads of a token have to lie together")
-    return t.data_ptr()
-
-
-def _ptr(t: Optional[torch.Tensor]) -> int:
-    return 0 if t is None else t.data_ptr()
+    return t.data_ptr(), token
 
 
 def qg_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: Optional[torch.Tensor] = None,
@@ -553,39 +550,53 @@ def qg_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residu
     """(y, h, scales) of rows x [rows][K]: h = x + residual in x's type (None without a residual), y its norm times the
     weight in `dtype` (x's own if not given); torch.float8_e4m3fn comes with scales [rows][K / group] (group 0: one for a
     row), other types with None.  x and residual may have rows that lie apart; h may be either."""
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError("x: expected [rows][K]")
-    rows, K = x.shape
-    kind = _type(_gpu(x, "x"), "x")
-    if dtype is None:
-        dtype = x.dtype if y is None else y.dtype
-    if dtype not in _TYPES:
-        raise ValueError(f"dtype: {dtype} is not supported")
-    if x.stride(1) != 1 and K > 1:
+    rows, K = shape
+    kind, device = _type(x, "x"), x.device
+    xstride, element = x.stride()
+    if element != 1 and K > 1:
         raise ValueError("x: expected contiguous rows")
-    wkind = _type(_dev(weight, weight.dtype, "weight"), "weight")
+    wkind = _type(weight, "weight")
     if weight.shape != (K,) or group < 0 or (group and K % group):
         _check(2, "qg_rms_norm")
-    e4m3 = dtype is _E4M3
-    y = _rows(rows, K, dtype, x.device) if y is None else y
-    yp = _whole(y, dtype, "y", (rows, K))
+    if not weight.is_contiguous():
+        raise ValueError("weight: expected a contiguous tensor")
+    if dtype is None:
+        dtype = x.dtype if y is None else y.dtype
+    ykind = _TYPES.get(dtype)
+    if ykind is None:
+        raise ValueError(f"dtype: {dtype} is not supported")
+    if y is None:
+        y = _rows(rows, K, dtype, device)
+    else:
+        _whole(y, dtype, "y", shape)
     hp = rp = rstride = sp = 0
     if residual is not None:
-        _gpu(residual, "residual", x.shape)
-        if residual.dtype != x.dtype or (residual.stride(1) != 1 and K > 1):
-            raise ValueError("residual: expected x's type and contiguous rows")
-        h = _rows(rows, K, x.dtype, x.device) if h is None else h
-        hp, rp, rstride = _whole(h, x.dtype, "h", (rows, K)), residual.data_ptr(), residual.stride(0)
+        if residual.dtype is not x.dtype or residual.shape != shape or not residual.is_cuda:
+            raise ValueError(f"residual: expected a {x.dtype} tensor of shape {tuple(shape)} on the GPU")
+        rstride, element = residual.stride()
+        if element != 1 and K > 1:
+            raise ValueError("residual: expected contiguous rows")
+        if h is None:
+            h = _rows(rows, K, x.dtype, device)
+        else:
+            _whole(h, x.dtype, "h", shape)
+        hp, rp = h.data_ptr(), residual.data_ptr()
     elif h is not None:
         raise ValueError("h: there is none without a residual")
-    if e4m3:
+    if ykind == QG_E4M3:
         groups = K // group if group else 1
-        scales = _rows(rows, groups, torch.float32, x.device) if scales is None else scales
-        sp = _whole(scales, torch.float32, "scales", (rows, groups))
+        if scales is None:
+            scales = _rows(rows, groups, torch.float32, device)
+        else:
+            _whole(scales, torch.float32, "scales", (rows, groups))
+        sp = scales.data_ptr()
     elif scales is not None:
         raise ValueError("scales: float8_e4m3fn only")
-    rc = (_LIB or lib()).qg_rms_norm(_NORM(x.data_ptr(), rp, weight.data_ptr(), hp, yp, sp, rows, K, x.stride(0), rstride,
-                                           kind, wkind, _TYPES[dtype], group, eps), _stream())
+    rc = (_LIB or lib()).qg_rms_norm(_NORM(x.data_ptr(), rp, weight.data_ptr(), hp, y.data_ptr(), sp, rows, K, xstride, rstride,
+                                           kind, wkind, ykind, group, eps), _stream())
     if rc != 0:
         _check(rc, "qg_rms_norm")
     return y, h, scales
@@ -594,19 +605,23 @@ def qg_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residu
 def _cache(k, v, tables, k_scale, v_scale):
     """The packed members of a qg_kv_cache, checked."""
     shape = k.shape
-    kind = _type(_dev(k, k.dtype, "k"), "k", (torch.bfloat16, torch.float16, _E4M3))
-    if len(shape) != 4:
-        raise ValueError("k: expected [pages][kv_heads][page][head_dim]")
-    vp = _whole(v, k.dtype, "v", shape)
+    kind = _type(k, "k", _CELLS)
+    if len(shape) != 4 or not k.is_contiguous():
+        raise ValueError("k: expected a contiguous tensor [pages][kv_heads][page][head_dim]")
     ksp = vsp = 0
     if kind == QG_E4M3:
         if k_scale is None or v_scale is None:
             raise ValueError("k_scale, v_scale: a cache in float8_e4m3fn has them")
         ksp, vsp = _whole(k_scale, torch.float32, "k_scale", shape[:3]), _whole(v_scale, torch.float32, "v_scale", shape[:3])
-    if not tables.is_cuda or tables.dtype != torch.int32 or tables.dim() != 2 or (tables.stride(1) != 1 and tables.shape[1] > 1):
-        raise ValueError("tables: expected an int32 tensor [rows][max_pages] on the GPU, rows contiguous")
-    return (k.data_ptr(), vp, ksp, vsp, tables.data_ptr(), tables.stride(0), shape[0], tables.shape[0], tables.shape[1], shape[1], shape[2],
-            shape[3], kind)
+    tshape = tables.shape
+    if tables.dtype is not torch.int32 or not tables.is_cuda or len(tshape) != 2:
+        raise ValueError("tables: expected an int32 tensor [rows][max_pages] on the GPU")
+    tstride, element = tables.stride()
+    if element != 1 and tshape[1] > 1:
+        raise ValueError("tables: expected contiguous rows")
+    pages, kv_heads, page, head_dim = shape
+    return (k.data_ptr(), _whole(v, k.dtype, "v", shape), ksp, vsp, tables.data_ptr(), tstride, pages, tshape[0], tshape[1], kv_heads, page,
+            head_dim, kind)
 
 
 def qg_kv_append(k_cache: torch.Tensor, v_cache: torch.Tensor, tables: torch.Tensor, rows: torch.Tensor, positions: torch.Tensor,
@@ -618,24 +633,29 @@ def qg_kv_append(k_cache: torch.Tensor, v_cache: torch.Tensor, tables: torch.Ten
     or position without a page (row -1, say) is padding."""
     cache = _cache(k_cache, v_cache, tables, k_scale, v_scale)
     kv_heads, D = cache[9], cache[11]
-    tokens, heads, qp, qs, qop = k.shape[0], 0, 0, 0, 0
+    tokens, dtype = k.shape[0], k.dtype
     kind = _type(k, "k")
-    kp, vp = _heads(k, "k", (tokens, kv_heads, D)), _heads(v, "v", (tokens, kv_heads, D))
-    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
-        raise ValueError("q, k, v: expected one type")
+    heads = qp = qs = qop = 0
+    kp, ks = _heads(k, dtype, "k", (tokens, kv_heads, D))
+    vp, vs = _heads(v, dtype, "v", (tokens, kv_heads, D))
     if q is not None:
-        heads = q.shape[1] if q.dim() == 3 else 0
-        qp, qs = _heads(q, "q", (tokens, heads, D)), q.stride(0)
+        if q.dim() != 3:
+            raise ValueError("q: expected [tokens][heads][head_dim]")
+        heads = q.shape[1]
+        qp, qs = _heads(q, dtype, "q", (tokens, heads, D))
         if q_out is None:
-            q_out = torch.empty_strided((tokens, heads, D), (heads * D, D, 1), dtype=q.dtype, device=q.device)
-        qop = _whole(q_out, q.dtype, "q_out", (tokens, heads, D))
+            q_out = torch.empty_strided((tokens, heads, D), (heads * D, D, 1), dtype=dtype, device=q.device)
+        else:
+            _whole(q_out, dtype, "q_out", (tokens, heads, D))
+        qop = q_out.data_ptr()
     rp, pp = _whole(rows, torch.int32, "rows", (tokens,)), _whole(positions, torch.int32, "positions", (tokens,))
     cp = rope = angles = 0
     if cos_sin is not None:
         if cos_sin.dim() != 2:
             raise ValueError("cos_sin: expected [positions][rope_dim]")
-        cp, angles, rope = _dev(cos_sin, torch.float32, "cos_sin").data_ptr(), cos_sin.shape[0], cos_sin.shape[1]
-    rc = (_LIB or lib()).qg_kv_append(_APPEND(*cache, rp, pp, qp, kp, vp, qop, cp, tokens, qs, k.stride(0), v.stride(0), angles,
+        angles, rope = cos_sin.shape
+        cp = _whole(cos_sin, torch.float32, "cos_sin", (angles, rope))
+    rc = (_LIB or lib()).qg_kv_append(_APPEND(*cache, rp, pp, qp, kp, vp, qop, cp, tokens, qs, ks, vs, angles,
                                               kind, heads, rope, 1 if interleaved else 0), _stream())
     if rc != 0:
         _check(rc, "qg_kv_append")
@@ -653,25 +673,30 @@ def qg_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
     """(out, lse) of one new token q [batch][heads][head_dim] of each sequence over its cells [max(first, lens - window), lens)
     of the cache.  lse [batch][heads] is written if asked for by True or handed in, otherwise None."""
     cache = _cache(k_cache, v_cache, tables, k_scale, v_scale)
-    if q.dim() != 3:
+    shape = q.shape
+    if len(shape) != 3:
         raise ValueError("q: expected [batch][heads][head_dim]")
-    batch, heads, D = q.shape
+    batch, heads, D = shape
+    dtype, device = q.dtype, q.device
     kind = _type(q, "q")
-    qp = _heads(q, "q", (batch, heads, cache[11]))
+    qp, qs = _heads(q, dtype, "q", (batch, heads, cache[11]))
     if out is None:
-        out = torch.empty_strided((batch, heads, D), (heads * D, D, 1), dtype=q.dtype, device=q.device)
-    op = _whole(out, q.dtype, "out", (batch, heads, D))
+        out = torch.empty_strided((batch, heads, D), (heads * D, D, 1), dtype=dtype, device=device)
+    else:
+        _whole(out, dtype, "out", shape)
     lp = _whole(lens, torch.int32, "lens", (batch,))
     fp = 0 if first is None else _whole(first, torch.int32, "first", (batch,))
     if lse is True:
-        lse = _rows(batch, heads, torch.float32, q.device)
-    elif lse is False:
-        lse = None
-    ep = 0 if lse is None else _whole(lse, torch.float32, "lse", (batch, heads))
+        lse = _rows(batch, heads, torch.float32, device)
+        ep = lse.data_ptr()
+    elif lse is False or lse is None:
+        lse, ep = None, 0
+    else:
+        ep = _whole(lse, torch.float32, "lse", (batch, heads))
     L = _LIB or lib()
     if workspace is None:
-        workspace = new_workspace(L.qg_paged_attention_workspace_bytes(batch, heads, cache[9], D), q.device)
-    rc = L.qg_paged_attention(_ATTENTION(*cache, lp, fp, qp, op, ep, q.stride(0), batch, heads, kind, window, scale,
+        workspace = new_workspace(L.qg_paged_attention_workspace_bytes(batch, heads, cache[9], D), device)
+    rc = L.qg_paged_attention(_ATTENTION(*cache, lp, fp, qp, out.data_ptr(), ep, qs, batch, heads, kind, window, scale,
                                          workspace.data_ptr(), workspace.numel() * workspace.element_size()), _stream())
     if rc != 0:
         _check(rc, "qg_paged_attention")
@@ -686,28 +711,37 @@ def _planes(planes, pages: int) -> bytes:
     """Tensors [layers][pages][...] whose pages move with the book, packed as qg_page_plane."""
     packed = b""
     for t in planes:
-        if not t.is_cuda or not t.is_contiguous() or t.dim() < 3 or t.shape[1] != pages:
+        shape = t.shape
+        if len(shape) < 3 or shape[1] != pages or not t.is_cuda or not t.is_contiguous():
             raise ValueError("planes: expected contiguous tensors [layers][pages][...] on the GPU")
-        packed += _PLANE(t.data_ptr(), t.shape[0], t.stride(1) * t.element_size())
+        packed += _PLANE(t.data_ptr(), shape[0], t.stride(1) * t.element_size())
     return packed
+
+
+def _ints(n: int, device) -> torch.Tensor:
+    return torch.empty_strided((n,), (1,), dtype=torch.int32, device=device)
 
 
 def _book(tables, lens, refs, page, out):
     """(packed qg_page_book, rows, max_pages, pages, tables_out, lens_out, refs_out)"""
-    if tables.dim() != 2:
-        raise ValueError("tables: expected [rows][max_pages]")
-    rows, columns = tables.shape
-    pages = refs.numel()
-    tp, rp = _dev(tables, torch.int32, "tables").data_ptr(), _whole(refs, torch.int32, "refs", (pages,))
-    lp = 0 if lens is None else _whole(lens, torch.int32, "lens", (rows,))
+    i32 = torch.int32
+    shape = tables.shape
+    if len(shape) != 2 or refs.dim() != 1:
+        raise ValueError("tables, refs: expected [rows][max_pages] and [pages]")
+    rows, columns = shape
+    pages = refs.shape[0]
+    tp, rp = _whole(tables, i32, "tables", shape), _whole(refs, i32, "refs", (pages,))
+    lp = 0 if lens is None else _whole(lens, i32, "lens", (rows,))
     if out is None:
         device = tables.device
-        out = (_rows(rows, columns, torch.int32, device), None if lens is None else torch.empty_strided((rows,), (1,), dtype=torch.int32, device=device),
-               torch.empty_strided((pages,), (1,), dtype=torch.int32, device=device))
-    t, n, r = out
-    packed = _BOOK(tp, lp, rp, _whole(t, torch.int32, "tables out", (rows, columns)), 0 if lens is None else _whole(n, torch.int32, "lens out", (rows,)),
-                   _whole(r, torch.int32, "refs out", (pages,)), pages, rows, columns, page)
-    return packed, rows, columns, pages, t, n, r
+        t, n, r = _rows(rows, columns, i32, device), None if lens is None else _ints(rows, device), _ints(pages, device)
+    else:
+        t, n, r = out
+        _whole(t, i32, "tables out", shape)
+        _whole(r, i32, "refs out", (pages,))
+        if lens is not None:
+            _whole(n, i32, "lens out", (rows,))
+    return _BOOK(tp, lp, rp, t.data_ptr(), 0 if n is None else n.data_ptr(), r.data_ptr(), pages, rows, columns, page), rows, columns, pages, t, n, r
 
 
 def qg_pages_resize(tables: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, page: int, new_lens: torch.Tensor,
@@ -718,11 +752,14 @@ def qg_pages_resize(tables: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor
     (then nothing changed).  out: (tables, lens, refs) to write into, the old ones for instance."""
     book, rows, columns, pages, t, n, r = _book(tables, lens, refs, page, out)
     np_ = _whole(new_lens, torch.int32, "new_lens", (rows,))
-    lacking = torch.empty_strided((1,), (1,), dtype=torch.int32, device=tables.device) if lacking is None else lacking
+    if lacking is None:
+        lacking = _ints(1, tables.device)
+    else:
+        _whole(lacking, torch.int32, "lacking", (1,))
     L = _LIB or lib()
     if workspace is None:
         workspace = _bytes(max(256, L.qg_pages_workspace_bytes(rows, columns, pages)), tables.device)
-    rc = L.qg_pages_resize(book, np_, _planes(planes, pages), len(planes), _whole(lacking, torch.int32, "lacking", (1,)),
+    rc = L.qg_pages_resize(book, np_, _planes(planes, pages), len(planes), lacking.data_ptr(),
                            workspace.data_ptr(), workspace.numel(), _stream())
     if rc != 0:
         _check(rc, "qg_pages_resize")
@@ -743,11 +780,14 @@ def qg_pages_compact(tables: torch.Tensor, refs: torch.Tensor, planes: Sequence[
     """(tables, refs, live) with the pages in use moved to the lower end of the pool in all planes; live [1]: how many
     there are.  out: (tables, refs) to write into, the old ones for instance."""
     book, rows, columns, pages, t, _, r = _book(tables, None, refs, 1, None if out is None else (out[0], None, out[1]))
-    live = torch.empty_strided((1,), (1,), dtype=torch.int32, device=tables.device) if live is None else live
+    if live is None:
+        live = _ints(1, tables.device)
+    else:
+        _whole(live, torch.int32, "live", (1,))
     L = _LIB or lib()
     if workspace is None:
         workspace = _bytes(max(256, L.qg_pages_workspace_bytes(rows, columns, pages)), tables.device)
-    rc = L.qg_pages_compact(book, _planes(planes, pages), len(planes), _whole(live, torch.int32, "live", (1,)),
+    rc = L.qg_pages_compact(book, _planes(planes, pages), len(planes), live.data_ptr(),
                             workspace.data_ptr(), workspace.numel(), _stream())
     if rc != 0:
         _check(rc, "qg_pages_compact")
