@@ -357,14 +357,15 @@ typedef struct qg_kv_cache {
  *   (a, b) -> (a cos - b sin, b cos + a sin),
  * the pair of angle j being elements j and j + rope_dim / 2, or 2 j and 2 j + 1 if interleaved.  A token whose row
  * or position has no page in the table (row or position < 0 or past the table, a page id that is none, a
- * position past cos_sin) is padding: nothing is stored for it, and its q comes out zero. */
+ * position past cos_sin) is padding: nothing is stored for it, and its q comes out zero.  Two tokens of one call must not have the
+ * same cell. */
 typedef struct qg_append_desc {
     qg_kv_cache cache;
     const int32_t *rows;       /* [tokens]: each token's row of the tables */
     const int32_t *positions;  /* [tokens] */
     const void *q, *k, *v;     /* [tokens][heads][head_dim] (q), [tokens][kv_heads][head_dim] of `type`, tokens *_stride apart;
                                   q may be NULL (heads 0).  16-byte aligned, strides multiples of 8 */
-    void *q_out;               /* [tokens][heads][head_dim] of `type` */
+    void *q_out;               /* [tokens][heads][head_dim] of `type`; not q itself */
     const float *cos_sin;      /* [cos_sin_rows][rope_dim]: rope_dim / 2 cosines, then as many sines; NULL if rope_dim is 0 */
     int64_t tokens, q_stride, k_stride, v_stride, cos_sin_rows;
     int type, heads, rope_dim, interleaved;
@@ -376,7 +377,7 @@ int qg_kv_append(const qg_append_desc *d /* HOST */, void *stream);
  *   out = sum_i p_i v_i / sum_i p_i,  p_i = exp(scale q.k_i),   lse = log sum_i p_i
  * A sequence without such a key has out = 0 and lse = -infinity.  What lies in cells outside that range is never
  * used, NaN included.  Sums, running maxima and the products' accumulators are fp32; q enters the matrix instructions
- * without loss and the p_i to 2^-16 of themselves or better.  Results are the same from run to run. */
+ * in parts that add up to it (in a QG_F16 cache to 2^-33 of it or 2^-39 of its head's largest) and the p_i to 2^-16 of themselves or better.  Results are the same from run to run. */
 typedef struct qg_attention_desc {
     qg_kv_cache cache;
     const int32_t *lens;    /* [batch]: cells in use (limited to max_pages * page); sequence b uses row b of the tables */

@@ -21,7 +21,7 @@ static inline int qg_check_cache(const qg_kv_cache &c, QgKv *kv)
     if (c.page < 16 || c.page > 4096 || (c.page & (c.page - 1))) return QG_ERR_UNSUPPORTED;
     if (c.head_dim < 8 || c.head_dim > 256 || c.head_dim % 8) return QG_ERR_UNSUPPORTED;
     if (c.rows < 0 || c.max_pages <= 0 || c.kv_heads <= 0 || c.kv_heads > QG_MAX_HEADS || c.pages <= 0 || c.pages > 0x7fffffff) return QG_ERR_SHAPE;
-    if ((int64_t)c.max_pages * c.page > 0x7fffffff) return QG_ERR_SHAPE;        // positions are 32-bit
+    if ((int64_t)c.max_pages * c.page > 0x7ffffe00) return QG_ERR_SHAPE;        // positions are 32-bit, with room to round up
     if (c.rows > 1 && c.table_stride < c.max_pages) return QG_ERR_SHAPE;
     if (!c.k || !c.v || !c.tables || (c.type == QG_E4M3 && (!c.k_scale || !c.v_scale))) return QG_ERR_NULL;
     if (!qg_aligned16(c.k) || !qg_aligned16(c.v) || !qg_aligned_to(c.tables, 4) || !qg_aligned16(c.k_scale) || !qg_aligned16(c.v_scale)) return QG_ERR_ALIGN;

@@ -184,6 +184,7 @@ extern "C" int qg_kv_append(const qg_append_desc *desc, void *stream)
     if (!qg_aligned16(d.k) || !qg_aligned16(d.v) || (d.heads && (!qg_aligned16(d.q) || !qg_aligned16(d.q_out))) || !qg_aligned_to(d.cos_sin, 4) ||
         !qg_aligned_to(d.rows, 4) || !qg_aligned_to(d.positions, 4) ||
         (d.tokens > 1 && (d.k_stride % 8 || d.v_stride % 8 || (d.heads && d.q_stride % 8)))) return QG_ERR_ALIGN;
+    if (d.heads && d.q == d.q_out) return QG_ERR_UNSUPPORTED;     // a lane reads what another has written
     const AppendArgs a = {kv, d.rows, d.positions, d.q, d.k, d.v, d.q_out, d.cos_sin, d.q_stride, d.k_stride, d.v_stride, d.cos_sin_rows,
                           d.heads, d.rope_dim, d.interleaved != 0};
     hipStream_t st = (hipStream_t)stream;

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 NORM = dict(x=64, residual=0, weight=64, h=0, y=64, scales=0, rows=2, K=64, x_stride=64, residual_stride=0, type=0, weight_type=0, y_type=0, group=0, eps=1e-5)
 CACHE = dict(k=64, v=64, k_scale=0, v_scale=0, tables=64, table_stride=4, pages=8, max_rows=2, max_pages=4, kv_heads=2, page=16, head_dim=64, cache_type=1)
-APPEND = dict(CACHE, rows=64, positions=64, q=64, new_k=64, new_v=64, q_out=64, cos_sin=64, tokens=3, q_stride=256, k_stride=128, v_stride=128, cos_sin_rows=9,
+APPEND = dict(CACHE, rows=64, positions=64, q=64, new_k=64, new_v=64, q_out=128, cos_sin=64, tokens=3, q_stride=256, k_stride=128, v_stride=128, cos_sin_rows=9,
               type=0, heads=4, rope_dim=64, interleaved=0)
 ATTENTION = dict(CACHE, lens=64, first=0, q=64, out=64, lse=0, q_stride=256, batch=2, heads=4, type=0, window=0, scale=1.0, workspace=64, workspace_bytes=1 << 40)
 BOOK = dict(tables=64, lens=64, refs=64, tables_out=128, lens_out=128, refs_out=128, pages=9, rows=2, max_pages=3, page=16)
@@ -63,7 +63,7 @@ BAD_CACHES = [
 @pytest.mark.parametrize("change,status", BAD_CACHES + [
     (dict(type=3), UNSUPPORTED), (dict(tokens=-1), SHAPE), (dict(rope_dim=63), SHAPE), (dict(rope_dim=66), SHAPE), (dict(heads=-1), SHAPE),
     (dict(q_stride=255), SHAPE), (dict(k_stride=120), SHAPE), (dict(rows=0), NULL), (dict(positions=0), NULL), (dict(new_k=0), NULL), (dict(q=0), NULL),
-    (dict(q_out=0), NULL), (dict(cos_sin=0), NULL), (dict(q=72), ALIGN), (dict(new_v=68), ALIGN), (dict(q_stride=260), ALIGN), (dict(tokens=0, rows=0, q=0), OK)])
+    (dict(q_out=0), NULL), (dict(q_out=128, q=128), UNSUPPORTED), (dict(cos_sin=0), NULL), (dict(q=72), ALIGN), (dict(new_v=68), ALIGN), (dict(q_stride=260), ALIGN), (dict(tokens=0, rows=0, q=0), OK)])
 def test_append_refuses(qg, change, status):
     assert qg.lib().qg_kv_append(qg._APPEND(*{**APPEND, **change}.values()), None) == status
 
@@ -107,6 +107,8 @@ def test_page_calls_refuse(qg):
     assert L.qg_pages_compact(book, b"", 0, None, 64, 1 << 40, None) == NULL
     assert L.qg_pages_compact(book, b"", 0, 64, None, 1 << 40, None) == WORKSPACE
     assert L.qg_pages_fork(book, None, None) == NULL
+    for half in ({"tables_out": 64}, {"lens_out": 64}):                    # tables and lens in place both or neither
+        assert L.qg_pages_resize(qg._BOOK(*{**BOOK, **half}.values()), 64, b"", 0, 64, 64, 1 << 40, None) == UNSUPPORTED
     assert L.qg_pages_fork(qg._BOOK(*{**BOOK, "refs_out": 64}.values()), 64, None) == UNSUPPORTED
     assert L.qg_pages_copy(plane(64, 1, 32), 1, 9, None, 3, None) == NULL
     assert L.qg_pages_copy(plane(64, 1, 32), 1, 9, 64, -1, None) == SHAPE
