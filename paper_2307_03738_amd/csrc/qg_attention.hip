@@ -348,16 +348,16 @@ struct Attend {
             Operand lower, upper;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                uint32_t x, y;
                 if constexpr (E4M3) {
-                    x = widen(vr[2 * r][n / 4], n % 4 != 0);
-                    y = widen(vr[2 * r + 1][n / 4], n % 4 != 0);
+                    // two dims of both keys in one word, side by side
+                    const uint32_t both = __builtin_amdgcn_perm(vr[2 * r + 1][n / 4], vr[2 * r][n / 4], n % 4 ? 0x07030602u : 0x05010400u);
+                    lower.r[r] = widen(both, false);
+                    upper.r[r] = widen(both, true);
                 } else {
-                    x = vr[2 * r][n / 2];
-                    y = vr[2 * r + 1][n / 2];
+                    const uint32_t x = vr[2 * r][n / 2], y = vr[2 * r + 1][n / 2];
+                    lower.r[r] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                    upper.r[r] = __builtin_amdgcn_perm(y, x, 0x07060302u);
                 }
-                lower.r[r] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                upper.r[r] = __builtin_amdgcn_perm(y, x, 0x07060302u);
             }
 #pragma unroll
             for (int k = P_PARTS - 1; k >= 0; --k) {
