@@ -11,10 +11,8 @@ static inline bool qg_aligned_to(const void *p, int bytes) { return ((uintptr_t)
 
 constexpr float QG_E4M3_MOST = 448.0f;
 
-// Vectors of N elements of 1, 2 or 4 bytes, loaded and stored as they lie in memory.
+// Vectors of 4, 8 or 16 bytes, loaded as they lie in memory.
 template <int BYTES> struct QgRaw;
-template <> struct QgRaw<1> { typedef uint8_t t; };
-template <> struct QgRaw<2> { typedef uint16_t t; };
 template <> struct QgRaw<4> { typedef uint32_t t; };
 template <> struct QgRaw<8> { typedef uint2 t; };
 template <> struct QgRaw<16> { typedef uint4 t; };
@@ -32,7 +30,6 @@ __device__ inline uint32_t floats_to_e4m3x2(float a, float b)
 {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xffffu;
 }
-__device__ inline float e4m3_to_float(uint32_t b) { return __builtin_amdgcn_cvt_f32_fp8((int)b, 0); }
 // NaN stays NaN
 __device__ inline float limit_e4m3(float v)
 {
@@ -44,8 +41,7 @@ __device__ inline float load_as_float(const void *p, int64_t i)
 {
     if constexpr (TYPE == QG_F32) return ((const float *)p)[i];
     else if constexpr (TYPE == QG_BF16) return bf16_to_float(((const uint16_t *)p)[i]);
-    else if constexpr (TYPE == QG_F16) return f16_to_float(((const uint16_t *)p)[i]);
-    else return e4m3_to_float(((const uint8_t *)p)[i]);
+    else return f16_to_float(((const uint16_t *)p)[i]);
 }
 
 template <int TYPE>

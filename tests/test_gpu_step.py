@@ -615,6 +615,68 @@ def test_copy_pages(qg):
     assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip(p, planes))
 
 
+def test_numbers_that_are_none_stay_with_their_head(qg):
+    # an 8-bit cell of a head with a NaN or infinity is NaN, scale and codes; its neighbours are as they would be; attention over such a
+    # cell is NaN for the heads that read it, and only where it is read
+    H, D, page = 3, 64, 16
+    k, v = (torch.zeros(4, H, page, D).to(F8).cuda() for _ in "kv")
+    ks, vs = (torch.ones(4, H, page).cuda() for _ in "kv")
+    t = torch.tensor([[2, 1]], dtype=torch.int32).cuda()
+    new = torch.randn(20, H, D, generator=gen(31))
+    new[5, 1, 7], new[9, 2, 60] = math.nan, math.inf
+    at = torch.arange(20, dtype=torch.int32).cuda()
+    qg.qg_kv_append(k, v, t, torch.zeros_like(at), at, new.cuda(), new.cuda(), k_scale=ks, v_scale=vs)
+    for cells, scales in ((k, ks), (v, vs)):
+        cells, scales = cells.cpu().float(), scales.cpu()
+        bad = torch.zeros(4, H, page, dtype=torch.bool)
+        bad[2, 1, 5] = bad[2, 2, 9] = True
+        assert torch.equal(torch.isnan(scales), bad) and torch.equal(torch.isnan(cells).all(-1), bad) and torch.equal(torch.isnan(cells).any(-1), bad)
+    q, n = torch.randn(1, H, D, generator=gen(32)).cuda(), torch.tensor([20], dtype=torch.int32).cuda()
+    for first, none in ((0, [False, True, True]), (6, [False, False, True]), (10, [False, False, False])):
+        out, lse = qg.qg_paged_attention(q, k, v, t, n, 0.1, first=torch.tensor([first], dtype=torch.int32).cuda(), k_scale=ks, v_scale=vs, lse=True)
+        assert torch.isnan(out[0]).all(-1).tolist() == none == torch.isnan(out[0]).any(-1).tolist() == torch.isnan(lse[0]).tolist()
+
+
+def test_books_in_a_graph(qg):
+    # a step, a fork and a compaction captured once and replayed on changing books, with the caller's own work in between
+    rows, columns, pages, page = 40, 12, 700, 16
+    planes = planes_of(8, pages)
+    held = [torch.from_numpy(a).cuda() for a in book(77, rows, columns, pages, page)]
+    p = up(*planes)
+    new, parents = torch.zeros(rows, dtype=torch.int32).cuda(), torch.zeros(rows, dtype=torch.int32).cuda()
+    space = torch.empty(qg.qg_pages_workspace_bytes(rows, columns, pages), dtype=torch.uint8, device="cuda")
+
+    def step():
+        t, n, f, lacking = qg.qg_pages_resize(*held, page, new, planes=p, workspace=space)
+        t, n, f = qg.qg_pages_fork(t, n, f, parents)
+        t, f, live = qg.qg_pages_compact(t, f, planes=p, workspace=space)
+        return t, n, f, lacking, live
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    r = np.random.default_rng(5)
+    for i in range(6):
+        new.copy_(torch.from_numpy(np.minimum(held[1].cpu().numpy() + r.integers(-3, 20, rows), columns * page).astype(np.int32)))
+        parents.copy_(torch.from_numpy(np.where(r.random(rows) < 0.8, np.arange(rows), r.integers(-1, rows, rows)).astype(np.int32)))
+        before = [t.clone() for t in p]
+        graph.replay()
+        torch.cuda.synchronize()
+        got, moved = [t.clone() for t in out], [t.clone() for t in p]
+        for a, b in zip(p, before):
+            a.copy_(b)
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and all(torch.equal(a, b) for a, b in zip(moved, p))
+        for a, b in zip(held, got):
+            a.copy_(b)
+
+
 # --- refusals of the Python entry points ------------------------------------------------------------------------
 
 def test_wrong_arguments_are_refused(qg):
