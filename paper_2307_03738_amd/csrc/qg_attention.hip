@@ -420,7 +420,7 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
     __shared__ float shared[SHARED_FLOATS];
     __shared__ u32x4 shared_q[A::Q_VECTORS];
     __shared__ float wave_m[16][16], wave_l[16][16];
-    __shared__ int is_last, found_b, wave_sums[2][WAVES];
+    __shared__ int is_last, found_b, wave_sums[3][WAVES];
     __shared__ int64_t found_at;
     __shared__ float head_m[16], head_l[16];
     const rsrc_t parts = buffer_of(a.parts, a.parts_bytes);
@@ -457,24 +457,29 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
     // Two ways to cut it.  In equal runs of spans (piece = 0): a worker's run may end one head's keys and begin another's, and every such
     // beginning (first page ids, first keys, adding up) costs 5 us, as much as some spans.  Or, where there is little to do, a unit is a
     // piece of at most `piece` spans of one head's keys and every worker takes one: the longest take a little more, but each begins
-    // once.  (16 sequences of up to 2000 tokens, 8 key heads: 22.6 -> 21.1 us; 32 of up to 4093 in 8 bits: 34.6 -> 32.4)
+    // once.  (16 sequences of up to 2000 tokens, 8 key heads: 22.6 -> 21.1 us; 32 of up to 4093 in 8 bits: 34.6 -> 30.8)
     int piece = 0;
     const int64_t least = total <= gridDim.x ? 1 : quotient(total + gridDim.x - 1, gridDim.x);
     if (a.batch <= 256 && least <= FEW) {
-        const uint32_t exact = (uint32_t)least, more = exact + 1 + exact / 4;
-        const int before_scan = mine;
-        scan((int)(divided(mine, exact) | divided(mine, more) << 16), wave_sums[1]);
-        const int low = chunk & 0xffff, high = chunk >> 16;
-        piece = low * heads <= (int)gridDim.x ? exact : high * heads <= (int)gridDim.x ? more : 0;
+        // the shortest of four pieces that workers suffice for; the units of two are added up in one word
+        const uint32_t exact = (uint32_t)least;
+        const int spans = mine;
+        int shift = 0;
+        for (int c = 0; c < 2 && !piece; ++c) {
+            const uint32_t shorter = exact + 2 * c, longer = c ? exact + 3 + exact / 4 : exact + 1;
+            scan((int)(divided(spans, shorter) | divided(spans, longer) << 16), wave_sums[1 + c]);
+            const int low = chunk & 0xffff, high = chunk >> 16;
+            piece = low * heads <= (int)gridDim.x ? shorter : high * heads <= (int)gridDim.x ? longer : 0;
+            shift = piece == (int)shorter ? 0 : 16;
+        }
         if (piece) {
-            const int shift = piece == (int)exact ? 0 : 16;
             mine = mine >> shift & 0xffff;
             up_to_mine = up_to_mine >> shift & 0xffff;
             chunk = chunk >> shift & 0xffff;
             total = (int64_t)chunk * heads;
         } else {
             __syncthreads();
-            scan(before_scan, wave_sums[0]);
+            scan(spans, wave_sums[0]);
         }
     }
     auto units_of = [&](int spans) { return piece ? (int)divided(spans, piece) : spans; };
