@@ -375,7 +375,7 @@ int qg_kv_append(const qg_append_desc *d /* HOST */, void *stream);
 /* Attention of one new token of each sequence over the cache.  Head h of `heads` reads key head
  * h / (heads / kv_heads).  With the keys i of [max(first, len - window), len):
  *   out = sum_i p_i v_i / sum_i p_i,  p_i = exp(scale q.k_i),   lse = log sum_i p_i
- * A sequence without such a key has out = 0 and lse = -infinity.  What lies in cells outside that range is never
+ * A sequence without such a key has out = 0 and lse = -infinity; a head whose scores are no numbers has NaN in both.  What lies in cells outside that range is never
  * used, NaN included.  Sums, running maxima and the products' accumulators are fp32; q enters the matrix instructions
  * in parts that add up to it (in a QG_F16 cache to 2^-33 of it or 2^-39 of its head's largest) and the p_i to 2^-16 of themselves or better.  Results are the same from run to run. */
 typedef struct qg_attention_desc {

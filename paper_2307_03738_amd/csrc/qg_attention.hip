@@ -108,6 +108,10 @@ __device__ inline T load_cells(const char *p)
     }
 }
 
+// What a sum of p relative to maximum m counts relative to maximum `top`.  Without a score above -infinity the sum is 0, or NaN where
+// scores were none, which has to come through.
+__device__ inline float weight_of(float m, float top) { return m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top); }
+
 __device__ inline float across_quads_max(float v)
 {
     v = fmaxf(v, __shfl_xor(v, 16));
@@ -621,7 +625,7 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
 #pragma unroll
                     for (int w = 0; w < WAVES; ++w) top = fmaxf(top, wave_m[w][row]);
 #pragma unroll
-                    for (int w = 0; w < WAVES; ++w) sum_l += wave_m[w][row] == -INFINITY ? 0.0f : wave_l[w][row] * __builtin_amdgcn_exp2f(wave_m[w][row] - top);
+                    for (int w = 0; w < WAVES; ++w) sum_l += wave_l[w][row] * weight_of(wave_m[w][row], top);
                     const int64_t at_out = ((int64_t)b * a.heads + head0 + row) * D + half * A::LDS_DIMS + d;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) store_float<TYPE>(a.out, at_out + k, sum_l == 0.0f ? 0.0f : v[k] / sum_l);
@@ -633,7 +637,7 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
         if (tid < rows) {
             float top = -INFINITY, sum_l = 0.0f;
             for (int w = 0; w < WAVES; ++w) top = fmaxf(top, wave_m[w][tid]);
-            for (int w = 0; w < WAVES; ++w) sum_l += wave_m[w][tid] == -INFINITY ? 0.0f : wave_l[w][tid] * __builtin_amdgcn_exp2f(wave_m[w][tid] - top);
+            for (int w = 0; w < WAVES; ++w) sum_l += wave_l[w][tid] * weight_of(wave_m[w][tid], top);
             if (whole) {
                 if (a.lse) a.lse[(int64_t)b * a.heads + head0 + tid] = sum_l == 0.0f ? -INFINITY : top * 0.6931471805599453f + logf(sum_l);
             } else {
@@ -678,8 +682,7 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
                             const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(parts, part_of(k) + 4 * (rows * D + 2 * row), 0, SC1);
                             const float m = __uint_as_float(x[0]), next = fmaxf(top, m);
                             if (k * rows + row < SHARED_FLOATS) shared[k * rows + row] = m;
-                            if (m != -INFINITY) sum_l = (top == -INFINITY ? 0.0f : sum_l * __builtin_amdgcn_exp2f(top - next)) +
-                                                        __uint_as_float(x[1]) * __builtin_amdgcn_exp2f(m - next);
+                            sum_l = sum_l * weight_of(top, next) + __uint_as_float(x[1]) * weight_of(m, next);
                             top = next;
                         }
                     wave_m[share][row] = top;
@@ -689,7 +692,7 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
                 if (tid < 16) {
                     float top = -INFINITY, sum_l = 0.0f;
                     for (int w = 0; w < 16; ++w) top = fmaxf(top, wave_m[w][tid]);
-                    for (int w = 0; w < 16; ++w) sum_l += wave_m[w][tid] == -INFINITY ? 0.0f : wave_l[w][tid] * __builtin_amdgcn_exp2f(wave_m[w][tid] - top);
+                    for (int w = 0; w < 16; ++w) sum_l += wave_l[w][tid] * weight_of(wave_m[w][tid], top);
                     head_m[tid] = top;
                     head_l[tid] = sum_l;
                     if (a.lse && tid < rows) a.lse[(int64_t)b * a.heads + head0 + tid] = sum_l == 0.0f ? -INFINITY : top * 0.6931471805599453f + logf(sum_l);

@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void append_heads(AppendArgs a)
 
 // A team of 1, 2, 4 ... 32 lanes, eight neighbouring elements each, takes heads of q, k and v of one token in turn and keeps the position's
 // cosines and sines in registers.  Memory bounds it: every element crosses once, the pair's other half a second time from the caches.
-// (8900 tokens of 64 + 16 heads of 128, bf16 into 8 bits: 53 us, 5.6 TB/s; a wavefront a head, an element at a time: 244.)
+// (7551 tokens of 64 + 16 heads of 128, bf16 into 8 bits: 53 us, 5.6 TB/s; a wavefront a head, an element at a time: 244.)
 template <int TYPE, int CACHE>
 __global__ __launch_bounds__(256) void append_eights(AppendArgs a, int team_shift)
 {

@@ -637,6 +637,23 @@ def test_numbers_that_are_none_stay_with_their_head(qg):
         assert torch.isnan(out[0]).all(-1).tolist() == none == torch.isnan(out[0]).any(-1).tolist() == torch.isnan(lse[0]).tolist()
 
 
+@pytest.mark.parametrize("lens", [[40, 7], [9000, 130]])
+def test_queries_that_are_no_numbers_come_out_as_none(qg, lens):
+    # a head whose q holds a NaN or an infinity has no score that is a number: its output is NaN, whether its keys are looked at by one
+    # workgroup or many; the other heads and sequences are as they would be
+    for ct in (torch.bfloat16, torch.float16):
+        k, v, _, _, tables, _, _ = cache_of(lens, 2, 64, 16, ct, gen(41))
+        q = torch.randn(2, 6, 64, generator=gen(42))
+        args = (k.cuda(), v.cuda(), tables.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), 0.1)
+        good, glse = qg.qg_paged_attention(q.cuda(), *args, lse=True)
+        q[0, 1, 5], q[0, 4], q[1, 3, 63] = math.nan, math.nan, math.inf
+        out, lse = qg.qg_paged_attention(q.cuda(), *args, lse=True)
+        none = torch.zeros(2, 6, dtype=torch.bool)
+        none[0, 1] = none[0, 4] = none[1, 3] = True
+        assert torch.equal(torch.isnan(out).all(-1).cpu(), none) and torch.equal(torch.isnan(lse).cpu(), none)
+        assert torch.equal(out.cpu()[~none], good.cpu()[~none]) and torch.equal(lse.cpu()[~none], glse.cpu()[~none])
+
+
 def test_books_in_a_graph(qg):
     # a step, a fork and a compaction captured once and replayed on changing books, with the caller's own work in between
     rows, columns, pages, page = 40, 12, 700, 16
