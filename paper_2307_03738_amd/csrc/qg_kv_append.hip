@@ -13,64 +13,11 @@ struct AppendArgs {
     int heads, rope_dim, interleaved;
 };
 
-// Heads whose rotation does not come in eights (the kernel below takes the others): one wavefront per token and head of q, k or v.
-template <int TYPE, int CACHE>
-__global__ __launch_bounds__(256) void append_heads(AppendArgs a)
-{
-    const int64_t token = blockIdx.x;
-    const int item = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int D = a.kv.head_dim, items = a.heads + 2 * a.kv.kv_heads;
-    if (item >= items) return;
-    const int64_t position = a.positions[token];
-    int64_t page = qg_page_of(a.kv, a.rows[token], position);
-    if (a.rope_dim && position >= a.cos_sin_rows) page = -1;
-    const bool is_q = item < a.heads, is_v = item >= a.heads + a.kv.kv_heads;
-    const int head = is_q ? item : is_v ? item - a.heads - a.kv.kv_heads : item - a.heads;
-    if (page < 0) {
-        if (is_q)
-            for (int i = lane; i < D; i += 64) store_float<TYPE>(a.q_out, (token * a.heads + head) * D + i, 0.0f);
-        return;
-    }
-    const void *src = is_q ? a.q : is_v ? a.v : a.k;
-    const int64_t at = token * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (int64_t)head * D;
-    const int half = a.rope_dim / 2;
-    const float *angle = a.cos_sin + (a.rope_dim ? position * a.rope_dim : 0);
-    float x[4];
-    for (int c = 0; c < 4; ++c) {
-        const int i = lane + 64 * c;
-        x[c] = 0.0f;
-        if (i >= D) continue;
-        x[c] = load_as_float<TYPE>(src, at + i);
-        if (is_v || i >= a.rope_dim) continue;
-        const int j = a.interleaved ? i >> 1 : i < half ? i : i - half;
-        const bool second = a.interleaved ? (i & 1) : i >= half;
-        const float other = load_as_float<TYPE>(src, at + (a.interleaved ? (i ^ 1) : second ? i - half : i + half));
-        const float cosine = angle[j], sine = angle[half + j];
-        x[c] = second ? x[c] * cosine + other * sine : x[c] * cosine - other * sine;
-    }
-    if (is_q) {
-        for (int c = 0; c < 4; ++c)
-            if (lane + 64 * c < D) store_float<TYPE>(a.q_out, (token * a.heads + head) * D + lane + 64 * c, x[c]);
-        return;
-    }
-    const int64_t cell = (page * a.kv.kv_heads + head) * a.kv.page + (position & (a.kv.page - 1));
-    float scale = 1.0f;
-    if constexpr (CACHE == QG_E4M3) {
-        uint32_t most = 0;
-        for (int c = 0; c < 4; ++c) most = max(most, magnitude_bits(x[c]));
-        for (int off = 32; off; off >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, off));
-        scale = e4m3_scale(most);
-        if (lane == 0) (is_v ? a.kv.v_scale : a.kv.k_scale)[cell] = scale;
-    }
-    for (int c = 0; c < 4; ++c)
-        if (lane + 64 * c < D)
-            store_float<CACHE>(is_v ? a.kv.v : a.kv.k, cell * D + lane + 64 * c, CACHE == QG_E4M3 ? limit_e4m3(x[c] / scale) : x[c]);
-}
-
 // A team of 1, 2, 4 ... 32 lanes, eight neighbouring elements each, takes heads of q, k and v of one token in turn and keeps the position's
 // cosines and sines in registers.  Memory bounds it: every element crosses once, the pair's other half a second time from the caches.
-// (7551 tokens of 64 + 16 heads of 128, bf16 into 8 bits: 53 us, 5.6 TB/s; a wavefront a head, an element at a time: 244.)
-template <int TYPE, int CACHE>
+// (7551 tokens of 64 + 16 heads of 128, bf16 into 8 bits: 53 us, 5.7 TB/s; a wavefront a head, an element at a time: 244.)
+// WHOLE: the rotated elements and their halves are whole eights (and the angles aligned); otherwise angles and partners are loaded one by one.
+template <int TYPE, int CACHE, bool WHOLE>
 __global__ __launch_bounds__(256) void append_eights(AppendArgs a, int team_shift)
 {
     const int64_t token = blockIdx.x;
@@ -83,7 +30,15 @@ __global__ __launch_bounds__(256) void append_eights(AppendArgs a, int team_shif
     float cosine[8], sine[8];
     if (turned && page >= 0) {
         const float *angle = a.cos_sin + position * a.rope_dim;
-        if (a.interleaved) {                                        // four pairs
+        if constexpr (!WHOLE) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = i + e, pair = a.interleaved ? k >> 1 : k < half ? k : k - half;
+                const bool late = a.interleaved ? k & 1 : k >= half;
+                cosine[e] = k < a.rope_dim ? angle[pair] : 1.0f;
+                sine[e] = k < a.rope_dim ? (late ? angle[half + pair] : -angle[half + pair]) : 0.0f;
+            }
+        } else if (a.interleaved) {                                 // four pairs
             const float4 c = *(const float4 *)(angle + i / 2), s = *(const float4 *)(angle + half + i / 2);
             cosine[0] = c.x; cosine[1] = c.y; cosine[2] = c.z; cosine[3] = c.w;
             sine[0] = s.x; sine[1] = s.y; sine[2] = s.z; sine[3] = s.w;
@@ -110,7 +65,16 @@ __global__ __launch_bounds__(256) void append_eights(AppendArgs a, int team_shif
         if (mine && page >= 0) {
             load_eight<TYPE>(src, at + i, x);
             if (turned && !is_v) {
-                if (a.interleaved) {
+                if constexpr (!WHOLE) {
+                    float other[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        other[e] = x[e ^ 1];
+                        if (!a.interleaved && i + e < a.rope_dim) other[e] = load_as_float<TYPE>(src, at + (i + e >= half ? i + e - half : i + e + half));
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = i + e < a.rope_dim ? x[e] * cosine[e] + other[e] * sine[e] : x[e];
+                } else if (a.interleaved) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float u = x[2 * e], w = x[2 * e + 1];
@@ -144,17 +108,16 @@ template <int TYPE, int CACHE>
 int launch_heads(int64_t tokens, const AppendArgs &a, hipStream_t st)
 {
     const int items = a.heads + 2 * a.kv.kv_heads, D = a.kv.head_dim;
-    if (a.rope_dim % (a.interleaved ? 8 : 16) == 0 && qg_aligned16(a.cos_sin)) {
-        int shift = 0;
-        while ((8 << shift) < D) ++shift;
-        // a workgroup takes all heads of a token (its angles are loaded once), or, where tokens are few, as many as it has teams
-        const int teams = 256 >> shift, most = (items + teams - 1) / teams;
-        const int64_t want = 4 * (int64_t)qg_compute_units() / tokens;
-        const dim3 grid((unsigned)tokens, (unsigned)(want < 1 ? 1 : want < most ? want : most));
-        hipLaunchKernelGGL((append_eights<TYPE, CACHE>), grid, dim3(256), 0, st, a, shift);
-    } else {
-        hipLaunchKernelGGL((append_heads<TYPE, CACHE>), dim3((unsigned)tokens, (unsigned)((items + 3) / 4)), dim3(256), 0, st, a);
-    }
+    int shift = 0;
+    while ((8 << shift) < D) ++shift;
+    // a workgroup takes all heads of a token (its angles are loaded once), or, where tokens are few, as many as it has teams
+    const int teams = 256 >> shift, most = (items + teams - 1) / teams;
+    const int64_t want = 4 * (int64_t)qg_compute_units() / tokens;
+    const dim3 grid((unsigned)tokens, (unsigned)(want < 1 ? 1 : want < most ? want : most));
+    if (a.rope_dim % (a.interleaved ? 8 : 16) == 0 && qg_aligned16(a.cos_sin))
+        hipLaunchKernelGGL((append_eights<TYPE, CACHE, true>), grid, dim3(256), 0, st, a, shift);
+    else
+        hipLaunchKernelGGL((append_eights<TYPE, CACHE, false>), grid, dim3(256), 0, st, a, shift);
     return qg_launch_status();
 }
 
