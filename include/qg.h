@@ -316,8 +316,8 @@ int qg_gemm_autotune_report(float *us /* HOST */, int capacity, int *timed, int 
  * Arithmetic is fp32; a result is rounded once, to nearest even, where it is stored.
  *
  * 8-bit values (QG_E4M3: sign, 4 exponent bits of bias 7, 3 of significand, no infinities, the type torch
- * calls float8_e4m3fn) come with fp32 scales: over the values that share one, s = max|y| / 448, or 1 where all are
- * zero, and what is stored is y / s; it stands for code * s.  A NaN or an infinity among them makes s and their codes NaN.
+ * calls float8_e4m3fn) come with fp32 scales: over the values that share one, s = max|y| / 448, or 1 where that is
+ * zero (all of them are, or none is above 224 x 2^-149, and codes are 0), and what is stored is y / s; it stands for code * s.  A NaN or an infinity among them makes s and their codes NaN.
  * --------------------------------------------------------------------------------------------- */
 typedef enum { QG_F32 = 0, QG_BF16 = 1, QG_F16 = 2, QG_E4M3 = 3 } qg_type;
 

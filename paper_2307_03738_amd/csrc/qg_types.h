@@ -59,7 +59,8 @@ __device__ inline uint32_t magnitude_bits(float v) { return __float_as_uint(v) &
 __device__ inline float e4m3_scale(uint32_t most)
 {
     if (most >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
-    return most == 0 ? 1.0f : __uint_as_float(most) / QG_E4M3_MOST;
+    const float scale = __uint_as_float(most) / QG_E4M3_MOST;
+    return scale == 0.0f ? 1.0f : scale;                            // (it is for the smallest of numbers, too: up to 224 x 2^-149)
 }
 
 // Eight neighbouring elements as floats, and back.

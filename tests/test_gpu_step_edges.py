@@ -1,4 +1,5 @@
-"""The calls between the products of a token's step where values lie on the edge of what their types hold: quotients in the middle of two codes.
+"""The calls between the products of a token's step where values lie on the edge of what their types hold: quotients in the middle of two codes,
+numbers so small that their scale would be zero.
 
 Exact comparisons unless a test derives a bound of its own."""
 import pytest
@@ -60,3 +61,49 @@ def test_codes_of_the_norm_are_the_quotients_to_nearest_even(qg, rows, K, group)
     assert torch.equal(s.cpu(), x.float().abs().view(rows, -1, group or K).amax(2) / 448)
     off = y.cpu().view(torch.uint8) != codes(x.float(), wide)
     assert not off.any(), f"{int(off.sum())} of {off.numel()} codes"
+
+
+# the largest of a group: its scale is 0 in fp32 up to 224 steps of 2^-149 (1 is taken), then a multiple of 2^-149
+TINY = [(1e-44, True), (224 * 2.0 ** -149, True), (225 * 2.0 ** -149, False), (448 * 2.0 ** -149, False), (1e-41, False)]
+
+
+@pytest.mark.parametrize("most,one", TINY)
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_tiny_heads_are_stored_as_numbers(qg, most, one, dt):
+    print("[case] append tiny", dt, most, flush=True)
+    H, D, page = 3, 64, 16
+    x = torch.zeros(4, H, D)
+    x[1, 1, 5], x[2, 0], x[3, 2, :9] = most, torch.linspace(-most, most, D), most
+    x = x.to(dt)
+    x[0] = torch.randn(H, D, generator=gen(3)).to(dt)
+    k, v = (torch.zeros(1, H, page, D).to(F8).cuda() for _ in "kv")
+    ks, vs = (torch.zeros(1, H, page).cuda() for _ in "kv")
+    at = torch.arange(4, dtype=torch.int32).cuda()
+    qg.qg_kv_append(k, v, torch.zeros(1, 1, dtype=torch.int32).cuda(), torch.zeros_like(at), at, x.cuda(), x.cuda(), k_scale=ks, v_scale=vs)
+    want = x.float().abs().amax(2) / 448
+    want = torch.where(want == 0, 1.0, want)
+    if dt is torch.float32:
+        assert (want[1, 1] == 1) == one
+    for cells, scales in ((k, ks), (v, vs)):
+        s = scales.cpu()[0, :, :4].t()
+        assert torch.equal(s, want)
+        assert torch.equal(cells.cpu().view(torch.uint8)[0, :, :4].transpose(0, 1) & 0x7f, codes(x.float(), s[..., None]) & 0x7f)
+    q = torch.randn(1, H, D, generator=gen(4)).cuda()
+    out, lse = qg.qg_paged_attention(q, k, v, torch.zeros(1, 1, dtype=torch.int32).cuda(), at[:1] + 4, 0.1, k_scale=ks, v_scale=vs, lse=True)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("most,one", TINY)
+@pytest.mark.parametrize("K,group", [(128, 32), (128, 0), (90, 9), (75, 0), (4096, 0)])
+def test_tiny_rows_of_the_norm_are_stored_as_numbers(qg, most, one, K, group):
+    # rows of one under a tiny weight: y is the weight
+    print("[case] norm tiny", most, K, group, flush=True)
+    w = torch.zeros(K)
+    w[3], w[K // 2] = most, -most
+    x = torch.ones(5, K)
+    y, _, s = qg.qg_rms_norm(x.cuda(), w.cuda(), 0.0, dtype=F8, group=group)
+    want = w.abs().view(-1, group or K).amax(1) / 448
+    assert (want[0] == 0) == one
+    want = torch.where(want == 0, 1.0, want).expand(5, -1)
+    assert torch.equal(s.cpu(), want)
+    assert torch.equal(y.cpu().view(torch.uint8) & 0x7f, codes(w, want.repeat_interleave(group or K, 1)) & 0x7f)
