@@ -377,7 +377,8 @@ int qg_kv_append(const qg_append_desc *d /* HOST */, void *stream);
  *   out = sum_i p_i v_i / sum_i p_i,  p_i = exp(scale q.k_i),   lse = log sum_i p_i
  * A sequence without such a key has out = 0 and lse = -infinity; a head whose scores are no numbers has NaN in both.  What lies in cells outside that range is never
  * used, NaN included.  Sums, running maxima and the products' accumulators are fp32; q enters the matrix instructions
- * in parts that add up to it (in a QG_F16 cache to 2^-33 of it or 2^-39 of its head's largest) and the p_i to 2^-16 of themselves or better.  Results are the same from run to run. */
+ * in parts that add up to it (in a QG_F16 cache to 2^-33 of it or 2^-39 of its head's largest) and the p_i to 2^-16 of themselves or better
+ * (in a QG_F16 cache to 2^-22, or 2^-43 of the head's largest).  Results are the same from run to run. */
 typedef struct qg_attention_desc {
     qg_kv_cache cache;
     const int32_t *lens;    /* [batch]: cells in use (limited to max_pages * page); sequence b uses row b of the tables */

@@ -16,8 +16,10 @@
 // maximum only when some score exceeds the running one by 8 (a factor of 2^8 that fp32 sums do not feel).
 //
 // q goes in as it is: as one, two or three parts of 8 (bf16 instruction) or 11 bits (f16, with a power of two for each head
-// taken out first); p as two or, for fp32 outputs on the bf16 instruction, three.  8-bit keys and values are exact in
-// bf16; their scales are applied to the scores and to the p_i.
+// taken out first); p as two or, for fp32 outputs on the bf16 instruction, three.  f16 has steps of 2^-24, below which many small p_i
+// beside a large one would be lost: there p is kept 2^7 times as large, and its second part 2^11 times as large again, in products of its
+// own that are added with 2^-11 (p to 2^-22 of itself or 2^-43 of the largest; 32 multiplications for 32 keys of 128 dims, which the memory hides).
+// 8-bit keys and values are exact in bf16; their scales are applied to the scores and to the p_i.
 //
 // Measured: 128 sequences of up to 8190 tokens, 64 heads on 8, bf16, 1.45 GB of cells: 252 us (5.8 TB/s; a workgroup per head with a key at a time:
 // 8200); one sequence of 131071, 40 heads on 8, f16: 107 us (5.0 TB/s); 757 MB of 8-bit cells 160 ... 176 us; one sequence of 777, 32 key
@@ -141,6 +143,8 @@ struct Attend {
     static constexpr bool F16 = CACHE == QG_F16, E4M3 = CACHE == QG_E4M3;
     static constexpr int Q_PARTS = TYPE == QG_F32 ? 3 : TYPE == QG_F16 && !F16 ? 2 : 1;
     static constexpr int P_PARTS = TYPE == QG_F32 && !F16 ? 3 : 2;
+    static constexpr float LIFT = F16 ? 7.0f : 0.0f;               // p is 2^LIFT times what it is to the maximum, so 2^15 at most in f16
+    static constexpr float REST = 2048.0f;                         // what p's second part in f16 is larger by
     static constexpr int CHUNKS = DPAD / 32;                       // products of 32 dims in a score
     static constexpr int SIZE = E4M3 ? 1 : 2;
     static constexpr int K_LOADS = DPAD * SIZE / 64;               // of 16 bytes, for each key of a lane
@@ -161,7 +165,7 @@ struct Attend {
     // q's operands wait in LDS, where the four wavefronts share them (in registers: up to 96 more)
     static constexpr int Q_VECTORS = Q_PARTS * CHUNKS * 64;
     floatx4 o[DIMS];
-    float m, l, factor;                                            // factor: of a score, for exp2
+    float m, l, factor;                                            // m: running maximum less LIFT; factor: of a score, for exp2
 
     // First dim of load c of a key's elements by the lanes of quad j (of 8 elements, or 16 bytes of e4m3).
     __device__ static int k_dim(int c, int j) { return E4M3 ? 64 * c + 16 * j : 32 * c + 8 * j; }
@@ -319,8 +323,8 @@ struct Attend {
             if constexpr (PARTIAL) p[e] = key + e >= begin && key + e < len ? p[e] : -INFINITY;
             most = fmaxf(most, p[e]);
         }
-        if (__any(most > m + SLACK)) {
-            most = fmaxf(m, across_quads_max(most));
+        if (__any(most > m + (SLACK + LIFT))) {
+            most = fmaxf(m, across_quads_max(most) - LIFT);
             const float keep = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - most);
             l *= keep;
 #pragma unroll
@@ -343,7 +347,13 @@ struct Attend {
 #pragma unroll
         for (int k = 0; k < P_PARTS; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) parts[k].r[e] = take_part<F16>(p[2 * e], p[2 * e + 1]);
+            for (int e = 0; e < 4; ++e) {
+                parts[k].r[e] = take_part<F16>(p[2 * e], p[2 * e + 1]);
+                if constexpr (F16) {
+                    p[2 * e] *= REST;
+                    p[2 * e + 1] *= REST;
+                }
+            }
         if constexpr (PARTIAL) {                                    // 0 times what lies there could be NaN
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -367,10 +377,21 @@ struct Attend {
                     upper.r[r] = __builtin_amdgcn_perm(y, x, 0x07060302u);
                 }
             }
+            if constexpr (F16) {
+                auto add = [&](const Operand &v, floatx4 &to) {
+                    const floatx4 rest = mma<F16>(v, parts[1], floatx4{0, 0, 0, 0});
+                    to = mma<F16>(v, parts[0], to);
 #pragma unroll
-            for (int k = P_PARTS - 1; k >= 0; --k) {
-                o[n] = mma<F16>(lower, parts[k], o[n]);
-                o[n + 1] = mma<F16>(upper, parts[k], o[n + 1]);
+                    for (int r = 0; r < 4; ++r) to[r] = __builtin_fmaf(rest[r], 1.0f / REST, to[r]);
+                };
+                add(lower, o[n]);
+                add(upper, o[n + 1]);
+            } else {
+#pragma unroll
+                for (int k = P_PARTS - 1; k >= 0; --k) {
+                    o[n] = mma<F16>(lower, parts[k], o[n]);
+                    o[n + 1] = mma<F16>(upper, parts[k], o[n + 1]);
+                }
             }
         }
     }

@@ -1,12 +1,15 @@
 """The calls between the products of a token's step where values lie on the edge of what their types hold: quotients in the middle of two codes,
-numbers so small that their scale would be zero.
+numbers so small that their scale would be zero, small probabilities beside large ones.
 
 Exact comparisons unless a test derives a bound of its own."""
+import math
+
 import pytest
 import torch
 
 pytestmark = pytest.mark.gpu
 
+U = 2.0 ** -24
 F8 = torch.float8_e4m3fn
 
 
@@ -107,3 +110,28 @@ def test_tiny_rows_of_the_norm_are_stored_as_numbers(qg, most, one, K, group):
     want = torch.where(want == 0, 1.0, want).expand(5, -1)
     assert torch.equal(s.cpu(), want)
     assert torch.equal(y.cpu().view(torch.uint8) & 0x7f, codes(w, want.repeat_interleave(group or K, 1)) & 0x7f)
+
+
+@pytest.mark.parametrize("D,H,n", [(64, 4, 900), (128, 4, 5000), (128, 1, 70), (256, 2, 2000), (80, 16, 3000)])
+@pytest.mark.parametrize("nats", [6, 9, 12, 15, 17, 20])
+@pytest.mark.parametrize("ct", [torch.bfloat16, torch.float16, F8])
+def test_many_small_probabilities_beside_large_ones(qg, ct, nats, D, H, n):
+    # Every 16th key is `nats` above the others and has values of 0, the others have 1: out is the others' share alone, and has to be right relative to
+    # itself.  Scores are exact; exp errs by 4 U and U of the score, the sums by sqrt(n) U each, p by 2^-22 of itself or 2^-43 of the largest, and
+    # out is rounded once.
+    print("[case] small p", ct, nats, D, H, n, flush=True)
+    page, pages = 16, -(-n // 16)
+    k, v = torch.zeros(pages, 1, page, D), torch.ones(pages, 1, page, D)
+    k[:, :, 0, 0], v[:, :, 0] = nats, 0
+    s = torch.ones(pages, 1, page).cuda() if ct is F8 else None
+    q = torch.zeros(1, H, D)
+    q[..., 0] = 1
+    out, lse = qg.qg_paged_attention(q.cuda(), k.to(ct).cuda(), v.to(ct).cuda(), torch.arange(pages, dtype=torch.int32).view(1, -1).cuda(),
+                                     torch.tensor([n], dtype=torch.int32).cuda(), 1.0, k_scale=s, v_scale=s, lse=True)
+    big, nats = pages, k.to(ct).float().max().item()                        # (17 is 16 in e4m3)
+    total = big * math.exp(nats) + n - big
+    want = (n - big) / total
+    e = 2 * (2.0 ** -22 + 2.0 ** -43 * math.exp(nats) + (4 + 2 * nats + math.sqrt(n)) * U) + U
+    off = (out.cpu().double() / want - 1).abs().max().item()
+    assert off <= e, f"off by {off:.2e} of itself, {e:.2e} allowed"
+    assert (lse.cpu().double() - math.log(total)).abs().max().item() <= e + 2 * U * math.log(total)
