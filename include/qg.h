@@ -375,7 +375,9 @@ int qg_kv_append(const qg_append_desc *d /* HOST */, void *stream);
 /* Attention of one new token of each sequence over the cache.  Head h of `heads` reads key head
  * h / (heads / kv_heads).  With the keys i of [max(first, len - window), len):
  *   out = sum_i p_i v_i / sum_i p_i,  p_i = exp(scale q.k_i),   lse = log sum_i p_i
- * A sequence without such a key has out = 0 and lse = -infinity; a head whose scores are no numbers has NaN in both.  What lies in cells outside that range is never
+ * A sequence without such a key has out = 0 and lse = -infinity; a head whose scores are no numbers has NaN in both.
+ * Infinities in cells (QG_F16 gets them from what is above 65504) are what they are in the formula: a value's comes out, with its sign, however small its p_i, a
+ * score of -infinity counts for nothing (times an infinite value it is NaN), one of +infinity makes the head NaN.  What lies in cells outside that range is never
  * used, NaN included.  Sums, running maxima and the products' accumulators are fp32; q enters the matrix instructions
  * in parts that add up to it (in a QG_F16 cache to 2^-33 of it or 2^-39 of its head's largest) and the p_i to 2^-16 of themselves or better
  * (in a QG_F16 cache to 2^-22, or 2^-43 of the head's largest).  Results are the same from run to run. */

@@ -21,6 +21,10 @@
 // own that are added with 2^-11 (p to 2^-22 of itself or 2^-43 of the largest; 32 multiplications for 32 keys of 128 dims, which the memory hides).
 // 8-bit keys and values are exact in bf16; their scales are applied to the scores and to the p_i.
 //
+// An infinite cell times a part that is 0 or of the other sign is NaN where the whole is not.  So a workgroup that has seen a head's keys looks
+// for NaN in what it has and, if there is one, sees them again with infinite cells in products of their own: with signs of q, and with
+// 1 for each p_i.  (8-bit cells have no infinities.)
+//
 // Measured: 128 sequences of up to 8190 tokens, 64 heads on 8, bf16, 1.45 GB of cells: 252 us (5.8 TB/s; a workgroup per head with a key at a time:
 // 8200); one sequence of 131071, 40 heads on 8, f16: 107 us (5.0 TB/s); 757 MB of 8-bit cells 160 ... 176 us; one sequence of 777, 32 key
 // heads: 12.4 us, of which lengths take 1.5, page ids and q 2.5, cells 1.4, adding up in LDS 1.0, parts written and counted 0.8, their sum 3.
@@ -110,6 +114,10 @@ __device__ inline T load_cells(const char *p)
     }
 }
 
+// What a head's sums of values at maximum m are multiplied by to be at `top`: never 0 if there is a maximum, so that infinities stay
+// (2^-149 of a finite one is nothing beside the largest value).
+__device__ inline float value_weight(float m, float top) { return m == -INFINITY ? 0.0f : fmaxf(__builtin_amdgcn_exp2f(m - top), 0x1p-149f); }
+
 // What a sum of p relative to maximum m counts relative to maximum `top`.  Without a score above -infinity the sum is 0, or NaN where
 // scores were none, which has to come through.
 __device__ inline float weight_of(float m, float top) { return m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top); }
@@ -159,6 +167,8 @@ struct Attend {
     // several instructions ask for, are not (8-bit values and padded heads lose 10 % by it)
     static constexpr bool ONCE_K = FULL, ONCE_V = FULL && !E4M3;
 
+    static constexpr uint32_t EXPONENT = F16 ? 0x7c00u : 0x7f80u, ONE = F16 ? 0x3c00u : 0x3f80u;
+
     u32x4 kr[2][K_LOADS];
     uint32_t vr[8][V_WORDS];
     float ks[8], vs[8];
@@ -170,32 +180,36 @@ struct Attend {
     // First dim of load c of a key's elements by the lanes of quad j (of 8 elements, or 16 bytes of e4m3).
     __device__ static int k_dim(int c, int j) { return E4M3 ? 64 * c + 16 * j : 32 * c + 8 * j; }
 
+    // Elements of operand c of q's head that are this lane's.
+    __device__ static void load_q(const AttentionArgs &a, int64_t b, int head, bool real, int c, int j, float x[8])
+    {
+        const int D = FULL ? DPAD : a.kv.head_dim;
+        const char *row = (const char *)a.q + (b * a.q_stride + (int64_t)head * D) * (TYPE == QG_F32 ? 4 : 2);
+        const int d = E4M3 ? k_dim(c / 2, j) + 8 * (c % 2) : k_dim(c, j);
+        const bool some = real && (FULL || d < D);
+        if constexpr (TYPE == QG_F32) {
+            floatx4 v[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+            if (some) {
+                v[0] = *(const floatx4 *)(row + 4 * d);
+                v[1] = *(const floatx4 *)(row + 4 * d + 16);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = v[e / 4][e % 4];
+        } else {
+            u32x4 v = {0, 0, 0, 0};
+            if (some) v = *(const u32x4 *)(row + 2 * d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t bits = e % 2 ? v[e / 2] >> 16 : v[e / 2] & 0xffffu;
+                x[e] = TYPE == QG_BF16 ? bf16_to_float(bits) : f16_to_float(bits);
+            }
+        }
+    }
+
     // Of q's CHUNKS operands a wavefront makes every fourth and puts its parts into LDS.
     __device__ void share_q(const AttentionArgs &a, int64_t b, int head, bool real, u32x4 *shared_q, int wave, int lane)
     {
-        const int D = FULL ? DPAD : a.kv.head_dim, j = lane >> 4;
-        const char *row = (const char *)a.q + (b * a.q_stride + (int64_t)head * D) * (TYPE == QG_F32 ? 4 : 2);
-        auto load = [&](int c, float x[8]) {
-            const int d = E4M3 ? k_dim(c / 2, j) + 8 * (c % 2) : k_dim(c, j);
-            const bool some = real && (FULL || d < D);
-            if constexpr (TYPE == QG_F32) {
-                floatx4 v[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-                if (some) {
-                    v[0] = *(const floatx4 *)(row + 4 * d);
-                    v[1] = *(const floatx4 *)(row + 4 * d + 16);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = v[e / 4][e % 4];
-            } else {
-                u32x4 v = {0, 0, 0, 0};
-                if (some) v = *(const u32x4 *)(row + 2 * d);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t bits = e % 2 ? v[e / 2] >> 16 : v[e / 2] & 0xffffu;
-                    x[e] = TYPE == QG_BF16 ? bf16_to_float(bits) : f16_to_float(bits);
-                }
-            }
-        };
+        auto load = [&](int c, float x[8]) { load_q(a, b, head, real, c, lane >> 4, x); };
         factor = a.scale * 1.4426950408889634f;
         int up = 0;
         if constexpr (F16) {
@@ -225,6 +239,19 @@ struct Attend {
                 for (int e = 0; e < 4; ++e) part[e] = take_part<F16>(x[2 * e], x[2 * e + 1]);
                 shared_q[(p * CHUNKS + c) * 64 + lane] = part;
             }
+        }
+    }
+
+    // ... and the elements' signs, as 1, -1, 0 or, where they are no finite numbers, NaN.
+    __device__ static void share_signs(const AttentionArgs &a, int64_t b, int head, bool real, u32x4 *shared_signs, int wave, int lane)
+    {
+        for (int c = wave; c < CHUNKS; c += WAVES) {
+            float x[8];
+            load_q(a, b, head, real, c, lane >> 4, x);
+            uint32_t bits[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) bits[e] = x[e] == 0.0f ? 0u : !(fabsf(x[e]) < INFINITY) ? EXPONENT | EXPONENT >> 1 : ONE | (x[e] < 0.0f ? 0x8000u : 0u);
+            shared_signs[c * 64 + lane] = u32x4{bits[0] | bits[1] << 16, bits[2] | bits[3] << 16, bits[4] | bits[5] << 16, bits[6] | bits[7] << 16};
         }
     }
 
@@ -311,6 +338,65 @@ struct Attend {
         }
     }
 
+    // The halves of a word that are no finite numbers; the others are 0.
+    __device__ static uint32_t not_finite(uint32_t w)
+    {
+        return ((w & EXPONENT) == EXPONENT ? w & 0xffffu : 0u) | ((w & EXPONENT << 16) == EXPONENT << 16 ? w & 0xffff0000u : 0u);
+    }
+
+    // Scores that are NaN are anew what the infinite elements of a key make of q's signs, if it has any.
+    __device__ void correct_scores(floatx4 s[2], const u32x4 *shared_signs, int lane)
+    {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            floatx4 x = {0, 0, 0, 0};
+            for (int c = 0; c < CHUNKS; ++c) {
+                Operand k, sign;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    k.r[r] = not_finite(kr[t][c][r]);
+                    sign.r[r] = shared_signs[c * 64 + lane][r];
+                }
+                x = mma<F16>(k, sign, x);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t][e] = s[t][e] != s[t][e] && x[e] != 0.0f ? x[e] : s[t][e];
+        }
+    }
+
+    // Takes the values that are no finite numbers out of the registers and adds them up, each by 1 (0 where the score is -infinity, NaN where it is).
+    __device__ void add_infinities(const floatx4 s[2], int key, int begin, int len)
+    {
+        Operand ones;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            ones.r[r] = 0;
+#pragma unroll
+            for (int e = 2 * r; e < 2 * r + 2; ++e) {
+                const float x = s[e / 4][e % 4] * factor;
+                const bool seen = key + e >= begin && key + e < len;
+                const uint32_t one = !seen || x == -INFINITY ? 0u : x != x ? EXPONENT | EXPONENT >> 1 : ONE;
+                ones.r[r] |= one << 16 * (e & 1);
+#pragma unroll
+                for (int w = 0; w < V_WORDS; ++w) vr[e][w] = seen ? vr[e][w] : 0u;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < DIMS; n += 2) {
+            Operand lower, upper;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t x = not_finite(vr[2 * r][n / 2]), y = not_finite(vr[2 * r + 1][n / 2]);
+                lower.r[r] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                upper.r[r] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                vr[2 * r][n / 2] ^= x;
+                vr[2 * r + 1][n / 2] ^= y;
+            }
+            o[n] = mma<F16>(lower, ones, o[n]);
+            o[n + 1] = mma<F16>(upper, ones, o[n + 1]);
+        }
+    }
+
     // The running maximum, and s as p.  The keys are key ... key + 7; those outside [begin, len) count for nothing.
     template <bool PARTIAL>
     __device__ void soften(floatx4 s[2], float p[8], int key, int begin, int len)
@@ -325,10 +411,10 @@ struct Attend {
         }
         if (__any(most > m + (SLACK + LIFT))) {
             most = fmaxf(m, across_quads_max(most) - LIFT);
-            const float keep = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - most);
+            const float keep = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - most), keep_o = fmaxf(keep, 0x1p-149f);
             l *= keep;
 #pragma unroll
-            for (int n = 0; n < DIMS; ++n) o[n] *= keep;
+            for (int n = 0; n < DIMS; ++n) o[n] *= keep_o;
             m = most;
         }
         const float base = m == -INFINITY ? 0.0f : m;
@@ -446,7 +532,7 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
     __shared__ u32x4 shared_q[A::Q_VECTORS];
     __shared__ float wave_m[16][16], wave_l[16][16];
     __shared__ int is_last, found_b, wave_sums[3][WAVES];
-    __shared__ int64_t found_at;
+    __shared__ int64_t found_at, seen_nan;                          // seen_nan: the segment that NaN has come out of
     __shared__ float head_m[16], head_l[16];
     const rsrc_t parts = buffer_of(a.parts, a.parts_bytes);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, j = lane >> 4;
@@ -533,7 +619,11 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
     Keys keys = keys_of(a, b);
 
     A t;
+    if (tid == 0) seen_nan = -1;                                    // (the first segment's barrier is before its first use)
     for (int64_t at = begin_at; at < end_at;) {
+        int tid = (int)threadIdx.x;
+        asm volatile("" : "+v"(tid));                               // (so that nothing made of it waits in registers through the loop over the keys)
+        const int lane = tid & 63, i = lane & 15, j = lane >> 4;
         int units = units_of(keys.spans);
         while (at - sequence_at >= (int64_t)units * heads) {
             sequence_at += (int64_t)units * heads;
@@ -605,17 +695,55 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
         }
 
         // the four wavefronts' parts: sums at one maximum
-        t.l += __shfl_xor(t.l, 16);
-        t.l += __shfl_xor(t.l, 32);
-        if (j == 0) {
-            wave_m[wave][i] = t.m;
-            wave_l[wave][i] = t.l;
+        auto share_sums = [&] {
+            t.l += __shfl_xor(t.l, 16);
+            t.l += __shfl_xor(t.l, 32);
+            if (j == 0) {
+                wave_m[wave][i] = t.m;
+                wave_l[wave][i] = t.l;
+            }
+        };
+        share_sums();
+        if constexpr (!A::E4M3) {
+            bool none = t.l != t.l;
+#pragma unroll
+            for (int n = 0; n < A::DIMS; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) none = none || t.o[n][r] != t.o[n][r];
+            if (__any(none && i < rows)) seen_nan = segment_at;       // (any lane's write is as good as another's)
         }
         __syncthreads();
+        if constexpr (!A::E4M3) {
+            if (seen_nan == segment_at) {                           // (of the whole workgroup)
+                u32x4 *signs = (u32x4 *)shared;
+                t.share_signs(a, b, head0 + i, i < rows, signs, wave, lane);
+                t.m = -INFINITY;
+                t.l = 0.0f;
+#pragma unroll
+                for (int n = 0; n < A::DIMS; ++n) t.o[n] = floatx4{0, 0, 0, 0};
+                __syncthreads();
+                for (int n = 0; n < tiles; ++n) {
+                    floatx4 s[2];
+                    float p[8];
+                    const int key = keys.base + 32 * (first + WAVES * n) + 8 * j;
+                    if ((n & 31) == 0) pages_from(n);
+                    fetch_k(n);
+                    t.scores(s, shared_q, lane);
+                    t.correct_scores(s, signs, lane);
+                    t.template soften<true>(s, p, key, keys.begin, keys.len);
+                    asm volatile("" ::: "memory");                  // (keys and values in registers one after the other: this is no place to hurry)
+                    fetch_v(n);
+                    t.add_infinities(s, key, keys.begin, keys.len);
+                    t.template add_values<true>(p, key, keys.begin, keys.len);
+                }
+                share_sums();
+                __syncthreads();
+            }
+        }
         float most = -INFINITY;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) most = fmaxf(most, wave_m[w][i]);
-        const float keep = t.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t.m - most);
+        const float keep = value_weight(t.m, most);
         const bool whole = from == 0 && to == keys.spans;
         // a worker's first part of a head's keys goes into its slot 0 unless it begins them
         const uint32_t part = 4u * (2 * worker + (from == 0)) * a.part_floats;
@@ -734,7 +862,7 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
                                     const int at_m = (k0 + c * shares) * rows + row;
                                     const float m = at_m < SHARED_FLOATS ? shared[at_m] : __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
                                                                                               parts, part_of(k0 + c * shares) + 4 * (rows * D + 2 * row), 0, SC1));
-                                    v += (m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top)) * __builtin_bit_cast(floatx4, y[c]);
+                                    v += value_weight(m, top) * __builtin_bit_cast(floatx4, y[c]);
                                 }
                         }
                     }

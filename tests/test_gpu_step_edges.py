@@ -1,5 +1,6 @@
 """The calls between the products of a token's step where values lie on the edge of what their types hold: quotients in the middle of two codes,
-numbers so small that their scale would be zero, small probabilities beside large ones.
+numbers so small that their scale would be zero, small probabilities beside large ones,
+infinite cells.
 
 Exact comparisons unless a test derives a bound of its own."""
 import math
@@ -135,3 +136,78 @@ def test_many_small_probabilities_beside_large_ones(qg, ct, nats, D, H, n):
     off = (out.cpu().double() / want - 1).abs().max().item()
     assert off <= e, f"off by {off:.2e} of itself, {e:.2e} allowed"
     assert (lse.cpu().double() - math.log(total)).abs().max().item() <= e + 2 * U * math.log(total)
+
+
+def formula(q, K, V, scale):
+    """(out, lse, largest error of a score) of one head over keys K, V [n][D], infinities and all."""
+    q, K, V = q.double(), K.double(), V.double()
+    s = (K * q).sum(1) * scale
+    p = torch.softmax(s, 0)
+    finite = torch.isfinite(K).all(1)
+    delta = (len(q) + 8) * U * scale * (K[finite].abs() @ q.abs()).max() + 4 * U + 2 * U * s[finite].abs().max()
+    return (p[:, None] * V).sum(0), torch.logsumexp(s, 0), float(delta)
+
+
+def same(got, want, slack, dtype):
+    """NaN and infinities where they belong, other values near."""
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"NaN: {int(torch.isnan(got).sum())}, not {int(torch.isnan(want).sum())}"
+    assert torch.equal(torch.isinf(got), torch.isinf(want)) and torch.equal(got[torch.isinf(want)], want[torch.isinf(want)])
+    at = torch.isfinite(want)
+    bound = slack + (want.abs() + slack) * {torch.float32: U, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}[dtype] + 2.0 ** -25
+    assert ((got - want).abs() <= bound)[at].all(), float(((got - want).abs() - bound)[at].max())
+
+
+@pytest.mark.parametrize("lens", [[40, 7, 129], [9000, 600, 1]])
+@pytest.mark.parametrize("D", [64, 80, 128, 256])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("ct", [torch.bfloat16, torch.float16])
+def test_infinite_cells_are_what_they_are_in_the_formula(qg, ct, dt, D, lens):
+    print("[case] infinite cells", ct, dt, D, lens, flush=True)
+    H, Hkv, page, scale = 6, 2, 16, 0.1
+    B, need = len(lens), [-(-n // page) for n in lens]
+    pages = sum(need)
+    tables = torch.full((B, max(need)), -1, dtype=torch.int32)
+    order, at = torch.randperm(pages, generator=gen(5)).to(torch.int32), 0
+    for b, n in enumerate(need):
+        tables[b, :n], at = order[at:at + n], at + n
+    g = gen(6)
+    k, v = (torch.randn(pages, Hkv, page, D, generator=g).to(ct) for _ in "kv")
+    q = torch.randn(B, H, D, generator=g).to(dt)
+    q[:, :, 3], q[:, :, 7] = 1, -2                                       # one part each, whose others are 0
+    q[:, 1, 11] = 0
+    cell = lambda b, i: (int(tables[b, i // page]), slice(None), i % page)  # noqa: E731
+    for b, n in enumerate(lens):
+        for i, d, x in ((0, 5, math.inf), (n - 1, 9, -math.inf), (n // 2, 20, math.inf), (n // 3, 20, -math.inf), (n // 4, 21, math.inf), (n // 5, 21, math.inf)):
+            v[cell(b, i)][:, d] = x
+        if n > 30:
+            k[cell(b, 17)][:, 3] = -math.inf                               # q is positive there: the key counts for nothing
+            k[cell(b, 18)][:, 7] = math.inf                                # q is negative
+            k[cell(b, n - 2)][0, 12] = math.inf                            # one key head: of heads 0, 1 and 2 those with positive q are NaN
+            k[cell(b, n - 4)][1, 11] = -math.inf
+            # a key far below the others, whose p has no place in fp32, has an infinite value
+            k[cell(b, 25)][:, 3], v[cell(b, 25)][:, 30] = -3000, math.inf
+    out, lse = qg.qg_paged_attention(q.cuda(), k.cuda(), v.cuda(), tables.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), scale, lse=True)
+    for b, n in enumerate(lens):
+        at = torch.arange(n)
+        for h in range(H):
+            cells = (tables[b, at // page].long(), h // (H // Hkv), at % page)
+            want, wlse, delta = formula(q[b, h], k[cells], v[cells], scale)
+            e = 2 * (delta + 2.0 ** -16 + math.sqrt(n) * U)
+            same(out[b, h].cpu().double(), want, e * v[torch.isfinite(v)].abs().max().item(), dt)
+            if not torch.isnan(want).all():
+                same(lse[b, h].cpu().double(), wlse, e + 2 * U * float(wlse.abs()), torch.float32)
+
+
+def test_values_past_the_range_of_f16_come_out_infinite(qg):
+    H, D, page, n = 2, 64, 16, 300
+    k, v = (torch.zeros(-(-n // page), H, page, D, dtype=torch.float16).cuda() for _ in "kv")
+    at, tables = torch.arange(n, dtype=torch.int32).cuda(), torch.arange(-(-n // page), dtype=torch.int32).view(1, -1).cuda()
+    new = torch.randn(n, H, D, generator=gen(7))
+    new[100, 1, 6], new[299, 0, 2] = 7e4, -1e30
+    qg.qg_kv_append(k, v, tables, torch.zeros_like(at), at, torch.randn(n, H, D, generator=gen(8)).cuda(), new.cuda())
+    q = torch.randn(1, H, D, generator=gen(9)).cuda()
+    for window in (0, 250, 190):
+        out, _ = qg.qg_paged_attention(q, k, v, tables, at[-1:] + 1, 0.1, window=window)
+        want = torch.zeros(H, D)
+        want[0, 2], want[1, 6] = -math.inf, math.inf if window != 190 else 0
+        assert torch.equal(torch.where(torch.isinf(out[0].cpu()), out[0].cpu(), 0.0), want) and not torch.isnan(out).any()
