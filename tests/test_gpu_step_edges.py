@@ -1,6 +1,6 @@
 """The calls between the products of a token's step where values lie on the edge of what their types hold: quotients in the middle of two codes,
 numbers so small that their scale would be zero, small probabilities beside large ones,
-infinite cells.
+infinite cells, the longest rows.
 
 Exact comparisons unless a test derives a bound of its own."""
 import math
@@ -211,3 +211,15 @@ def test_values_past_the_range_of_f16_come_out_infinite(qg):
         want = torch.zeros(H, D)
         want[0, 2], want[1, 6] = -math.inf, math.inf if window != 190 else 0
         assert torch.equal(torch.where(torch.isinf(out[0].cpu()), out[0].cpu(), 0.0), want) and not torch.isnan(out).any()
+
+
+@pytest.mark.parametrize("value", [3.3, 1.1, 0.9])
+@pytest.mark.parametrize("rows,K,residual", [(2, 65536 + 7, False), (2, (1 << 20) + 3, True), (1, 1 << 24, False), (1, (1 << 24) - 1, True)])
+def test_norm_of_the_longest_rows(qg, rows, K, residual, value):
+    # equal values, whose sum's roundings do not average out.  A sum of K squares in pieces of at most 64 terms and ten levels of a tree errs
+    # by at most 74 U of itself, half of that under the root, six roundings around it: 43 U of |y|
+    print("[case] long rows", rows, K, residual, value, flush=True)
+    x = torch.full((rows, K), value)
+    r = torch.full((rows, K), value / 2) if residual else None
+    y, _, _ = qg.qg_rms_norm(x.cuda(), torch.ones(K).cuda(), 0.0, residual=None if r is None else r.cuda())
+    assert (y.double() - 1).abs().max().item() <= 43 * U + U
