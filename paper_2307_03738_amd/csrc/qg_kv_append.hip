@@ -105,20 +105,33 @@ __global__ __launch_bounds__(256) void append_eights(AppendArgs a, int team_shif
 }
 
 template <int TYPE, int CACHE>
-int launch_heads(int64_t tokens, const AppendArgs &a, hipStream_t st)
+int launch_heads(int64_t all_tokens, const AppendArgs &all, hipStream_t st)
 {
-    const int items = a.heads + 2 * a.kv.kv_heads, D = a.kv.head_dim;
+    const int items = all.heads + 2 * all.kv.kv_heads, D = all.kv.head_dim, size = qg_type_bytes(TYPE);
     int shift = 0;
     while ((8 << shift) < D) ++shift;
-    // a workgroup takes all heads of a token (its angles are loaded once), or, where tokens are few, as many as it has teams
-    const int teams = 256 >> shift, most = (items + teams - 1) / teams;
-    const int64_t want = 4 * (int64_t)qg_compute_units() / tokens;
-    const dim3 grid((unsigned)tokens, (unsigned)(want < 1 ? 1 : want < most ? want : most));
-    if (a.rope_dim % (a.interleaved ? 8 : 16) == 0 && qg_aligned16(a.cos_sin))
-        hipLaunchKernelGGL((append_eights<TYPE, CACHE, true>), grid, dim3(256), 0, st, a, shift);
-    else
-        hipLaunchKernelGGL((append_eights<TYPE, CACHE, false>), grid, dim3(256), 0, st, a, shift);
-    return qg_launch_status();
+    const bool whole = all.rope_dim % (all.interleaved ? 8 : 16) == 0 && qg_aligned16(all.cos_sin);
+    for (int64_t token = 0; token < all_tokens; token += QG_MOST_GROUPS) {
+        const int64_t tokens = all_tokens - token < QG_MOST_GROUPS ? all_tokens - token : QG_MOST_GROUPS;
+        AppendArgs a = all;
+        a.rows += token;
+        a.positions += token;
+        a.k = (const char *)a.k + token * a.k_stride * size;
+        a.v = (const char *)a.v + token * a.v_stride * size;
+        if (a.heads) {
+            a.q = (const char *)a.q + token * a.q_stride * size;
+            a.q_out = (char *)a.q_out + token * a.heads * D * size;
+        }
+        // a workgroup takes all heads of a token (its angles are loaded once), or, where tokens are few, as many as it has teams
+        const int teams = 256 >> shift, most = (items + teams - 1) / teams;
+        const int64_t want = 4 * (int64_t)qg_compute_units() / tokens;
+        const dim3 grid((unsigned)tokens, (unsigned)(want < 1 ? 1 : want < most ? want : most));
+        if (whole) hipLaunchKernelGGL((append_eights<TYPE, CACHE, true>), grid, dim3(256), 0, st, a, shift);
+        else hipLaunchKernelGGL((append_eights<TYPE, CACHE, false>), grid, dim3(256), 0, st, a, shift);
+        const int rc = qg_launch_status();
+        if (rc != QG_OK) return rc;
+    }
+    return QG_OK;
 }
 
 template <int TYPE>

@@ -199,8 +199,20 @@ int launch_rows(const qg_norm_desc &d, const NormArgs &a, hipStream_t st)
                  (d.rows == 1 || (d.x_stride % 8 == 0 && d.residual_stride % 8 == 0));
     if (YTYPE == QG_E4M3 && group != K) eight = eight && group % 8 == 0 && group <= 512 && (group & (group - 1)) == 0;
     if (!eight) {
-        hipLaunchKernelGGL((norm_rows<TYPE, YTYPE>), dim3((unsigned)d.rows), dim3(256), 0, st, a, d.weight_type);
-        return qg_launch_status();
+        const int size = qg_type_bytes(TYPE);
+        for (int64_t row = 0; row < d.rows; row += QG_MOST_GROUPS) {
+            const int64_t rows = d.rows - row < QG_MOST_GROUPS ? d.rows - row : QG_MOST_GROUPS;
+            NormArgs turn = a;
+            turn.x = (const char *)a.x + row * a.x_stride * size;
+            if (a.residual) turn.residual = (const char *)a.residual + row * a.residual_stride * size;
+            if (a.h) turn.h = (char *)a.h + row * K * size;
+            turn.y = (char *)a.y + row * K * qg_type_bytes(YTYPE);
+            if (a.scales) turn.scales = a.scales + row * (K / group);
+            hipLaunchKernelGGL((norm_rows<TYPE, YTYPE>), dim3((unsigned)rows), dim3(256), 0, st, turn, d.weight_type);
+            const int rc = qg_launch_status();
+            if (rc != QG_OK) return rc;
+        }
+        return QG_OK;
     }
     // few rows: as many lanes as there are eights; many: two eights a lane (four would spill: a row asked for ahead doubles the registers)
     const int units = qg_compute_units();

@@ -303,9 +303,9 @@ __global__ __launch_bounds__(256) void fork_refs(Book b)
     if (p < b.pages) b.refs_out[p] = b.refs[p];
 }
 
-__global__ __launch_bounds__(256) void fork_rows(Book b, const int32_t *parents)
+__global__ __launch_bounds__(256) void fork_rows(Book b, const int32_t *parents, int first_row)
 {
-    const int row = blockIdx.x;
+    const int row = first_row + (int)blockIdx.x;
     const int parent = parents[row];
     const bool some = parent >= 0 && parent < b.rows;
     for (int column = threadIdx.x; column < b.max_pages; column += 256) {
@@ -492,7 +492,9 @@ extern "C" int qg_pages_fork(const qg_page_book *book, const int32_t *parents, v
     if (b.refs == b.refs_out || (b.rows && (b.tables == b.tables_out || b.lens == b.lens_out))) return QG_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;
     hipLaunchKernelGGL(fork_refs, dim3((unsigned)((b.pages + 255) / 256)), dim3(256), 0, st, b);
-    if (b.rows) hipLaunchKernelGGL(fork_rows, dim3((unsigned)b.rows), dim3(256), 0, st, b, parents);
+    constexpr int MOST = 1 << 23;                                   // (a launch has less than 2^32 lanes)
+    for (int row = 0; row < b.rows; row += MOST)
+        hipLaunchKernelGGL(fork_rows, dim3((unsigned)(b.rows - row < MOST ? b.rows - row : MOST)), dim3(256), 0, st, b, parents, row);
     return qg_launch_status();
 }
 

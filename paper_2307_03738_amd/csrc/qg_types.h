@@ -11,6 +11,9 @@ static inline bool qg_aligned_to(const void *p, int bytes) { return ((uintptr_t)
 
 constexpr float QG_E4M3_MOST = 448.0f;
 
+// Workgroups of 256 of one launch, whose lanes have to number less than 2^32; what needs more is launched in turns.
+constexpr int64_t QG_MOST_GROUPS = 1 << 23;
+
 // Vectors of 4, 8 or 16 bytes, loaded as they lie in memory.
 template <int BYTES> struct QgRaw;
 template <> struct QgRaw<4> { typedef uint32_t t; };

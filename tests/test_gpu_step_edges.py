@@ -1,6 +1,6 @@
 """The calls between the products of a token's step where values lie on the edge of what their types hold: quotients in the middle of two codes,
 numbers so small that their scale would be zero, small probabilities beside large ones,
-infinite cells, the longest rows.
+infinite cells, the longest rows, the most of them.
 
 Exact comparisons unless a test derives a bound of its own."""
 import math
@@ -223,3 +223,53 @@ def test_norm_of_the_longest_rows(qg, rows, K, residual, value):
     r = torch.full((rows, K), value / 2) if residual else None
     y, _, _ = qg.qg_rms_norm(x.cuda(), torch.ones(K).cuda(), 0.0, residual=None if r is None else r.cuda())
     assert (y.double() - 1).abs().max().item() <= 43 * U + U
+
+
+def test_norm_of_more_rows_than_one_launch_takes(qg):
+    rows, K = (1 << 23) + 5, 3
+    print("[case] rows", rows, K, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(11)
+    x = torch.randn(rows, K, generator=g, device="cuda").to(torch.float16)
+    r = torch.randn(rows, K, generator=g, device="cuda").to(torch.float16)
+    w = torch.tensor([1.0, 0.5, 2.0]).cuda()
+    at = torch.tensor([0, 1, rows // 2, (1 << 23) - 1, 1 << 23, rows - 1]).cuda()
+    y, h, _ = qg.qg_rms_norm(x, w, residual=r)
+    part = qg.qg_rms_norm(x[at].contiguous(), w, residual=r[at].contiguous())
+    assert torch.equal(y[at], part[0]) and torch.equal(h[at], part[1]) and torch.equal(h[-1 << 20:], (x[-1 << 20:].float() + r[-1 << 20:].float()).half())
+    y, _, s = qg.qg_rms_norm(x, w, dtype=F8, group=1)
+    part = qg.qg_rms_norm(x[at].contiguous(), w, dtype=F8, group=1)
+    assert torch.equal(y.view(torch.uint8)[at], part[0].view(torch.uint8)) and torch.equal(s[at], part[2])
+
+
+def test_append_of_more_tokens_than_one_launch_takes(qg):
+    T, D, page, n = (1 << 23) + 5, 8, 16, 48
+    print("[case] tokens", T, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    q, k, v = (torch.randn(T, 1, D, generator=g, device="cuda").to(torch.bfloat16) for _ in "qkv")
+    rows, positions = torch.full((T,), -1, dtype=torch.int32).cuda(), torch.zeros(T, dtype=torch.int32).cuda()
+    at = torch.cat((torch.arange(n - 10), torch.arange(T - 10, T))).cuda()
+    rows[at], positions[at] = 0, torch.arange(n, dtype=torch.int32).cuda()
+    kc, vc = (torch.zeros(n // page, 1, page, D, dtype=torch.bfloat16).cuda() for _ in "kv")
+    angles = torch.rand(64, 2, generator=g, device="cuda")
+    turn = torch.cat((angles.cos(), angles.sin()), 1)
+    tables = torch.arange(n // page, dtype=torch.int32).view(1, -1).cuda()
+    out = qg.qg_kv_append(kc, vc, tables, rows, positions, k, v, q=q, cos_sin=turn)
+    k2, v2 = torch.zeros_like(kc), torch.zeros_like(vc)
+    out2 = qg.qg_kv_append(k2, v2, tables, rows[at], positions[at], k[at], v[at], q=q[at], cos_sin=turn)
+    assert torch.equal(kc, k2) and torch.equal(vc, v2) and torch.equal(out[at], out2) and torch.equal(vc.view(n, D), v[at, 0])
+    assert (out[n:-10] == 0).all()
+
+
+def test_fork_of_more_rows_than_one_launch_takes(qg):
+    rows, pages = (1 << 23) + 5, 64
+    print("[case] rows", rows, flush=True)
+    tables = (torch.arange(rows, dtype=torch.int32) % pages).view(-1, 1).cuda()
+    lens, refs = torch.arange(rows, dtype=torch.int32).cuda() % 7, torch.bincount(tables.view(-1), minlength=pages).to(torch.int32)
+    parents = torch.arange(rows, dtype=torch.int32).flip(0).cuda()
+    parents[-3] = -1
+    t, n, r = qg.qg_pages_fork(tables, lens, refs, parents)
+    want = tables.flip(0)
+    want[-3] = -1
+    wlens = lens.flip(0)
+    wlens[-3] = 0
+    assert torch.equal(t, want) and torch.equal(n, wlens) and torch.equal(r, torch.bincount(want[want >= 0], minlength=pages).to(torch.int32))
