@@ -51,11 +51,14 @@ class Decoder:
         self.cos_sin = torch.cat((angles.cos(), angles.sin()), 1).float()
         self.workspace = qg.new_workspace(qg.qg_paged_attention_workspace_bytes(rows, heads, kv_heads, head_dim), device)
         self.order = torch.arange(rows, dtype=torch.int32, device=device)
+        self.lacking = torch.zeros(1, dtype=torch.int32, device=device)
 
     def resize(self, new_lens: torch.Tensor) -> torch.Tensor:
-        """Begins (from 0), grows, cuts and ends (0) sequences; the number of pages that were missing, 0 if it was done."""
-        return qg.qg_pages_resize(self.tables, self.lens, self.refs, self.page, new_lens, planes=self.planes,
-                                  out=(self.tables, self.lens, self.refs))[3]
+        """Begins (from 0), grows, cuts and ends (0) sequences; the number of pages that were missing, 0 if it was done.  If some were,
+        nothing has changed, and step() passes over all rows until a resize has been done."""
+        self.lacking = qg.qg_pages_resize(self.tables, self.lens, self.refs, self.page, new_lens, planes=self.planes,
+                                          out=(self.tables, self.lens, self.refs))[3]
+        return self.lacking
 
     def fork(self, parents: torch.Tensor) -> None:
         """Row b goes on from where row parents[b] is (-1: is empty)."""
@@ -72,8 +75,10 @@ class Decoder:
     def step(self, x: torch.Tensor, live: torch.Tensor) -> torch.Tensor:
         """Hidden states after the last layer of one new token for each row of x [rows][hidden] (fp32) that `live` (bool) marks; its
         place, the last cell of its row, has been made by resize().  The other rows are passed over: nothing is stored
-        for them and what comes out is of no use."""
+        for them and what comes out is of no use.  Where the last resize lacked pages that holds for all rows, as their last cells are
+        those of tokens before (and maybe of other rows)."""
         H, Hkv, D, rows = self.heads, self.kv_heads, self.head_dim, self.rows
+        live = live & (self.lacking == 0)
         where = torch.where(live, self.order, -1)
         positions, lens = self.lens - 1, torch.where(live, self.lens, 0)
         update, stream = x, None
@@ -119,9 +124,9 @@ def main() -> None:
             ends[3:5] = 60
         grows = (t < ends) | (t >= 45) & (model.lens > 0)
         lacking = model.resize(torch.where(grows, model.lens + 1, model.lens))
-        y = model.step(torch.randn(rows, hidden, generator=g, device="cuda"), grows)
         if int(lacking):
             raise SystemExit("the pool is full")
+        y = model.step(torch.randn(rows, hidden, generator=g, device="cuda"), grows)
         if not bool(torch.isfinite(y[grows]).all()):
             raise SystemExit("the step gave values that are no numbers")
     live = model.compact()

@@ -98,3 +98,26 @@ def test_decoder_matches_the_whole_history(decoder, cache, bits, bound):
 def test_example_runs(decoder, capsys):
     decoder.main()
     assert "pages in use" in capsys.readouterr().out
+
+
+def test_a_full_pool_leaves_the_cells_alone(decoder):
+    # 4 pages: two rows fill them, a third row shares one's pages; a resize that lacks pages changes nothing, and neither does the step after it
+    print("[case] full pool", flush=True)
+    weights, final = decoder.random_weights(1, HIDDEN, INNER, H, HKV, D, 4, GROUP)
+    model = decoder.Decoder(weights, final, H, HKV, D, 4, GROUP, 3, pages=4, max_pages=6, page=PAGE)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = lambda: torch.randn(3, HIDDEN, generator=g, device="cuda")  # noqa: E731
+    for t in range(32):
+        assert int(model.resize(ints(t + 1, t + 1, 0))) == 0
+        model.step(x(), ints(1, 1, 0).bool())
+    model.fork(ints(0, 1, 0))
+    before = [t.clone() for t in [*model.planes, model.tables, model.lens, model.refs]]
+    assert int(model.resize(ints(33, 33, 33))) == 3
+    model.step(x(), ints(1, 1, 1).bool())
+    assert all(torch.equal(a, b) for a, b in zip(before, [*model.planes, model.tables, model.lens, model.refs]))
+    # once a row has ended the others go on
+    assert int(model.resize(ints(33, 0, 32))) == 0
+    at = (int(model.tables[0, 2]), slice(None), 0)
+    y = model.step(x(), ints(1, 0, 0).bool())
+    assert torch.isfinite(y[0]).all() and not torch.equal(model.k[0][at], before[0][0][at])
