@@ -273,3 +273,41 @@ def test_fork_of_more_rows_than_one_launch_takes(qg):
     wlens = lens.flip(0)
     wlens[-3] = 0
     assert torch.equal(t, want) and torch.equal(n, wlens) and torch.equal(r, torch.bincount(want[want >= 0], minlength=pages).to(torch.int32))
+
+
+@pytest.mark.parametrize("D", [8, 64, 128, 200, 256])
+@pytest.mark.parametrize("ct", [torch.bfloat16, torch.float16, F8])
+def test_probabilities_keep_fp32_for_fp32(qg, ct, D):
+    # Two keys, with scores 0 and s and values 0 and 1: out = p / (1 + p).  Scores are exact (s has 8 bits, or is the scale of a key of 1); exp errs by 4 U
+    # and U of the score, p by 2^-22 of itself in f16 and 2^-24 in bf16 (in two parts of 8 bits it would be off by 107 U here), out is rounded once.
+    print("[case] p", ct, D, flush=True)
+    s = torch.linspace(-1, 1, 65).to(torch.bfloat16).float()
+    n, page = len(s), 16
+    k, v = torch.zeros(n, 1, page, D), torch.zeros(n, 1, page, D)
+    k[:, 0, 1, 0], v[:, 0, 1] = 1 if ct is F8 else s, 1
+    ks = vs = None
+    if ct is F8:
+        ks, vs = torch.ones(n, 1, page), torch.ones(n, 1, page).cuda()
+        ks[:, 0, 1] = s
+        ks = ks.cuda()
+    q = torch.zeros(n, 2, D)
+    q[..., 0] = 1
+    out, lse = qg.qg_paged_attention(q.cuda(), k.to(ct).cuda(), v.to(ct).cuda(), torch.arange(n, dtype=torch.int32).view(-1, 1).cuda(),
+                                     torch.full((n,), 2, dtype=torch.int32).cuda(), 1.0, k_scale=ks, v_scale=vs, lse=True)
+    p = torch.exp(s.double())
+    want = (p / (1 + p))[:, None, None]
+    e = 2 * (2.0 ** -22 + 6 * U) + U
+    assert ((out.cpu().double() / want - 1).abs() <= e).all(), float((out.cpu().double() / want - 1).abs().max() / U)
+    assert ((lse.cpu().double() - torch.log(1 + p)[:, None]).abs() <= e).all()
+
+
+@pytest.mark.parametrize("rows,K,dt,out,group", [(37, 4099, torch.float32, torch.float32, 0), (5, 20000, torch.bfloat16, torch.float16, 0),
+                                                 (9, 90, torch.float16, F8, 9), (3, 4099, torch.bfloat16, F8, 0), (300, 1, torch.float32, F8, 1)])
+def test_norm_writes_h_over_its_inputs_element_by_element(qg, rows, K, dt, out, group):
+    for which in ("x", "residual"):
+        x, r = (torch.randn(rows, K, generator=gen(i)).to(dt).cuda() for i in (13, 14))
+        w = torch.randn(K, generator=gen(15)).cuda()
+        y0, h0, s0 = qg.qg_rms_norm(x, w, 1e-6, residual=r, dtype=out, group=group)
+        y, h, s = qg.qg_rms_norm(x, w, 1e-6, residual=r, h=x if which == "x" else r, dtype=out, group=group)
+        assert torch.equal(y.view(torch.uint8), y0.view(torch.uint8)) and torch.equal(h, h0) and h.data_ptr() == (x if which == "x" else r).data_ptr()
+        assert s is None or torch.equal(s, s0)
