@@ -566,18 +566,20 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
     total *= heads;
 
     // Two ways to cut it.  In equal runs of spans (piece = 0): a worker's run may end one head's keys and begin another's, and every such
-    // beginning (first page ids, first keys, adding up) costs 5 us, as much as some spans.  Or, where there is little to do, a unit is a
-    // piece of at most `piece` spans of one head's keys and every worker takes one: the longest take a little more, but each begins
-    // once.  (16 sequences of up to 2000 tokens, 8 key heads: 22.6 -> 21.1 us; 32 of up to 4093 in 8 bits: 34.6 -> 30.8)
+    // beginning (first page ids, first keys, adding up) costs as much as some spans.  Or a unit is a piece of at most `piece` spans of one
+    // head's keys and every worker takes one: the longest take a little more, but each begins once.  Pieces it is where the workers suffice for those of
+    // one span more than the longest run, or of three more in 8 bits, whose spans are half as long.  (One sequence of 14000, 8 key heads, bf16: runs 30.3 us,
+    // pieces 26.6; 16 in 8 bits: 45.1 and 39.5; but with pieces of 25 spans for runs of 21, 16 of 30000 in bf16, 115.7 and 132.6, of 21 for 17 with 32 key heads
+    // 91.7 and 111.2.  Where neither fits, the question costs half a microsecond.)
     int piece = 0;
     const int64_t least = total <= gridDim.x ? 1 : quotient(total + gridDim.x - 1, gridDim.x);
     if (a.batch <= 256 && least <= FEW) {
-        // the shortest of four pieces that workers suffice for; the units of two are added up in one word
+        // the shortest that will do; the units of two lengths are added up in one word
         const uint32_t exact = (uint32_t)least;
         const int spans = mine;
         int shift = 0;
-        for (int c = 0; c < 2 && !piece; ++c) {
-            const uint32_t shorter = exact + 2 * c, longer = c ? exact + 3 + exact / 4 : exact + 1;
+        for (int c = 0; c < (A::E4M3 ? 2 : 1) && !piece; ++c) {
+            const uint32_t shorter = exact + 2 * c, longer = shorter + 1;
             scan((int)(divided(spans, shorter) | divided(spans, longer) << 16), wave_sums[1 + c]);
             const int low = chunk & 0xffff, high = chunk >> 16;
             piece = low * heads <= (int)gridDim.x ? shorter : high * heads <= (int)gridDim.x ? longer : 0;
