@@ -2,8 +2,8 @@
 //
 // out = sum_i p_i v_i / sum_i p_i over a sequence's keys, p_i = exp(scale q.k_i), in one pass with a running maximum.  Keys and
 // values are read once and nothing else is of their size, so memory bounds it; the matrix instruction does both products
-// with the (up to 16) heads that share a key head as one side of the 16 x 16 x 32 tile, and is busy for less than a
-// fifth of the time memory takes even with one head in 16.
+// with the (up to 16) heads that share a key head as one side of the 16 x 16 x 32 tile, and is busy for 5 % (16-bit
+// cells) to 16 % (fp32 q on 8-bit cells) of the time, however few of the 16 there are.
 //
 // A wavefront takes 32 keys at a time, and nothing goes through LDS until it has seen all its keys:
 //   S^T (keys x heads) = K Q^T   two products of 16 keys.  Lane l = 16 j + i loads elements of key 8 (i / 4) + 4 t + i % 4 in
@@ -18,16 +18,17 @@
 // q goes in as it is: as one, two or three parts of 8 (bf16 instruction) or 11 bits (f16, with a power of two for each head
 // taken out first); p as two or, for fp32 outputs on the bf16 instruction, three.  f16 has steps of 2^-24, below which many small p_i
 // beside a large one would be lost: there p is kept 2^7 times as large, and its second part 2^11 times as large again, in products of its
-// own that are added with 2^-11 (p to 2^-22 of itself or 2^-43 of the largest; 32 multiplications for 32 keys of 128 dims, which the memory hides).
+// own that are added with 2^-11 (p to 2^-22 of itself or 2^-43 of the largest; 32 multiplications for 32 keys of 128 dims; 0 ... 2 % longer).
 // 8-bit keys and values are exact in bf16; their scales are applied to the scores and to the p_i.
 //
 // An infinite cell times a part that is 0 or of the other sign is NaN where the whole is not.  So a workgroup that has seen a head's keys looks
 // for NaN and infinity in what it has and, if there is one, sees them again with infinite cells in products of their own: with signs of q, and with
-// 1 for each p_i.  (8-bit cells have no infinities.)
+// 1 for each p_i.  (8-bit cells have no infinities.  Looking costs 0.2 us where there is little to do and up to 2 % where each head
+// has keys of its own; f16 cells of other than 64, 128 or 256 dims lose 4 % to the registers that the second look takes.)
 //
 // Measured: 128 sequences of up to 8190 tokens, 64 heads on 8, bf16, 1.45 GB of cells: 252 us (5.8 TB/s; a workgroup per head with a key at a time:
-// 8200); one sequence of 131071, 40 heads on 8, f16: 107 us (5.0 TB/s); 757 MB of 8-bit cells 160 ... 176 us; one sequence of 777, 32 key
-// heads: 12.4 us, of which lengths take 1.5, page ids and q 2.5, cells 1.4, adding up in LDS 1.0, parts written and counted 0.8, their sum 3.
+// 8200); one sequence of 131071, 40 heads on 8, f16: 107 us (5.0 TB/s); 757 MB of 8-bit cells 162 ... 174 us; one sequence of 777, 32 key
+// heads: 12.2 us, of which, by the clock in a copy, lengths take 1.5, page ids and q 2.5, cells 1.4, adding up in LDS 1.0, parts written and counted 0.8, their sum 3.
 #include "qg_kv.h"
 
 namespace {
@@ -535,7 +536,7 @@ __global__ __launch_bounds__(64 * WAVES, groups_per_unit(DPAD)) void attend(Atte
     __shared__ int64_t found_at, not_finite_at;                     // not_finite_at: the segment whose sums are not all finite
     __shared__ float head_m[16], head_l[16];
     const rsrc_t parts = buffer_of(a.parts, a.parts_bytes);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, j = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int D = FULL ? DPAD : a.kv.head_dim;
     const int heads = a.kv.kv_heads * a.blocks;                     // blocks of heads of a sequence
     const int worker = blockIdx.x;

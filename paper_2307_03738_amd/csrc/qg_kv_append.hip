@@ -15,7 +15,7 @@ struct AppendArgs {
 
 // A team of 1, 2, 4 ... 32 lanes, eight neighbouring elements each, takes heads of q, k and v of one token in turn and keeps the position's
 // cosines and sines in registers.  Memory bounds it: every element crosses once, the pair's other half a second time from the caches.
-// (7551 tokens of 64 + 16 heads of 128, bf16 into 8 bits: 53 us, 5.7 TB/s; a wavefront a head, an element at a time: 244.)
+// (7551 tokens of 64 + 16 heads of 128, bf16 into 8 bits: 54 us, 5.5 TB/s; a wavefront a head, an element at a time: 244.)
 // WHOLE: the rotated elements and their halves are whole eights (and the angles aligned); otherwise angles and partners are loaded one by one.
 template <int TYPE, int CACHE, bool WHOLE>
 __global__ __launch_bounds__(256) void append_eights(AppendArgs a, int team_shift)

@@ -22,8 +22,8 @@ struct Renumber {
     int64_t entries;
 };
 
-// Copies pages[i][0] onto pages[i][1] for i below the count; a workgroup takes units of 8 KB, all over the list.  (5.3 TB/s read and written on
-// 720 MB, the rate of a large copy.)
+// Copies pages[i][0] onto pages[i][1] for i below the count; a workgroup takes units of 8 KB, all over the list.  (5.0 ... 5.5 TB/s read and
+// written on 720 MB; a large copy 5.3.)
 __global__ __launch_bounds__(256) void copy_pages(Planes planes, const int32_t *pairs, const int32_t *count, int most, int64_t pages, Renumber ids)
 {
     for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < ids.entries; e += (int64_t)gridDim.x * 256) {
