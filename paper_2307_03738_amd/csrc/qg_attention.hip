@@ -26,9 +26,9 @@
 // 1 for each p_i.  (8-bit cells have no infinities.  Looking costs 0.2 us where there is little to do and up to 2 % where each head
 // has keys of its own; f16 cells of other than 64, 128 or 256 dims lose 4 % to the registers that the second look takes.)
 //
-// Measured: 128 sequences of up to 8190 tokens, 64 heads on 8, bf16, 1.45 GB of cells: 252 us (5.8 TB/s; a workgroup per head with a key at a time:
-// 8200); one sequence of 131071, 40 heads on 8, f16: 107 us (5.0 TB/s); 757 MB of 8-bit cells 162 ... 174 us; one sequence of 777, 32 key
-// heads: 12.2 us, of which, by the clock in a copy, lengths take 1.5, page ids and q 2.5, cells 1.4, adding up in LDS 1.0, parts written and counted 0.8, their sum 3.
+// Measured: 128 sequences of up to 8190 tokens, 64 heads on 8, bf16, 1.45 GB of cells: 253 us (5.8 TB/s; a workgroup per head with a key at a time:
+// 8200); one sequence of 131071, 40 heads on 8, f16: 106 us (5.1 TB/s); 757 MB of 8-bit cells 167 ... 180 us; one sequence of 777, 32 key
+// heads: 12.3 us, of which, by the clock in a copy, lengths take 1.5, page ids and q 2.5, cells 1.4, adding up in LDS 1.0, parts written and counted 0.8, their sum 3.
 #include "qg_kv.h"
 
 namespace {

@@ -89,7 +89,7 @@ __device__ inline float sum_of_wave(float v)
 // A row in the registers of `team` lanes (64 ... 1024), eight neighbouring elements at a time, R times; rows, residual, h and y cross memory
 // once.  Memory bounds it from some hundred rows on, the one way through loads, two sums and stores below.  A workgroup takes rows
 // in turn, keeps the weight and asks for the next row before it adds up this one.  (A workgroup of 256 per row that reads the row again for
-// its output: 8.7 us for one row of 4096, 238 for 4099 x 8192 bf16 to e4m3; this 2.7 and 48, 4.9 TB/s, 100 for 8192 x 4096 fp32, 5.4 TB/s.)
+// its output: 8.7 us for one row of 4096, 238 for 4099 x 8192 bf16 to e4m3; this 2.6 and 48, 5.0 TB/s, 102 for 8192 x 4096 fp32, 5.3 TB/s.)
 template <int TYPE, int YTYPE, int R>
 __global__ __launch_bounds__(1024, 4) void norm_rows8(NormArgs a, int weight_type, int64_t rows, int team)
 {

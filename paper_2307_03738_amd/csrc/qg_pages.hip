@@ -133,7 +133,7 @@ constexpr int FREE_IN_LDS = 4096;
 
 // Workgroup 0 keeps the book: pages that go and pages that come are dealt out over its lanes one by one, whatever their rows, so its time
 // follows what changes (and the references, which it passes on and searches for free pages from the lowest id on).  The other
-// workgroups pass on the table entries that do not change.  (64 rows of 256 entries, 8192 pages: 13.7 us, a chain of some ten loads and sums; one
+// workgroups pass on the table entries that do not change.  (64 rows of 256 entries, 8192 pages: 14.2 us, a chain of some ten loads and sums; one
 // workgroup for all of it, an entry a lane: 33.)
 __global__ __launch_bounds__(BOOK_LANES) void resize_book(Book b, const int32_t *new_lens, ResizeSpace w, int32_t *lacking)
 {
