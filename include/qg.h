@@ -437,6 +437,78 @@ int qg_pages_copy(const qg_page_plane *planes /* HOST */, int n_planes, int64_t 
 /* Scratch of qg_pages_resize and qg_pages_compact (16-byte aligned, needs no preparation). */
 size_t qg_pages_workspace_bytes(int rows, int max_pages, int64_t pages);
 
+/* ---------------------------------------------------------------------------------------------
+ * Experts: a layer whose matrices are chosen by token.  A token's router gives a logit for each expert; qg_route chooses and
+ * weighs, qg_expert_plan orders the choices by expert, qg_experts_product multiplies each expert's tokens with its packed matrix,
+ * qg_experts_combine adds a token's results up.  The conventions above hold; an empty batch is QG_OK and nothing about the choices
+ * is asked of the host (the calls can be captured and replayed).  Forward only, as all of this library.
+ * --------------------------------------------------------------------------------------------- */
+typedef enum { QG_SOFTMAX = 0, QG_SIGMOID = 1 } qg_score;
+#define QG_MAX_EXPERTS 1024
+#define QG_MAX_CHOICES 64
+
+/* The top_k experts of each token.  p = softmax of the token's logits, or sigmoid of each.  Experts rank by p + bias, or by their logits
+ * if there is no bias; of equal ones the lower index comes first.  With top_groups < groups only experts of the top_groups best groups
+ * (of experts / groups neighbours) take part; a group ranks as its best expert does (group_best 1) or by the sum of its two
+ * largest p (+ bias) (group_best 2; of the one, if there is one).  weights = p, without the bias, times scale; renormalised: p over the sum of the chosen ones' p
+ * (0 where that is 0) times scale.  Scores that rank are kept in 64 bits.
+ * An expert whose logit (or bias) is -infinity is switched off; where fewer than top_k are left the last ids are -1 and their weights 0.
+ * NaN among a token's logits, or biases: experts that have it are switched off, and the token's weights are NaN. */
+typedef struct qg_route_desc {
+    const void *logits;   /* [tokens][experts] of `type`, rows logits_stride elements apart */
+    const float *bias;    /* [experts], or NULL */
+    int32_t *ids;         /* [tokens][top_k], the best first */
+    float *weights;       /* [tokens][top_k] */
+    int64_t tokens, logits_stride;
+    int type;             /* QG_F32, QG_BF16 or QG_F16 */
+    int experts, top_k;   /* top_k experts of top_groups groups at most */
+    int score;            /* qg_score */
+    int groups, top_groups, group_best;
+    int renormalise;
+    float scale;
+} qg_route_desc;
+int qg_route(const qg_route_desc *d /* HOST */, void *stream);
+
+/* Slots for all choices, ordered by expert, those of one expert by token and choice:
+ *   offsets [experts + 1]: expert e has the slots offsets[e] ... offsets[e + 1] - 1
+ *   slot_tokens [tokens * top_k]: each slot's token, -1 from offsets[experts] on
+ *   slots [tokens][top_k]: each choice's slot; -1 for an id outside 0 ... experts - 1, which gets none */
+int qg_expert_plan(const int32_t *ids, int64_t tokens, int top_k, int experts, int32_t *offsets, int32_t *slot_tokens, int32_t *slots, void *stream);
+
+/* For each slot p of expert e, with x the row rows[p] of X (row p, if rows is NULL):
+ *   y[p][n] = sum_k What_e[n][k] x[k]                  (N columns), or, gated, with gate and up side by side as in qg_gemv_swiglu,
+ *   y[p][n] = silu(gate[n]) * up[n]                    (N / 2 columns: What_e rows [0, N / 2) are gate, the others up)
+ * per group as s * sum (q - z) x, sums in fp32.  A row outside 0 ... x_rows - 1 counts as zeros.  Rows of y past offsets[experts] are left
+ * as they were.  NaN and infinity in X reach their own rows of y alone.  y overlaps no input. */
+typedef struct qg_experts_desc {
+    const void *packed;       /* [experts] blobs of QG_LAYOUT_DEVICE (qg_pack), expert_stride bytes apart; 16-byte aligned */
+    const void *x;            /* [x_rows][K] of x_type, rows x_stride elements apart (a multiple of 8); 16-byte aligned */
+    const int32_t *offsets;   /* [experts + 1], not decreasing, of qg_expert_plan */
+    const int32_t *rows;      /* [slots], or NULL */
+    void *y;                  /* [slots][N or N / 2] of y_type */
+    int64_t N, K, expert_stride, x_rows, x_stride, slots;
+    int bits, group, experts;
+    int x_type, y_type;       /* QG_F32, QG_BF16 or QG_F16 */
+    int gated;
+    void *workspace;          /* 16-byte aligned, needs no preparation; calls that overlap in time must not share one */
+    size_t workspace_bytes;   /* qg_experts_workspace_bytes() */
+} qg_experts_desc;
+int qg_experts_product(const qg_experts_desc *d /* HOST */, void *stream);
+size_t qg_experts_workspace_bytes(int64_t x_rows, int64_t slots, int64_t K, int experts, int x_type);
+
+/* out[t][n] = residual[t][n] + sum_j weights[t][j] * y[slots[t][j]][n], in fp32 in the order of j, rounded once.  A slot outside 0 ... y_rows - 1 adds nothing. */
+typedef struct qg_combine_desc {
+    const void *y;            /* [y_rows][N] of `type` */
+    const int32_t *slots;     /* [tokens][top_k] */
+    const float *weights;     /* [tokens][top_k] */
+    const void *residual;     /* [tokens][N] of out_type, rows residual_stride apart, or NULL */
+    void *out;                /* [tokens][N] of out_type; may be the residual where its rows lie N apart */
+    int64_t y_rows, tokens, N, residual_stride;
+    int type, out_type;       /* QG_F32, QG_BF16 or QG_F16 */
+    int top_k;
+} qg_combine_desc;
+int qg_experts_combine(const qg_combine_desc *d /* HOST */, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -127,6 +127,16 @@ def lib():
         L.qg_pages_copy.argtypes = [cp, i32, i64, vp, i32, vp]
         L.qg_pages_workspace_bytes.restype = sz
         L.qg_pages_workspace_bytes.argtypes = [i32, i32, i64]
+        L.qg_route.restype = i32
+        L.qg_route.argtypes = [cp, vp]
+        L.qg_expert_plan.restype = i32
+        L.qg_expert_plan.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp]
+        L.qg_experts_product.restype = i32
+        L.qg_experts_product.argtypes = [cp, vp]
+        L.qg_experts_workspace_bytes.restype = sz
+        L.qg_experts_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+        L.qg_experts_combine.restype = i32
+        L.qg_experts_combine.argtypes = [cp, vp]
         _LIB = L
     return _LIB
 
@@ -801,3 +811,150 @@ def qg_pages_copy(planes: Sequence[torch.Tensor], pairs: torch.Tensor):
         raise ValueError("pairs: expected [count][2]")
     _check((_LIB or lib()).qg_pages_copy(_planes(planes, pages), len(planes), pages, _dev(pairs, torch.int32, "pairs").data_ptr(),
                                          pairs.shape[0], _stream()), "qg_pages_copy")
+
+
+# --- a layer of experts -----------------------------------------------------------------------------------------
+
+_ROUTE = struct.Struct("4Q2q8if4x").pack
+_EXPERTS = struct.Struct("5Q6q6i2Q").pack
+_COMBINE = struct.Struct("5Q4q3i4x").pack
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _matrix_rows(t: torch.Tensor, name: str, shape=None, types=_FLOATS):
+    """(address, stride of rows, type) of a matrix whose rows may lie apart."""
+    kind = _type(t, name, types)
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name}: expected a matrix" + (f" of shape {tuple(shape)}" if shape is not None else ""))
+    stride, element = t.stride()
+    if element != 1 and t.shape[1] > 1:
+        raise ValueError(f"{name}: expected contiguous rows")
+    return t.data_ptr(), stride, kind
+
+
+def qg_route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = None, score: str = "softmax", groups: int = 1,
+             top_groups: Optional[int] = None, group_best: int = 1, renormalise: bool = True, scale: float = 1.0,
+             ids: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None):
+    """(ids, weights) [tokens][top_k] of the experts that logits [tokens][experts] choose, the best first: scores are softmax or sigmoid of the
+    logits, `bias` [experts] counts for the choice alone, and of `groups` of neighbouring experts the top_groups best take part.
+    An id -1 has weight 0: no expert was left (a logit of -inf is an expert that is switched off)."""
+    lp, stride, kind = _matrix_rows(logits, "logits")
+    tokens, experts = logits.shape
+    if score not in _SCORES:
+        raise ValueError("score: softmax or sigmoid")
+    bp = 0 if bias is None else _whole(bias, torch.float32, "bias", (experts,))
+    shape, device = (tokens, top_k), logits.device
+    if top_k <= 0:
+        _check(2, "qg_route")
+    if ids is None:
+        ids = _rows(tokens, top_k, torch.int32, device)
+    else:
+        _whole(ids, torch.int32, "ids", shape)
+    if weights is None:
+        weights = _rows(tokens, top_k, torch.float32, device)
+    else:
+        _whole(weights, torch.float32, "weights", shape)
+    rc = (_LIB or lib()).qg_route(_ROUTE(lp, bp, ids.data_ptr(), weights.data_ptr(), tokens, stride, kind, experts, top_k, _SCORES[score],
+                                         groups, groups if top_groups is None else top_groups, group_best, 1 if renormalise else 0, scale), _stream())
+    if rc != 0:
+        _check(rc, "qg_route")
+    return ids, weights
+
+
+def qg_expert_plan(ids: torch.Tensor, experts: int, out=None):
+    """(offsets [experts + 1], slot_tokens [tokens * top_k], slots [tokens][top_k]): the choices ids [tokens][top_k] ordered by expert.
+    Expert e has the slots offsets[e] ... offsets[e + 1] - 1; an id outside 0 ... experts - 1 gets none (-1).  out: the three to write into."""
+    shape = ids.shape
+    if len(shape) != 2:
+        raise ValueError("ids: expected [tokens][top_k]")
+    tokens, top_k = shape
+    ip, device = _whole(ids, torch.int32, "ids", shape), ids.device
+    if experts <= 0 or top_k <= 0:
+        _check(2, "qg_expert_plan")
+    if out is None:
+        offsets, slot_tokens, slots = _ints(experts + 1, device), _ints(tokens * top_k, device), _rows(tokens, top_k, torch.int32, device)
+    else:
+        offsets, slot_tokens, slots = out
+        _whole(offsets, torch.int32, "offsets", (experts + 1,))
+        _whole(slot_tokens, torch.int32, "slot_tokens", (tokens * top_k,))
+        _whole(slots, torch.int32, "slots", shape)
+    rc = (_LIB or lib()).qg_expert_plan(ip, tokens, top_k, experts, offsets.data_ptr(), slot_tokens.data_ptr(), slots.data_ptr(), _stream())
+    if rc != 0:
+        _check(rc, "qg_expert_plan")
+    return offsets, slot_tokens, slots
+
+
+def qg_experts_workspace_bytes(x_rows: int, slots: int, K: int, experts: int, dtype: torch.dtype = torch.float32) -> int:
+    return int(lib().qg_experts_workspace_bytes(x_rows, slots, K, experts, _FLOATS[dtype]))
+
+
+def qg_experts_product(packed: torch.Tensor, N: int, K: int, bits: int, group: int, x: torch.Tensor, offsets: torch.Tensor,
+                       rows: Optional[torch.Tensor] = None, gated: bool = False, dtype: Optional[torch.dtype] = None,
+                       y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y[p] = What_e x[rows[p]] (x[p], if rows is None) for each slot p of each expert e (offsets of qg_expert_plan) in `dtype` (x's own if not given);
+    gated: silu(gate) * up of N / 2 columns, What_e's first N / 2 rows being gate.  packed: [experts][bytes], an expert's qg_pack blob a row.
+    Slots past the last expert's are not written."""
+    xp, xs, kind = _matrix_rows(x, "x")
+    if packed.dtype is not torch.uint8 or packed.dim() != 2 or not packed.is_cuda or (packed.stride(1) != 1 and packed.shape[1] > 1):
+        raise ValueError("packed: expected a uint8 tensor [experts][bytes] on the GPU")
+    experts, nbytes = packed.shape
+    x_rows, width = x.shape
+    if width != K or nbytes < qg_packed_bytes(N, K, bits, group, QG_LAYOUT_DEVICE):
+        _check(2, "qg_experts_product")
+    op = _whole(offsets, torch.int32, "offsets", (experts + 1,))
+    if rows is None:
+        rp, slots = 0, x_rows if y is None else y.shape[0]
+    else:
+        slots = rows.shape[0]
+        rp = _whole(rows, torch.int32, "rows", (slots,))
+    columns = N // 2 if gated else N
+    if y is None:
+        y = _rows(slots, columns, x.dtype if dtype is None else dtype, x.device)
+    else:
+        _whole(y, y.dtype if dtype is None else dtype, "y", (slots, columns))
+    ykind = _type(y, "y")
+    L = _LIB or lib()
+    if workspace is None:
+        size = L.qg_experts_workspace_bytes(x_rows, slots, K, experts, kind)
+        wp = 0
+        if size:
+            workspace = _bytes(size, x.device)
+            wp = workspace.data_ptr()
+    else:
+        wp, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    rc = L.qg_experts_product(_EXPERTS(packed.data_ptr(), xp, op, rp, y.data_ptr(), N, K, packed.stride(0), x_rows, xs, slots,
+                                       bits, group, experts, kind, ykind, 1 if gated else 0, wp, size), _stream())
+    if rc != 0:
+        _check(rc, "qg_experts_product")
+    return y
+
+
+def qg_experts_combine(y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                       dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[t] = residual[t] + sum over j of weights[t][j] y[slots[t][j]] in `dtype` (the residual's, or y's own, if not given); a slot
+    outside y's rows adds nothing.  out may be the residual."""
+    kind = _type(y, "y")
+    if y.dim() != 2 or not y.is_contiguous():
+        raise ValueError("y: expected a contiguous matrix [slots][N]")
+    y_rows, N = y.shape
+    shape = slots.shape
+    if len(shape) != 2:
+        raise ValueError("slots: expected [tokens][top_k]")
+    tokens, top_k = shape
+    sp, wp = _whole(slots, torch.int32, "slots", shape), _whole(weights, torch.float32, "weights", shape)
+    if dtype is None:
+        dtype = out.dtype if out is not None else residual.dtype if residual is not None else y.dtype
+    if out is None:
+        out = _rows(tokens, N, dtype, y.device)
+    else:
+        _whole(out, dtype, "out", (tokens, N))
+    okind = _type(out, "out")
+    rp = rs = 0
+    if residual is not None:
+        if residual.dtype is not dtype:
+            raise ValueError(f"residual: expected a {dtype} tensor")
+        rp, rs, _ = _matrix_rows(residual, "residual", (tokens, N))
+    rc = (_LIB or lib()).qg_experts_combine(_COMBINE(y.data_ptr(), sp, wp, rp, out.data_ptr(), y_rows, tokens, N, rs, kind, okind, top_k), _stream())
+    if rc != 0:
+        _check(rc, "qg_experts_combine")
+    return out

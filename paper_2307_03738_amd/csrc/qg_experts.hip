@@ -1,0 +1,163 @@
+// qg_experts_product: y[p] = What_e x[rows[p]] for the slots p of each expert e.
+#include "qg_experts.h"
+
+namespace {
+
+constexpr int ANY_ROWS = 4;
+
+template <int TYPE>
+__device__ inline void eight_of(const char *x, int64_t at, float *v) { load_eight<TYPE>(x, at, v); }
+
+// Codes of a cell less its zero-point, exact.
+template <int BITS>
+__device__ inline void cell_weights(const uint4 (&v)[Fmt<BITS>::PLANES], int j, float zero, float *w)
+{
+    if constexpr (BITS == 3) {
+        const uint32_t a = word_of(v[0], j), b = word_of(v[1], j), c = word_of(v[2], j);
+        const uint32_t t = ((a >> 6) & 0x03030303u) | ((b >> 4) & 0x0c0c0c0cu) | ((c >> 2) & 0x30303030u);
+        const uint32_t words[4] = {a, b, c, t};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = (float)((words[i / 8] >> (8 * (i % 4) + (i % 8 < 4 ? 0 : 3))) & 7u) - zero;
+    } else {
+        const uint32_t word = word_of(v[0], j);
+#pragma unroll
+        for (int i = 0; i < 32 / BITS; ++i) w[i] = (float)((word >> (BITS * i)) & ((1u << BITS) - 1)) - zero;
+    }
+}
+
+// Any group of whole cells, in fp32 multiply-adds: a wavefront takes 64 outputs (a lane one) of four slots and a quarter of K's units,
+// the quarters meet in LDS.  Bound by the vector ALU from a few rows on; groups of whole 32 k have kernels of their own.
+template <int BITS, int TYPE>
+__global__ __launch_bounds__(256) void experts_any(QgExpertsArgs a)
+{
+    using F = Fmt<BITS>;
+    constexpr int CELL = F::CELL, P = F::PLANES, ZPER = 32 / F::ZBITS;
+    __shared__ float sums[3][2][ANY_ROWS][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t block = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
+    const int64_t column_tile = block / a.row_tiles;
+    const ExpertTile t = expert_tile(a, block - column_tile * a.row_tiles, ANY_ROWS);
+    const int64_t column = column_tile * 64 + lane;
+    if (t.rows == 0 || column_tile * 64 >= a.columns) return;
+    const char *blob = a.packed + t.expert * a.expert_stride;
+    int64_t from[ANY_ROWS];
+#pragma unroll
+    for (int r = 0; r < ANY_ROWS; ++r) {
+        int64_t row = -1;
+        if (r < t.rows) row = a.rows ? a.rows[t.begin + r] : t.begin + r;
+        from[r] = row >= 0 && row < a.x_rows ? row * a.x_stride : -1;
+    }
+    float acc[2][ANY_ROWS] = {};
+    const int units = (a.K + 4 * CELL - 1) / (4 * CELL);
+    for (int part = 0; part < 1 + a.gated; ++part) {
+        const int64_t n = (column < a.columns ? column : a.columns - 1) + (int64_t)part * a.columns;
+        const char *codes = blob + (n >> 6) * a.tile_codes + (n & 63) * 16;
+        const char *scales = blob + a.scales_off + (n >> 6) * a.tile_scales + (n & 63) * 4;
+        const char *zeros = blob + a.zeros_off + (n >> 6) * a.tile_zeros + (n & 63) * 4;
+        for (int u = wave; u < units; u += 4) {
+            uint4 v[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p) v[p] = *(const uint4 *)(codes + ((int64_t)u * P + p) * 1024);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = (u * 4 + j) * CELL;
+                if (k >= a.K) break;
+                const int g = k / a.group;
+                const float s = *(const float *)(scales + (int64_t)g * 256);
+                const uint32_t zw = *(const uint32_t *)(zeros + (int64_t)(g / ZPER) * 256);
+                float w[CELL];
+                cell_weights<BITS>(v, j, (float)((zw >> (g % ZPER * F::ZBITS)) & ((1u << F::ZBITS) - 1)), w);
+#pragma unroll
+                for (int r = 0; r < ANY_ROWS; ++r) {
+                    if (from[r] < 0) continue;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int o = 0; o < CELL; o += 8) {
+                        float x[8];
+                        eight_of<TYPE>(a.x, from[r] + k + o, x);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(w[o + i], x[i], sum);
+                    }
+                    acc[part][r] = __builtin_fmaf(s, sum, acc[part][r]);
+                }
+            }
+        }
+    }
+    if (wave > 0)
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int r = 0; r < ANY_ROWS; ++r) sums[wave - 1][part][r][lane] = acc[part][r];
+    __syncthreads();
+    if (wave > 0 || column >= a.columns) return;
+#pragma unroll
+    for (int r = 0; r < ANY_ROWS; ++r) {
+        if (r >= t.rows) break;
+        float y[2];
+#pragma unroll
+        for (int part = 0; part < 2; ++part) y[part] = acc[part][r] + sums[0][part][r][lane] + sums[1][part][r][lane] + sums[2][part][r][lane];
+        store_typed(a.y_type, a.y, (t.begin + r) * a.columns + column, a.gated ? silu(y[0]) * y[1] : y[0]);
+    }
+}
+
+template <int BITS>
+int any_launch(const QgExpertsArgs &a, int64_t blocks, hipStream_t st)
+{
+    const unsigned across = (unsigned)(blocks < QG_MOST_GROUPS ? blocks : QG_MOST_GROUPS);
+    const dim3 grid(across, (unsigned)((blocks + across - 1) / across));
+    if (a.x_type == QG_F32) experts_any<BITS, QG_F32><<<grid, 256, 0, st>>>(a);
+    else if (a.x_type == QG_BF16) experts_any<BITS, QG_BF16><<<grid, 256, 0, st>>>(a);
+    else experts_any<BITS, QG_F16><<<grid, 256, 0, st>>>(a);
+    return qg_launch_status();
+}
+
+}  // namespace
+
+extern "C" size_t qg_experts_workspace_bytes(int64_t x_rows, int64_t slots, int64_t K, int experts, int x_type)
+{
+    return 0;
+}
+
+extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
+{
+    if (!d) return QG_ERR_NULL;
+    QgLayout L;
+    const int status = qg_make_layout(d->N, d->K, d->bits, d->group, &L);
+    if (status != QG_OK) return status;
+    if (!qg_float_type(d->x_type) || !qg_float_type(d->y_type) || d->experts > QG_MAX_EXPERTS) return QG_ERR_UNSUPPORTED;
+    if (d->experts <= 0 || d->slots < 0 || d->slots > 0x7fffffff || d->x_rows < 0 || d->x_rows > 0x7fffffff || (d->gated && d->N % 2)) return QG_ERR_SHAPE;
+    if ((d->x_rows > 1 && d->x_stride < d->K) || (d->experts > 1 && (d->expert_stride < 0 || (size_t)d->expert_stride < L.total))) return QG_ERR_SHAPE;
+    if (d->slots == 0) return QG_OK;
+    if (!d->packed || (!d->x && d->x_rows) || !d->offsets || !d->y) return QG_ERR_NULL;
+    if (!qg_aligned16(d->packed) || d->expert_stride % 16 || !qg_aligned16(d->x) || (d->x_rows > 1 && d->x_stride % 8) || !qg_aligned_to(d->offsets, 4) ||
+        !qg_aligned_to(d->rows, 4) || !qg_aligned_to(d->y, qg_type_bytes(d->y_type)) || !qg_aligned16(d->workspace)) return QG_ERR_ALIGN;
+    if (d->workspace_bytes < qg_experts_workspace_bytes(d->x_rows, d->slots, d->K, d->experts, d->x_type)) return QG_ERR_WORKSPACE;
+    QgExpertsArgs a = {};
+    a.packed = (const char *)d->packed;
+    a.x = (const char *)d->x;
+    a.offsets = d->offsets;
+    a.rows = d->rows;
+    a.y = d->y;
+    a.expert_stride = d->expert_stride;
+    a.x_rows = d->x_rows;
+    a.x_stride = d->x_stride;
+    a.slots = d->slots;
+    a.scales_off = (int64_t)L.scales_off;
+    a.zeros_off = (int64_t)L.zeros_off;
+    a.tile_codes = (int64_t)L.units * L.planes * 1024;
+    a.tile_scales = L.ngroups * 256;
+    a.tile_zeros = L.zwords * 256;
+    a.N = (int)d->N;
+    a.K = (int)d->K;
+    a.gated = d->gated != 0;
+    a.columns = a.gated ? a.N / 2 : a.N;
+    a.group = d->group;
+    a.experts = d->experts;
+    a.x_type = d->x_type;
+    a.y_type = d->y_type;
+    const hipStream_t st = (hipStream_t)stream;
+    a.row_tiles = (int)qg_most_tiles(d->slots, d->experts, ANY_ROWS);
+    const int64_t blocks = (int64_t)a.row_tiles * ((a.columns + 63) / 64);
+    if (blocks > (int64_t)QG_MOST_GROUPS * 65535) return QG_ERR_SHAPE;
+    return d->bits == 4 ? any_launch<4>(a, blocks, st) : d->bits == 3 ? any_launch<3>(a, blocks, st) : any_launch<2>(a, blocks, st);
+}

@@ -1,0 +1,435 @@
+// qg_route, qg_expert_plan, qg_experts_combine: what surrounds the experts' products.
+#include "qg_types.h"
+
+namespace {
+
+// --- choice -------------------------------------------------------------------------------------------------------
+
+struct RouteArgs {
+    const void *logits;
+    const float *bias;
+    int32_t *ids;
+    float *weights;
+    int64_t tokens, stride;
+    int type, experts, top_k, sigmoid, groups, top_groups, two, renormalise;
+    uint32_t group_magic;      // 2^32 / group size, rounded up: e / size = umulhi(e, magic) (e < 2^16, size > 1)
+    float scale;
+};
+
+template <typename T> __device__ inline T lowest() { return (T)-__builtin_inff(); }
+
+template <int L, typename T>
+__device__ inline T team_max(T v)
+{
+#pragma unroll
+    for (int off = 1; off < L; off *= 2) {
+        const T o = __shfl_xor(v, off);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+template <int L>
+__device__ inline int team_min(int v)
+{
+#pragma unroll
+    for (int off = 1; off < L; off *= 2) v = min(v, __shfl_xor(v, off));
+    return v;
+}
+template <int L, typename T>
+__device__ inline T team_sum(T v)
+{
+#pragma unroll
+    for (int off = 1; off < L; off *= 2) v += __shfl_xor(v, off);
+    return v;
+}
+
+__device__ inline float logit_of(const RouteArgs &a, int64_t at)
+{
+    return a.type == QG_F32 ? load_as_float<QG_F32>(a.logits, at) : a.type == QG_BF16 ? load_as_float<QG_BF16>(a.logits, at) : load_as_float<QG_F16>(a.logits, at);
+}
+
+// L lanes take a token, V experts each: expert v * L + lane.  KEY: what experts rank by, fp32 logits, or, with a bias or
+// groups ranked by sums, scores in fp64 (two fp32 scores with a bias tie or swap in about one of 10^5 choices).
+template <int L, int V, typename KEY>
+__global__ __launch_bounds__(256) void route(RouteArgs a)
+{
+    constexpr bool SCORES = sizeof(KEY) == 8;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    const int64_t wanted = (int64_t)blockIdx.x * (256 / L) + team;
+    const int64_t token = wanted < a.tokens ? wanted : a.tokens - 1;      // lanes past the end work along and store nothing
+    const int64_t row = token * a.stride;
+
+    float l[V];
+    bool nan = false;
+    float most = lowest<float>();
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int e = v * L + lane;
+        l[v] = e < a.experts ? logit_of(a, row + e) : lowest<float>();
+        if (l[v] != l[v]) {
+            nan = true;
+            l[v] = lowest<float>();
+        }
+        most = l[v] > most ? l[v] : most;
+    }
+    // softmax: the largest logit and, where a weight needs it, the sum of exponentials; of infinite logits each counts 1 and the others 0
+    const bool sums = !a.sigmoid && (SCORES || !a.renormalise);
+    if (!a.sigmoid) most = team_max<L>(most);
+    const bool infinite = most == __builtin_inff();
+    auto raised = [&](float x) { return infinite ? (x == most ? 1.0 : 0.0) : x == lowest<float>() ? 0.0 : exp((double)x - (double)most); };
+    double total = 1.0;
+    KEY key[V];
+    double part = 0.0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if constexpr (SCORES) {
+            const double p = a.sigmoid ? 1.0 / (1.0 + exp(-(double)l[v])) : raised(l[v]);
+            part += p;
+            key[v] = p;
+        } else {
+            key[v] = l[v];
+            if (sums) part += raised(l[v]);
+        }
+    }
+    if (sums) total = team_sum<L>(part);
+    if constexpr (SCORES) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = v * L + lane;
+            if (!a.sigmoid) key[v] /= total;
+            if (a.bias && e < a.experts) key[v] += (double)a.bias[e];
+            if (l[v] == lowest<float>() || key[v] != key[v]) {
+                nan |= key[v] != key[v] && l[v] != lowest<float>();
+                key[v] = lowest<KEY>();
+            }
+        }
+    }
+    const uint64_t nans = __ballot(nan);
+    nan = ((nans >> (threadIdx.x % 64 / L * L)) & (L == 64 ? ~0ull : (1ull << (L % 64)) - 1)) != 0;
+
+    if (a.top_groups < a.groups) {
+        // keys of the token, then its groups' ranks
+        KEY *keys = (KEY *)smem + (size_t)team * (a.experts + a.groups), *ranks = keys + a.experts;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = v * L + lane;
+            if (e < a.experts) keys[e] = key[v];
+        }
+        __syncthreads();
+        const int size = a.experts / a.groups;
+        for (int g = lane; g < a.groups; g += L) {
+            KEY first = lowest<KEY>(), second = lowest<KEY>();
+            for (int i = 0; i < size; ++i) {
+                const KEY k = keys[g * size + i];
+                if (k > first) {
+                    second = first;
+                    first = k;
+                } else if (k > second) {
+                    second = k;
+                }
+            }
+            ranks[g] = a.two && second > lowest<KEY>() ? first + second : first;
+        }
+        __syncthreads();
+        // scores rank groups; without a bias experts rank by their logits all the same (sigmoids near 1 and far softmaxes tie)
+        bool kept[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = v * L + lane, g = size == 1 ? e : (int)__umulhi((uint32_t)e, a.group_magic);
+            int before = 0;
+            if (e < a.experts) {
+                const KEY mine = ranks[g];
+                for (int o = 0; o < a.groups; ++o) {
+                    const KEY r = ranks[o];
+                    before += r > mine || (r == mine && o < g);
+                }
+            }
+            kept[v] = before < a.top_groups;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            key[v] = !kept[v] ? lowest<KEY>() : SCORES && !a.bias ? (KEY)l[v] : key[v];
+    }
+
+    int mine = -1;                         // lane j: the token's choice j
+    for (int j = 0; j < a.top_k; ++j) {
+        KEY best = key[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) best = key[v] > best ? key[v] : best;
+        best = team_max<L>(best);
+        if (!(best > lowest<KEY>())) {     // none is left for this token; others of the wavefront may go on
+            best = lowest<KEY>();
+        }
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int v = V - 1; v >= 0; --v)
+            if (key[v] == best) at = v * L + lane;
+        at = team_min<L>(at);
+        const bool real = best > lowest<KEY>();
+        if (lane == j) mine = real ? at : -1;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v * L + lane == at) key[v] = lowest<KEY>();
+    }
+    double p = 0.0;
+    if (mine >= 0) {
+        const float x = logit_of(a, row + mine);
+        p = a.sigmoid ? 1.0 / (1.0 + exp(-(double)x)) : raised(x);
+    }
+    if (a.renormalise) {
+        const double sum = team_sum<L>(p);
+        p = sum == 0.0 ? 0.0 : p / sum;
+    } else if (!a.sigmoid) {
+        p /= total == 0.0 ? 1.0 : total;
+    }
+    if (wanted < a.tokens && lane < a.top_k) {
+        a.ids[token * a.top_k + lane] = mine;
+        a.weights[token * a.top_k + lane] = nan ? __uint_as_float(0x7fc00000u) : (float)(p * (double)a.scale);
+    }
+}
+
+template <int L, int V>
+void route_launch(const RouteArgs &a, bool scores, hipStream_t st)
+{
+    const int teams = 256 / L;
+    RouteArgs b = a;
+    const int64_t turn = QG_MOST_GROUPS * teams;
+    for (int64_t done = 0; done < a.tokens; done += turn) {
+        b.tokens = a.tokens - done < turn ? a.tokens - done : turn;
+        b.logits = (const char *)a.logits + done * a.stride * qg_type_bytes(a.type);
+        b.ids = a.ids + done * a.top_k;
+        b.weights = a.weights + done * a.top_k;
+        const unsigned blocks = (unsigned)((b.tokens + teams - 1) / teams);
+        const size_t lds = a.top_groups < a.groups ? (size_t)teams * (a.experts + a.groups) * (scores ? 8 : 4) : 0;
+        if (scores) route<L, V, double><<<blocks, 256, lds, st>>>(b);
+        else route<L, V, float><<<blocks, 256, lds, st>>>(b);
+    }
+}
+
+// --- order --------------------------------------------------------------------------------------------------------
+
+struct PlanArgs {
+    const int32_t *ids;
+    int32_t *offsets, *slot_tokens, *slots;
+    uint32_t pairs, part;      // choices in all, and of a workgroup
+    int top_k, experts, bits;  // bits: of an expert's number
+};
+
+constexpr int PLAN_WAVES = 16;
+
+// A stable counting sort in one launch: every workgroup counts all choices, those before its own part apart, adds the counts up to where
+// each expert begins, and places its part: wavefront by wavefront in order, inside a wavefront by the lanes with the same expert before it.
+// LDS: counts of all choices [experts], where the next choice goes [wave][experts].
+__global__ __launch_bounds__(64 * PLAN_WAVES) void plan(PlanArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int E = a.experts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int32_t *all = (int32_t *)smem, *next = all + E;
+    __shared__ int32_t sums[PLAN_WAVES];
+    for (int i = threadIdx.x; i < E * (PLAN_WAVES + 1); i += 64 * PLAN_WAVES) all[i] = 0;
+    __syncthreads();
+    const uint32_t begin = blockIdx.x * a.part, end = min(a.pairs, begin + a.part);
+    const uint32_t per_wave = (a.part / PLAN_WAVES), w0 = min(end, begin + wave * per_wave), w1 = min(end, w0 + per_wave);
+    // choices before the part count into the first wavefront's places, as do those of wavefronts before another's into its own
+    for (uint32_t i = threadIdx.x; i < a.pairs; i += 64 * PLAN_WAVES) {
+        const uint32_t e = (uint32_t)a.ids[i];
+        if (e < (uint32_t)E) {
+            atomicAdd(&all[e], 1);
+            if (i < begin) atomicAdd(&next[e], 1);
+        }
+    }
+    for (uint32_t i = w0 + lane; i < w1; i += 64) {
+        const uint32_t e = (uint32_t)a.ids[i];
+        if (e < (uint32_t)E && wave + 1 < PLAN_WAVES) atomicAdd(&next[(wave + 1) * E + e], 1);
+    }
+    __syncthreads();
+    // where experts begin: sums over 64 x PLAN_WAVES >= QG_MAX_EXPERTS lanes
+    const int e = threadIdx.x;
+    const int count = e < E ? all[e] : 0;
+    int upto = count;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+        const int o = __shfl_up(upto, off);
+        if (lane >= off) upto += o;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int total = 0;
+    for (int w = 0; w < PLAN_WAVES; ++w) {
+        if (w < wave) upto += sums[w];
+        total += sums[w];
+    }
+    if (e < E) {
+        int at = upto - count;
+        if (blockIdx.x == 0) a.offsets[e] = at;
+        for (int w = 0; w < PLAN_WAVES; ++w) {
+            at += next[w * E + e];
+            next[w * E + e] = at;
+        }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.offsets[E] = total;
+    for (uint32_t i = total + blockIdx.x * 64 * PLAN_WAVES + threadIdx.x; i < a.pairs; i += gridDim.x * 64 * PLAN_WAVES) a.slot_tokens[i] = -1;
+    __syncthreads();
+    int32_t *places = next + wave * E;
+    for (uint32_t i0 = w0; i0 < w1; i0 += 64) {
+        const uint32_t i = i0 + lane;
+        const uint32_t id = i < w1 ? (uint32_t)a.ids[i] : 0xffffffffu;
+        const bool real = id < (uint32_t)E;
+        uint64_t same = __ballot(real);
+        for (int b = 0; b < a.bits; ++b) {
+            const bool bit = (id >> b) & 1;
+            const uint64_t set = __ballot(bit);
+            same &= bit ? set : ~set;
+        }
+        const int before = __popcll(same & ((1ull << lane) - 1));
+        int slot = -1;
+        if (real) slot = places[id] + before;
+        __builtin_amdgcn_wave_barrier();
+        if (real && before == 0) places[id] += __popcll(same);
+        __builtin_amdgcn_wave_barrier();
+        if (i < w1) a.slots[i] = slot;
+        if (real) a.slot_tokens[slot] = (int32_t)(i / (uint32_t)a.top_k);
+    }
+}
+
+// --- sum ----------------------------------------------------------------------------------------------------------
+
+struct CombineArgs {
+    const void *y;
+    const int32_t *slots;
+    const float *weights;
+    const void *residual;
+    void *out;
+    int64_t y_rows, tokens, N, residual_stride;
+    int top_k;
+    uint32_t chunks;           // workgroups of a token
+};
+
+// A lane takes VEC neighbouring columns of a token.
+template <int TYPE, int OUT, int VEC>
+__global__ __launch_bounds__(256) void combine(CombineArgs a)
+{
+    const uint32_t token = blockIdx.x / a.chunks;
+    const int64_t n = ((int64_t)(blockIdx.x - token * a.chunks) * 256 + threadIdx.x) * VEC;
+    if (n >= a.N) return;
+    float sum[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) sum[v] = 0.0f;
+    if (a.residual) {
+        const int64_t at = (int64_t)token * a.residual_stride + n;
+        if constexpr (VEC == 8) load_eight<OUT>(a.residual, at, sum);
+        else sum[0] = load_as_float<OUT>(a.residual, at);
+    }
+    for (int j = 0; j < a.top_k; ++j) {
+        const int64_t pair = (int64_t)token * a.top_k + j;
+        const int32_t slot = a.slots[pair];
+        const float w = a.weights[pair];
+        if (slot < 0 || slot >= a.y_rows) continue;
+        float v[VEC];
+        if constexpr (VEC == 8) load_eight<TYPE>(a.y, slot * a.N + n, v);
+        else v[0] = load_as_float<TYPE>(a.y, slot * a.N + n);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum[i] = __builtin_fmaf(w, v[i], sum[i]);
+    }
+    if constexpr (VEC == 8) store_eight<OUT>(a.out, (int64_t)token * a.N + n, sum);
+    else store_float<OUT>(a.out, (int64_t)token * a.N + n, sum[0]);
+}
+
+template <int TYPE, int OUT>
+void combine_launch(const CombineArgs &a, bool eights, hipStream_t st)
+{
+    CombineArgs b = a;
+    const int64_t per = 256 * (eights ? 8 : 1);
+    b.chunks = (uint32_t)((a.N + per - 1) / per);
+    const int64_t turn = QG_MOST_GROUPS / b.chunks > 0 ? QG_MOST_GROUPS / b.chunks : 1;
+    for (int64_t done = 0; done < a.tokens; done += turn) {
+        b.tokens = a.tokens - done < turn ? a.tokens - done : turn;
+        b.slots = a.slots + done * a.top_k;
+        b.weights = a.weights + done * a.top_k;
+        if (a.residual) b.residual = (const char *)a.residual + done * a.residual_stride * qg_type_bytes(OUT);
+        b.out = (char *)a.out + done * a.N * qg_type_bytes(OUT);
+        const unsigned blocks = (unsigned)(b.tokens * b.chunks);
+        if (eights) combine<TYPE, OUT, 8><<<blocks, 256, 0, st>>>(b);
+        else combine<TYPE, OUT, 1><<<blocks, 256, 0, st>>>(b);
+    }
+}
+
+template <int TYPE>
+void combine_typed(const CombineArgs &a, int out, bool eights, hipStream_t st)
+{
+    if (out == QG_F32) combine_launch<TYPE, QG_F32>(a, eights, st);
+    else if (out == QG_BF16) combine_launch<TYPE, QG_BF16>(a, eights, st);
+    else combine_launch<TYPE, QG_F16>(a, eights, st);
+}
+
+}  // namespace
+
+extern "C" int qg_route(const qg_route_desc *d, void *stream)
+{
+    if (!d) return QG_ERR_NULL;
+    if (!qg_float_type(d->type) || (d->score != QG_SOFTMAX && d->score != QG_SIGMOID)) return QG_ERR_UNSUPPORTED;
+    if (d->experts > QG_MAX_EXPERTS || d->top_k > QG_MAX_CHOICES || (d->group_best != 1 && d->group_best != 2)) return QG_ERR_UNSUPPORTED;
+    if (d->tokens < 0 || d->experts <= 0 || d->top_k <= 0 || d->groups <= 0 || d->experts % d->groups || d->top_groups <= 0 || d->top_groups > d->groups) return QG_ERR_SHAPE;
+    if (d->top_k > d->experts / d->groups * d->top_groups || d->tokens > 0x7fffffff / d->top_k) return QG_ERR_SHAPE;
+    if (d->tokens > 1 && d->logits_stride < d->experts) return QG_ERR_SHAPE;
+    if (d->tokens == 0) return QG_OK;
+    if (!d->logits || !d->ids || !d->weights) return QG_ERR_NULL;
+    if (!qg_aligned_to(d->logits, qg_type_bytes(d->type)) || !qg_aligned_to(d->bias, 4) || !qg_aligned_to(d->ids, 4) || !qg_aligned_to(d->weights, 4)) return QG_ERR_ALIGN;
+    const uint32_t size = (uint32_t)(d->experts / d->groups);
+    const RouteArgs a = {d->logits, d->bias, d->ids, d->weights, d->tokens, d->logits_stride, d->type, d->experts, d->top_k, d->score == QG_SIGMOID,
+                         d->groups, d->top_groups, d->group_best == 2, d->renormalise != 0, size > 1 ? (uint32_t)(((uint64_t)1 << 32) / size + 1) : 0, d->scale};
+    const bool scores = d->bias || (d->top_groups < d->groups && d->group_best == 2);
+    const hipStream_t st = (hipStream_t)stream;
+    const int E = d->experts, k = d->top_k;
+    // as few lanes a token as eight experts a lane allow, and one a choice at least
+    if (E <= 64 && k <= 16) route_launch<16, 4>(a, scores, st);
+    else if (E <= 128 && k <= 16) route_launch<16, 8>(a, scores, st);
+    else if (E <= 256 && k <= 32) route_launch<32, 8>(a, scores, st);
+    else if (E <= 512) route_launch<64, 8>(a, scores, st);
+    else route_launch<64, 16>(a, scores, st);
+    return qg_launch_status();
+}
+
+extern "C" int qg_expert_plan(const int32_t *ids, int64_t tokens, int top_k, int experts, int32_t *offsets, int32_t *slot_tokens, int32_t *slots, void *stream)
+{
+    if (experts > QG_MAX_EXPERTS) return QG_ERR_UNSUPPORTED;
+    if (tokens < 0 || top_k <= 0 || experts <= 0 || tokens > 0x3fffffff / top_k) return QG_ERR_SHAPE;
+    if (!offsets || (tokens && (!ids || !slot_tokens || !slots))) return QG_ERR_NULL;
+    if (!qg_aligned_to(ids, 4) || !qg_aligned_to(offsets, 4) || !qg_aligned_to(slot_tokens, 4) || !qg_aligned_to(slots, 4)) return QG_ERR_ALIGN;
+    PlanArgs a = {ids, offsets, slot_tokens, slots, (uint32_t)(tokens * top_k), 64 * PLAN_WAVES, top_k, experts, 0};
+    while (a.bits < 10 && (experts - 1) >> a.bits) ++a.bits;
+    // parts of 2048 choices, of more where that would take more workgroups than compute units
+    const uint32_t blocks = (uint32_t)qg_compute_units();
+    a.part = 2048;
+    while ((uint64_t)a.part * blocks < a.pairs) a.part *= 2;
+    const unsigned grid = a.pairs ? (a.pairs + a.part - 1) / a.part : 1;
+    const size_t lds = (size_t)experts * (PLAN_WAVES + 1) * 4;
+    if (lds > 65536 && hipFuncSetAttribute((const void *)plan, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
+        (void)hipGetLastError();
+        return QG_ERR_DEVICE;
+    }
+    plan<<<grid, 64 * PLAN_WAVES, lds, (hipStream_t)stream>>>(a);
+    return qg_launch_status();
+}
+
+extern "C" int qg_experts_combine(const qg_combine_desc *d, void *stream)
+{
+    if (!d) return QG_ERR_NULL;
+    if (!qg_float_type(d->type) || !qg_float_type(d->out_type)) return QG_ERR_UNSUPPORTED;
+    if (d->top_k > QG_MAX_CHOICES) return QG_ERR_UNSUPPORTED;
+    if (d->tokens < 0 || d->N <= 0 || d->N > (int64_t)1 << 24 || d->top_k <= 0 || d->y_rows < 0 || d->y_rows > 0x7fffffff || d->tokens > 0x7fffffff / d->top_k) return QG_ERR_SHAPE;
+    if (d->residual && d->tokens > 1 && d->residual_stride < d->N) return QG_ERR_SHAPE;
+    if (d->tokens == 0) return QG_OK;
+    if ((!d->y && d->y_rows) || !d->slots || !d->weights || !d->out) return QG_ERR_NULL;
+    const int in = qg_type_bytes(d->type), out = qg_type_bytes(d->out_type);
+    if (!qg_aligned_to(d->y, in) || !qg_aligned_to(d->residual, out) || !qg_aligned_to(d->out, out) || !qg_aligned_to(d->slots, 4) || !qg_aligned_to(d->weights, 4))
+        return QG_ERR_ALIGN;
+    const CombineArgs a = {d->y, d->slots, d->weights, d->residual, d->out, d->y_rows, d->tokens, d->N, d->residual_stride, d->top_k, 0};
+    const bool eights = d->N % 8 == 0 && qg_aligned16(d->y) && qg_aligned16(d->out) && (!d->residual || (qg_aligned16(d->residual) && d->residual_stride % 8 == 0));
+    const hipStream_t st = (hipStream_t)stream;
+    if (d->type == QG_F32) combine_typed<QG_F32>(a, d->out_type, eights, st);
+    else if (d->type == QG_BF16) combine_typed<QG_BF16>(a, d->out_type, eights, st);
+    else combine_typed<QG_F16>(a, d->out_type, eights, st);
+    return qg_launch_status();
+}
