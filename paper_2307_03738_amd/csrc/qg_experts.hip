@@ -1,5 +1,5 @@
 // qg_experts_product: y[p] = What_e x[rows[p]] for the slots p of each expert e.
-#include "qg_experts.h"
+#include "qg_experts_few.h"
 
 namespace {
 
@@ -100,6 +100,23 @@ __global__ __launch_bounds__(256) void experts_any(QgExpertsArgs a)
     }
 }
 
+void few_plan(const QgExpertsArgs &a, int bits, hipStream_t st)
+{
+    QgFewArgs f = {};
+    f.e = a;
+    f.tile_rows = a.x_type == QG_F32 ? FEW_ROWS / 2 : FEW_ROWS;
+    f.e.row_tiles = (int)qg_most_tiles(a.slots, a.experts, f.tile_rows);
+    const int64_t used = a.experts < a.slots ? a.experts : a.slots;
+    f.tiles = a.gated || used * ((a.columns + 127) / 128) >= 2 * qg_compute_units() ? 2 : 1;
+    const int width = a.gated || f.tiles == 1 ? 64 : 128;
+    f.g32 = a.group / 32;
+    f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);
+    const int quantum = bits == 2 ? 256 : 128;
+    f.quanta = (a.K + quantum - 1) / quantum;
+    f.blocks = (int)((int64_t)f.e.row_tiles * ((a.columns + width - 1) / width));
+    (bits == 4 ? qg_few_launch_b4 : bits == 3 ? qg_few_launch_b3 : qg_few_launch_b2)(f, st);
+}
+
 template <int BITS>
 int any_launch(const QgExpertsArgs &a, int64_t blocks, hipStream_t st)
 {
@@ -156,6 +173,10 @@ extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
     a.x_type = d->x_type;
     a.y_type = d->y_type;
     const hipStream_t st = (hipStream_t)stream;
+    if (d->group % 32 == 0) {
+        few_plan(a, d->bits, st);
+        return qg_launch_status();
+    }
     a.row_tiles = (int)qg_most_tiles(d->slots, d->experts, ANY_ROWS);
     const int64_t blocks = (int64_t)a.row_tiles * ((a.columns + 63) / 64);
     if (blocks > (int64_t)QG_MOST_GROUPS * 65535) return QG_ERR_SHAPE;
