@@ -1,5 +1,6 @@
 // qg_experts_product: y[p] = What_e x[rows[p]] for the slots p of each expert e.
 #include "qg_experts_few.h"
+#include "qg_experts_many.h"
 
 namespace {
 
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(256) void experts_any(QgExpertsArgs a)
     }
 }
 
-void few_plan(const QgExpertsArgs &a, int bits, hipStream_t st)
+int few_plan(const QgExpertsArgs &a, int bits, hipStream_t st)
 {
     QgFewArgs f = {};
     f.e = a;
@@ -113,8 +114,53 @@ void few_plan(const QgExpertsArgs &a, int bits, hipStream_t st)
     f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);
     const int quantum = bits == 2 ? 256 : 128;
     f.quanta = (a.K + quantum - 1) / quantum;
-    f.blocks = (int)((int64_t)f.e.row_tiles * ((a.columns + width - 1) / width));
+    const int64_t blocks = (int64_t)f.e.row_tiles * ((a.columns + width - 1) / width);
+    if (blocks > QG_MOST_GROUPS / 2) return QG_ERR_SHAPE;
+    f.blocks = (int)blocks;
     (bits == 4 ? qg_few_launch_b4 : bits == 3 ? qg_few_launch_b3 : qg_few_launch_b2)(f, st);
+    return QG_OK;
+}
+
+// Of the rows of X as f16, and their powers of two.
+struct RowsSpace {
+    int64_t padded, bytes, total;
+    int parts;
+};
+RowsSpace rows_space(int64_t x_rows, int64_t K, int x_type)
+{
+    RowsSpace s;
+    s.parts = x_type == QG_F32 ? 2 : 1;
+    s.padded = (K + 127) / 128 * 128;
+    s.bytes = (x_rows + 1) * s.parts * s.padded * 2;
+    s.total = s.bytes + (x_rows + 1) * 4;
+    return s;
+}
+
+// Whether an expert has rows enough, on average, for the kernel of many rows.
+bool many_of(int64_t slots, int experts)
+{
+    return slots >= (int64_t)24 * experts;
+}
+
+int many_plan(const QgExpertsArgs &a, int bits, void *workspace, hipStream_t st)
+{
+    const RowsSpace s = rows_space(a.x_rows, a.K, a.x_type);
+    QgManyArgs f = {};
+    f.e = a;
+    f.e.row_tiles = (int)qg_most_tiles(a.slots, a.experts, MANY_ROWS);
+    f.xh = (const char *)workspace;
+    f.up = (const int32_t *)((const char *)workspace + s.bytes);
+    f.padded = s.padded;
+    f.parts = s.parts;
+    f.g32 = a.group / 32;
+    f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);
+    const int width = a.gated ? 128 : 256;
+    f.column_blocks = (a.columns + width - 1) / width;
+    const int64_t blocks = (int64_t)f.e.row_tiles * f.column_blocks;
+    if (blocks > QG_MOST_GROUPS) return QG_ERR_SHAPE;
+    f.blocks = (int)blocks;
+    const QgPrepareArgs p = {a.x, (char *)workspace, (int32_t *)((char *)workspace + s.bytes), a.x_rows, a.x_stride, s.padded, a.K, a.x_type};
+    return (bits == 4 ? qg_many_launch_b4 : bits == 3 ? qg_many_launch_b3 : qg_many_launch_b2)(f, p, st);
 }
 
 template <int BITS>
@@ -132,7 +178,9 @@ int any_launch(const QgExpertsArgs &a, int64_t blocks, hipStream_t st)
 
 extern "C" size_t qg_experts_workspace_bytes(int64_t x_rows, int64_t slots, int64_t K, int experts, int x_type)
 {
-    return 0;
+    if (x_rows < 0 || x_rows > 0x7fffffff || slots < 0 || slots > 0x7fffffff || K <= 0 || K > (int64_t)1 << 24 || experts <= 0 || experts > QG_MAX_EXPERTS ||
+        !qg_float_type(x_type)) return 0;
+    return many_of(slots, experts) ? (size_t)rows_space(x_rows, K, x_type).total : 0;
 }
 
 extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
@@ -148,7 +196,8 @@ extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
     if (!d->packed || (!d->x && d->x_rows) || !d->offsets || !d->y) return QG_ERR_NULL;
     if (!qg_aligned16(d->packed) || d->expert_stride % 16 || !qg_aligned16(d->x) || (d->x_rows > 1 && d->x_stride % 8) || !qg_aligned_to(d->offsets, 4) ||
         !qg_aligned_to(d->rows, 4) || !qg_aligned_to(d->y, qg_type_bytes(d->y_type)) || !qg_aligned16(d->workspace)) return QG_ERR_ALIGN;
-    if (d->workspace_bytes < qg_experts_workspace_bytes(d->x_rows, d->slots, d->K, d->experts, d->x_type)) return QG_ERR_WORKSPACE;
+    const size_t space = qg_experts_workspace_bytes(d->x_rows, d->slots, d->K, d->experts, d->x_type);
+    if (space && (!d->workspace || d->workspace_bytes < space)) return QG_ERR_WORKSPACE;
     QgExpertsArgs a = {};
     a.packed = (const char *)d->packed;
     a.x = (const char *)d->x;
@@ -174,8 +223,8 @@ extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
     a.y_type = d->y_type;
     const hipStream_t st = (hipStream_t)stream;
     if (d->group % 32 == 0) {
-        few_plan(a, d->bits, st);
-        return qg_launch_status();
+        const int launched = many_of(d->slots, d->experts) ? many_plan(a, d->bits, d->workspace, st) : few_plan(a, d->bits, st);
+        return launched != QG_OK ? launched : qg_launch_status();
     }
     a.row_tiles = (int)qg_most_tiles(d->slots, d->experts, ANY_ROWS);
     const int64_t blocks = (int64_t)a.row_tiles * ((a.columns + 63) / 64);

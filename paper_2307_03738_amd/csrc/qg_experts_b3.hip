@@ -1,5 +1,9 @@
 // The experts' products on 3-bit codes.
+#include <atomic>
+
 #define QG_EXPERTS_KERNELS
 #include "qg_experts_few.h"
+#include "qg_experts_many.h"
 
 void qg_few_launch_b3(const QgFewArgs &f, hipStream_t st) { few_launch<3>(f, st); }
+int qg_many_launch_b3(const QgManyArgs &f, const QgPrepareArgs &p, hipStream_t st) { return many_launch<3>(f, p, st); }

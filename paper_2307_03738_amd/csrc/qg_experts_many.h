@@ -1,0 +1,320 @@
+// The experts' products where an expert has many rows: bound by the matrix cores and by what turns codes into operands.
+//
+// prepare_rows converts each row of X once: f16 in the order in which codes come out of their words, one part or, fp32, two, and the
+// row's power of two.  experts_many: a workgroup of four wavefronts takes up to 128 slots of an expert and 256 outputs, a wavefront all of the
+// slots and 64 outputs of its own (gated: gate and up of 32 columns), so that every weight is unpacked once per workgroup.  X's rows, gathered
+// by slot, go from memory to LDS without passing through registers, 128 k ahead, codes to registers; a wavefront reads each operand
+// of X for two 32 x 32 x 16 matrix instructions (half of LDS's rate at full speed of the matrix cores).
+#pragma once
+
+#include "qg_experts_codes.h"
+
+constexpr int MANY_ROWS = 128;
+
+struct QgManyArgs {
+    QgExpertsArgs e;
+    const char *xh;            // rows of f16, [x_rows + 1][parts][padded]: the last one zeros
+    const int32_t *up;         // [x_rows + 1]: their powers of two
+    int64_t padded;            // k a row is filled up to: a multiple of 128
+    int parts;
+    int g32, gshift;
+    int column_blocks;         // of 256 outputs
+    int blocks;
+};
+
+struct QgPrepareArgs {
+    const char *x;
+    char *xh;
+    int32_t *up;
+    int64_t x_rows, x_stride, padded;
+    int K, type;
+};
+
+#ifdef QG_EXPERTS_KERNELS
+namespace {
+
+// Position of k (0 ... 31) in two operands of 16 k: operand position / 16, lanes of half position / 8 % 2, element position % 8.
+template <int BITS>
+__device__ inline int k_position_32(int k)
+{
+    if constexpr (BITS == 2) {
+        const int w = k >> 4, r = k & 15;
+        return ((r & 7) >> 2) * 16 + w * 8 + 2 * (r & 3) + (r >> 3);
+    } else {
+        return k_position<BITS>(k);
+    }
+}
+
+// A wavefront a row; a lane takes 32 k at a time, whose order is all in its registers then.
+template <int BITS>
+__global__ __launch_bounds__(256) void prepare_rows(const QgPrepareArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row > a.x_rows) return;
+    const int parts = a.type == QG_F32 ? 2 : 1;
+    char *to = a.xh + row * parts * a.padded * 2;
+    if (row == a.x_rows) {
+        for (int64_t k = lane * 8; k < parts * a.padded; k += 512) *(uint4 *)(to + k * 2) = make_uint4(0, 0, 0, 0);
+        if (lane == 0) a.up[row] = 0;
+        return;
+    }
+    const int64_t from = row * a.x_stride;
+    auto eight = [&](int64_t k, float *v) {
+        if (k < a.K) {
+            if (a.type == QG_F32) load_eight<QG_F32>(a.x, from + k, v);
+            else if (a.type == QG_BF16) load_eight<QG_BF16>(a.x, from + k, v);
+            else load_eight<QG_F16>(a.x, from + k, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+        }
+    };
+    int up = 0;
+    if (a.type != QG_F16) {
+        uint32_t most = 0;
+        for (int64_t k = lane * 8; k < a.K; k += 512) {
+            float v[8];
+            eight(k, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, magnitude_bits(v[e]));
+        }
+        up = row_exponent(most_of(most, 64));
+    }
+    if (lane == 0) a.up[row] = up;
+    constexpr int OCT = BITS == 2 ? 32 : 8;
+    for (int64_t k = lane * OCT; k < a.padded; k += 64 * OCT) {
+        float v[OCT], p[OCT];
+#pragma unroll
+        for (int o = 0; o < OCT; o += 8) eight(k + o, v + o);
+#pragma unroll
+        for (int e = 0; e < OCT; ++e) p[k_position_32<BITS>(e)] = a.type == QG_F16 ? v[e] : __builtin_amdgcn_ldexpf(v[e], up);
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            if (part < parts) {
+#pragma unroll
+                for (int o = 0; o < OCT; o += 8)
+                    *(uint4 *)(to + (part * a.padded + k + o) * 2) =
+                        make_uint4(two_halves(p[o], p[o + 1]), two_halves(p[o + 2], p[o + 3]), two_halves(p[o + 4], p[o + 5]), two_halves(p[o + 6], p[o + 7]));
+#pragma unroll
+                for (int e = 0; e < OCT; ++e) p[e] = left_over(p[e]);
+            }
+        }
+    }
+}
+
+// MB: blocks of 32 slots.
+template <int BITS, int GP, int PARTS, int MB>
+__device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64_t column0, char *smem, int32_t *ups)
+{
+    using F = Fmt<BITS>;
+    constexpr int LOADS = BITS, FOLDS = 4 / GP, ZPER = 32 / F::ZBITS;      // of 128 k
+    constexpr int ROWS = 32 * MB, STAGE = ROWS * 256 * PARTS;
+    constexpr int COPIES = ROWS * PARTS / 16;                              // of 4 rows, a wavefront's
+    const QgExpertsArgs &a = f.e;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int half = lane >> 5;
+
+    // this lane's output
+    const int64_t wave_column = column0 + wave * (a.gated ? 32 : 64);
+    const int64_t column = wave_column + (a.gated ? lane & 31 : lane);
+    const int64_t n = (column < a.columns ? column : a.columns - 1) + (a.gated && half ? (int64_t)a.columns : 0);
+    const char *blob = a.packed + t.expert * a.expert_stride;
+    const char *codes = blob + (n >> 6) * a.tile_codes + (n & 63) * 16;
+    const char *scales = blob + a.scales_off + (n >> 6) * a.tile_scales + (n & 63) * 4;
+    const char *zeros = blob + a.zeros_off + (n >> 6) * a.tile_zeros + (n & 63) * 4;
+    const int last_group = a.K / a.group - 1;
+    const int steps = (a.K + 127) / 128;
+
+    // the rows it copies: 16 bytes of row 4 j + lane / 16 each, octet (lane % 16) ^ (row % 16) of the 128 k, so that 16 rows' octets of the same k
+    // lie on distinct banks
+    uint64_t from[COPIES];
+#pragma unroll
+    for (int j = 0; j < COPIES; ++j) {
+        const int at = (wave * COPIES + j) * 4 + (lane >> 4), part = at / ROWS, r = at % ROWS;
+        int64_t row = a.x_rows;
+        if (r < t.rows) {
+            row = a.rows ? a.rows[t.begin + r] : t.begin + r;
+            row = row >= 0 && row < a.x_rows ? row : a.x_rows;
+        }
+        if (part == 0 && (lane & 15) == 0) ups[r] = f.up[row];
+        from[j] = (uint64_t)(uintptr_t)(f.xh + ((row * PARTS + part) * f.padded) * 2 + (((lane & 15) ^ (r & 15)) * 16));
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    auto copy = [&](int step, int stage) {
+#pragma unroll
+        for (int j = 0; j < COPIES; ++j) {
+            const uint64_t src = from[j] + (uint64_t)step * 256;
+            const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + stage * STAGE + (wave * COPIES + j) * 1024);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
+        }
+    };
+    struct Weights {
+        uint4 v[LOADS];
+        uint32_t s[FOLDS], z[FOLDS];
+    };
+    auto load = [&](int step, Weights &w) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) w.v[i] = *(const uint4 *)(codes + ((int64_t)step * LOADS + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < FOLDS; ++i) {
+            const int k32 = step * 4 + i * GP;
+            int g = f.gshift >= 0 ? k32 >> f.gshift : k32 / f.g32;
+            g = g < last_group ? g : last_group;
+            w.s[i] = *(const uint32_t *)(scales + (int64_t)g * 256);
+            w.z[i] = *(const uint32_t *)(zeros + (int64_t)(g / ZPER) * 256) >> (g % ZPER * F::ZBITS);
+        }
+    };
+
+    float16v y[MB][2];
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) y[m][b] = 0.0f;
+    const HalfConst hc = half_constants<BITS>();
+    const int r0 = lane & 31;
+
+    Weights next;
+    copy(0, 0);
+    load(0, next);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    for (int step = 0; step < steps; ++step) {
+        const Weights w = next;
+        const char *x = smem + (step & 1) * STAGE;
+        if (step + 1 < steps) {
+            copy(step + 1, (step + 1) & 1);
+            load(step + 1, next);
+        }
+#pragma unroll
+        for (int i = 0; i < FOLDS; ++i) {
+            const auto s = __builtin_amdgcn_permlane32_swap(w.s[i], w.s[i], false, false);
+            const uint32_t z = w.z[i] & ((1u << F::ZBITS) - 1);
+            const auto zz = __builtin_amdgcn_permlane32_swap(z, z, false, false);
+            uint32_t zc[2][4];
+            zero_operands<BITS>(zz[0], zc[0]);
+            zero_operands<BITS>(zz[1], zc[1]);
+            HalfOperand o[2][2 * GP];
+#pragma unroll
+            for (int g = 0; g < GP; ++g) {
+                uint32_t words[4];
+                words_of<BITS>(w.v, i * GP + g, words);
+                if constexpr (BITS == 2) {
+                    const auto p = __builtin_amdgcn_permlane32_swap(words[0], words[1], false, false);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        unpack_halves<BITS>(p[b], hc, zc[b], o[b][2 * g]);
+                        unpack_halves<BITS>(p[b] >> 8, hc, zc[b], o[b][2 * g + 1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const auto p = __builtin_amdgcn_permlane32_swap(words[2 * h], words[2 * h + 1], false, false);
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) unpack_halves<BITS>(p[b], hc, zc[b], o[b][2 * g + h]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < MB; ++m) {
+                float16v sum[2];
+                sum[0] = 0.0f;
+                sum[1] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 2 * GP; ++k)
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) {
+                        const int octet = (i * GP * 2 + k) * 2 + half;
+                        HalfOperand xo;
+                        xo.q = *(const uint4 *)(x + (part * ROWS + m * 32 + r0) * 256 + ((octet ^ (r0 & 15)) * 16));
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) sum[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xo.v, o[b][k].v, sum[b], 0, 0, 0);
+                    }
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[m][b][e] = __builtin_fmaf(__uint_as_float(s[b]), sum[b][e], y[m][b][e]);
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+    }
+
+    const int64_t c = wave_column + r0;
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int r = 32 * m + 8 * (e / 4) + 4 * half + e % 4;
+            const int down = -ups[r];
+            if (r >= t.rows) continue;
+            const float v0 = __builtin_amdgcn_ldexpf(y[m][0][e], down), v1 = __builtin_amdgcn_ldexpf(y[m][1][e], down);
+            const int64_t at = (t.begin + r) * a.columns + c;
+            if (a.gated) {
+                if (c < a.columns) store_typed(a.y_type, a.y, at, silu(v0) * v1);
+            } else {
+                if (c < a.columns) store_typed(a.y_type, a.y, at, v0);
+                if (c + 32 < a.columns) store_typed(a.y_type, a.y, at + 32, v1);
+            }
+        }
+}
+
+template <int BITS, int GP, int PARTS>
+__global__ __launch_bounds__(256, 1) void experts_many(const QgManyArgs f)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ int32_t ups[MANY_ROWS];
+    // A die's workgroups (i % 8) take neighbouring pieces, eight blocks of columns by as many tiles of slots: they share X's rows and weights in its L2.
+    int block = blockIdx.x;
+    {
+        const int die = block & 7, each = f.blocks >> 3, more = f.blocks & 7;
+        block = die * each + (die < more ? die : more) + (block >> 3);
+    }
+    const int band = block / (8 * f.e.row_tiles), across = min(8, f.column_blocks - 8 * band);
+    const int rest = block - band * 8 * f.e.row_tiles;
+    const ExpertTile t = expert_tile(f.e, rest / across, MANY_ROWS);
+    if (t.rows == 0) return;
+    const int expert = __builtin_amdgcn_readfirstlane(t.expert), rows = __builtin_amdgcn_readfirstlane(t.rows);
+    const ExpertTile u = {expert, rows, (int64_t)__builtin_amdgcn_readfirstlane((int)t.begin)};
+    const int64_t column0 = (int64_t)(8 * band + rest % across) * (f.e.gated ? 128 : 256);
+    if (rows <= 32) many_rows<BITS, GP, PARTS, 1>(f, u, column0, smem, ups);
+    else if (rows <= 64) many_rows<BITS, GP, PARTS, 2>(f, u, column0, smem, ups);
+    else many_rows<BITS, GP, PARTS, 4>(f, u, column0, smem, ups);
+}
+
+template <int BITS, int GP, int PARTS>
+int many_typed(const QgManyArgs &f, hipStream_t st)
+{
+    constexpr size_t lds = (size_t)2 * MANY_ROWS * 256 * PARTS;
+    if (lds > 63 << 10) {
+        static std::atomic<bool> prepared[64];      // once per device (devices past the table: every time)
+        int dev = -1;
+        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = -1;
+        if (dev < 0 || !prepared[dev].load(std::memory_order_acquire)) {
+            if (hipFuncSetAttribute((const void *)experts_many<BITS, GP, PARTS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
+                (void)hipGetLastError();
+                return QG_ERR_DEVICE;
+            }
+            if (dev >= 0) prepared[dev].store(true, std::memory_order_release);
+        }
+    }
+    experts_many<BITS, GP, PARTS><<<f.blocks, 256, lds, st>>>(f);
+    return QG_OK;
+}
+
+template <int BITS>
+int many_launch(const QgManyArgs &f, const QgPrepareArgs &p, hipStream_t st)
+{
+    const int64_t blocks = (p.x_rows + 4) / 4;
+    const unsigned across = (unsigned)(blocks < QG_MOST_GROUPS ? blocks : QG_MOST_GROUPS);
+    prepare_rows<BITS><<<dim3(across, (unsigned)((blocks + across - 1) / across)), 256, 0, st>>>(p);
+    if (f.parts == 2) return f.g32 % 4 == 0 ? many_typed<BITS, 4, 2>(f, st) : f.g32 % 2 == 0 ? many_typed<BITS, 2, 2>(f, st) : many_typed<BITS, 1, 2>(f, st);
+    return f.g32 % 4 == 0 ? many_typed<BITS, 4, 1>(f, st) : f.g32 % 2 == 0 ? many_typed<BITS, 2, 1>(f, st) : many_typed<BITS, 1, 1>(f, st);
+}
+
+}  // namespace
+#endif
+
+int qg_many_launch_b2(const QgManyArgs &f, const QgPrepareArgs &p, hipStream_t st);
+int qg_many_launch_b3(const QgManyArgs &f, const QgPrepareArgs &p, hipStream_t st);
+int qg_many_launch_b4(const QgManyArgs &f, const QgPrepareArgs &p, hipStream_t st);
