@@ -1,15 +1,16 @@
 // The experts' products where an expert has many rows: bound by the matrix cores and by what turns codes into operands.
 //
 // prepare_rows converts each row of X once: f16 in the order in which codes come out of their words, one part or, fp32, two, and the
-// row's power of two.  experts_many: a workgroup of four wavefronts takes up to 128 slots of an expert and 256 outputs, a wavefront all of the
+// row's power of two.  experts_many: a workgroup of four wavefronts takes up to 64 slots of an expert and 256 outputs, a wavefront all of the
 // slots and 64 outputs of its own (gated: gate and up of 32 columns), so that every weight is unpacked once per workgroup.  X's rows, gathered
 // by slot, go from memory to LDS without passing through registers, 128 k ahead, codes to registers; a wavefront reads each operand
-// of X for two 32 x 32 x 16 matrix instructions (half of LDS's rate at full speed of the matrix cores).
+// of X for two 32 x 32 x 16 matrix instructions (half of LDS's rate at full speed of the matrix cores).  Two workgroups share a compute unit: with 128
+// slots and one wavefront a SIMD nothing covers what a wavefront waits for (a prompt of 4096 tokens, 22016 x 4096 4-bit, two of eight: 2.55 ms against 1.71).
 #pragma once
 
 #include "qg_experts_codes.h"
 
-constexpr int MANY_ROWS = 128;
+constexpr int MANY_ROWS = 64;
 
 struct QgManyArgs {
     QgExpertsArgs e;
@@ -260,7 +261,7 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
 }
 
 template <int BITS, int GP, int PARTS>
-__global__ __launch_bounds__(256, 1) void experts_many(const QgManyArgs f)
+__global__ __launch_bounds__(256, 2) void experts_many(const QgManyArgs f)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ int32_t ups[MANY_ROWS];
@@ -278,8 +279,8 @@ __global__ __launch_bounds__(256, 1) void experts_many(const QgManyArgs f)
     const ExpertTile u = {expert, rows, (int64_t)__builtin_amdgcn_readfirstlane((int)t.begin)};
     const int64_t column0 = (int64_t)(8 * band + rest % across) * (f.e.gated ? 128 : 256);
     if (rows <= 32) many_rows<BITS, GP, PARTS, 1>(f, u, column0, smem, ups);
-    else if (rows <= 64) many_rows<BITS, GP, PARTS, 2>(f, u, column0, smem, ups);
-    else many_rows<BITS, GP, PARTS, 4>(f, u, column0, smem, ups);
+    else many_rows<BITS, GP, PARTS, 2>(f, u, column0, smem, ups);
+
 }
 
 template <int BITS, int GP, int PARTS>
