@@ -31,7 +31,8 @@ template <int BITS> constexpr int few_loads() { return BITS == 3 ? 3 : 4; }
 template <int BITS, int FOLDS>
 struct FewWeights {
     uint4 v[few_loads<BITS>()];
-    uint32_t s[FOLDS], z[FOLDS];               // scale, and the word with the zero-point
+    uint32_t s[FOLDS], z[FOLDS];               // scale, and the word with the zero-point (shifted where it is used: a shift here would wait)
+    int shift[FOLDS];
 };
 
 template <int BITS, int GP, int MB>
@@ -73,7 +74,8 @@ __device__ inline void few_rows(const QgFewArgs &f, const ExpertTile &t, int64_t
             int g = f.gshift >= 0 ? k32 >> f.gshift : k32 / f.g32;
             g = g < last_group ? g : last_group;
             w.s[i] = *(const uint32_t *)(scales + (int64_t)g * 256);
-            w.z[i] = *(const uint32_t *)(zeros + (int64_t)(g / ZPER) * 256) >> (g % ZPER * F::ZBITS);
+            w.z[i] = *(const uint32_t *)(zeros + (int64_t)(g / ZPER) * 256);
+            w.shift[i] = g % ZPER * F::ZBITS;
         }
     };
 
@@ -184,7 +186,7 @@ __device__ inline void few_rows(const QgFewArgs &f, const ExpertTile &t, int64_t
             for (int i = 0; i < FOLDS; ++i) {
                 uint32_t s[4], zw[4];
                 spread_16(w.s[i], s);
-                spread_16(w.z[i] & ((1u << F::ZBITS) - 1), zw);
+                spread_16((w.z[i] >> w.shift[i]) & ((1u << F::ZBITS) - 1), zw);
                 uint32_t ops[GP][4];
                 HalfOperand x[GP][MB];
 #pragma unroll

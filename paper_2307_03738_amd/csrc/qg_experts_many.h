@@ -152,7 +152,8 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
     };
     struct Weights {
         uint4 v[LOADS];
-        uint32_t s[FOLDS], z[FOLDS];
+        uint32_t s[FOLDS], z[FOLDS];           // scale, and the word with the zero-point (shifted where it is used: a shift here would wait)
+        int shift[FOLDS];
     };
     auto load = [&](int step, Weights &w) {
 #pragma unroll
@@ -163,7 +164,8 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
             int g = f.gshift >= 0 ? k32 >> f.gshift : k32 / f.g32;
             g = g < last_group ? g : last_group;
             w.s[i] = *(const uint32_t *)(scales + (int64_t)g * 256);
-            w.z[i] = *(const uint32_t *)(zeros + (int64_t)(g / ZPER) * 256) >> (g % ZPER * F::ZBITS);
+            w.z[i] = *(const uint32_t *)(zeros + (int64_t)(g / ZPER) * 256);
+            w.shift[i] = g % ZPER * F::ZBITS;
         }
     };
 
@@ -190,7 +192,7 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
 #pragma unroll
         for (int i = 0; i < FOLDS; ++i) {
             const auto s = __builtin_amdgcn_permlane32_swap(w.s[i], w.s[i], false, false);
-            const uint32_t z = w.z[i] & ((1u << F::ZBITS) - 1);
+            const uint32_t z = (w.z[i] >> w.shift[i]) & ((1u << F::ZBITS) - 1);
             const auto zz = __builtin_amdgcn_permlane32_swap(z, z, false, false);
             uint32_t zc[2][4];
             zero_operands<BITS>(zz[0], zc[0]);
