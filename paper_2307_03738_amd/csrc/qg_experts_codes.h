@@ -64,10 +64,11 @@ __device__ inline HalfConst half_constants()
 template <int BITS>
 __device__ inline void zero_operands(uint32_t z, uint32_t *c)
 {
+    const uint32_t two = z << 16 | z;
 #pragma unroll
     for (int i = 0; i < zero_constants<BITS>(); ++i) {
         const uint32_t f = BITS * i;
-        c[i] = z * (0x00010001u << f) + (0xe400e400u - (f << 10) * 0x00010001u);
+        c[i] = (two << f) + (0xe400e400u - (f << 10) * 0x00010001u);
     }
 }
 

@@ -189,6 +189,18 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
             copy(step + 1, (step + 1) & 1);
             load(step + 1, next);
         }
+        // sixteens of k: operands of X are read AHEAD sixteens before they are multiplied, codes unpacked right before
+        constexpr int KS = 2 * GP, AHEAD = 2;
+        HalfOperand xo[8][MB * PARTS];
+        auto read = [&](int k) {
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part)
+                    xo[k][m * PARTS + part].q = *(const uint4 *)(x + (part * ROWS + m * 32 + r0) * 256 + (((2 * k + half) ^ (r0 & 15)) * 16));
+        };
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) read(k);
 #pragma unroll
         for (int i = 0; i < FOLDS; ++i) {
             const auto s = __builtin_amdgcn_permlane32_swap(w.s[i], w.s[i], false, false);
@@ -197,47 +209,43 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
             uint32_t zc[2][4];
             zero_operands<BITS>(zz[0], zc[0]);
             zero_operands<BITS>(zz[1], zc[1]);
-            HalfOperand o[2][2 * GP];
+            float16v sum[MB][2];
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) sum[m][b] = 0.0f;
 #pragma unroll
             for (int g = 0; g < GP; ++g) {
                 uint32_t words[4];
                 words_of<BITS>(w.v, i * GP + g, words);
-                if constexpr (BITS == 2) {
-                    const auto p = __builtin_amdgcn_permlane32_swap(words[0], words[1], false, false);
+                const auto p2 = __builtin_amdgcn_permlane32_swap(words[0], words[1], false, false);
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        unpack_halves<BITS>(p[b], hc, zc[b], o[b][2 * g]);
-                        unpack_halves<BITS>(p[b] >> 8, hc, zc[b], o[b][2 * g + 1]);
+                for (int h = 0; h < 2; ++h) {
+                    const int k = i * KS + 2 * g + h;
+                    if (k + AHEAD < 8) read(k + AHEAD);
+                    HalfOperand o[2];
+                    if constexpr (BITS == 2) {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) unpack_halves<BITS>(p2[b] >> (8 * h), hc, zc[b], o[b]);
+                    } else {
+                        const auto p = h == 0 ? p2 : __builtin_amdgcn_permlane32_swap(words[2 % words_of_32<BITS>()], words[3 % words_of_32<BITS>()], false, false);
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) unpack_halves<BITS>(p[b], hc, zc[b], o[b]);
                     }
-                } else {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const auto p = __builtin_amdgcn_permlane32_swap(words[2 * h], words[2 * h + 1], false, false);
+                    for (int m = 0; m < MB; ++m)
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) unpack_halves<BITS>(p[b], hc, zc[b], o[b][2 * g + h]);
-                    }
+                        for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) sum[m][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xo[k][m * PARTS + part].v, o[b].v, sum[m][b], 0, 0, 0);
                 }
             }
 #pragma unroll
-            for (int m = 0; m < MB; ++m) {
-                float16v sum[2];
-                sum[0] = 0.0f;
-                sum[1] = 0.0f;
-#pragma unroll
-                for (int k = 0; k < 2 * GP; ++k)
-#pragma unroll
-                    for (int part = 0; part < PARTS; ++part) {
-                        const int octet = (i * GP * 2 + k) * 2 + half;
-                        HalfOperand xo;
-                        xo.q = *(const uint4 *)(x + (part * ROWS + m * 32 + r0) * 256 + ((octet ^ (r0 & 15)) * 16));
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) sum[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xo.v, o[b][k].v, sum[b], 0, 0, 0);
-                    }
+            for (int m = 0; m < MB; ++m)
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) y[m][b][e] = __builtin_fmaf(__uint_as_float(s[b]), sum[b][e], y[m][b][e]);
-            }
+                    for (int e = 0; e < 16; ++e) y[m][b][e] = __builtin_fmaf(__uint_as_float(s[b]), sum[m][b][e], y[m][b][e]);
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
