@@ -71,6 +71,25 @@ __device__ inline ExpertTile expert_tile(const QgExpertsArgs &a, int64_t tile, i
     return {0, 0, 0};
 }
 
+// Where the weights of a lane's output lie: addresses for the whole wavefront (of the first output's tile) and the lane's distance from them.
+struct OutputWeights {
+    const char *codes, *scales, *zeros;
+    uint32_t codes_lane, scales_lane, zeros_lane;
+};
+__device__ inline OutputWeights output_weights(const QgExpertsArgs &a, int expert, int64_t n)
+{
+    const uint32_t tile = (uint32_t)(n >> 6), first = __builtin_amdgcn_readfirstlane(tile), in_tile = (uint32_t)n & 63;
+    const char *blob = a.packed + expert * a.expert_stride;
+    OutputWeights w;
+    w.codes = blob + first * a.tile_codes;
+    w.scales = blob + a.scales_off + first * a.tile_scales;
+    w.zeros = blob + a.zeros_off + first * a.tile_zeros;
+    w.codes_lane = (tile - first) * (uint32_t)a.tile_codes + in_tile * 16;
+    w.scales_lane = (tile - first) * (uint32_t)a.tile_scales + in_tile * 4;
+    w.zeros_lane = (tile - first) * (uint32_t)a.tile_zeros + in_tile * 4;
+    return w;
+}
+
 __device__ inline float silu(float v) { return v / (1.0f + expf(-v)); }
 
 __device__ inline void store_typed(int type, void *p, int64_t i, float v)

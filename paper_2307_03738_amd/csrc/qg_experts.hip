@@ -105,15 +105,19 @@ int few_plan(const QgExpertsArgs &a, int bits, hipStream_t st)
 {
     QgFewArgs f = {};
     f.e = a;
-    f.tile_rows = a.x_type == QG_F32 ? FEW_ROWS / 2 : FEW_ROWS;
+    const int parts = a.x_type == QG_F32 ? 2 : 1;
+    f.most = a.slots * parts <= (int64_t)8 * a.experts ? 16 : FEW_ROWS;
+    f.tile_rows = f.most / parts;
     f.e.row_tiles = (int)qg_most_tiles(a.slots, a.experts, f.tile_rows);
     const int64_t used = a.experts < a.slots ? a.experts : a.slots;
-    f.tiles = a.gated || used * ((a.columns + 127) / 128) >= 2 * qg_compute_units() ? 2 : 1;
-    const int width = a.gated || f.tiles == 1 ? 64 : 128;
+    // as few tiles as leave one round of workgroups, two of 16 operand rows on a compute unit or one of more
+    f.tile_shift = a.gated;
+    while (f.tile_shift < 3 && used * ((a.columns + (64 << (f.tile_shift - a.gated)) - 1) >> (6 + f.tile_shift - a.gated)) > (f.most == 16 ? 2 : 1) * qg_compute_units()) ++f.tile_shift;
+    f.tiles = 1 << f.tile_shift;
+    const int width = 64 << (f.tile_shift - a.gated);
     f.g32 = a.group / 32;
     f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);
-    const int quantum = bits == 2 ? 256 : 128;
-    f.quanta = (a.K + quantum - 1) / quantum;
+    f.quanta = (a.K + 127) / 128;
     const int64_t blocks = (int64_t)f.e.row_tiles * ((a.columns + width - 1) / width);
     if (blocks > QG_MOST_GROUPS / 2) return QG_ERR_SHAPE;
     f.blocks = (int)blocks;
