@@ -1,6 +1,6 @@
 // The experts' products where an expert has few rows: bound by reading the packed matrices once.
 //
-// A workgroup of eight wavefronts takes 1, 2, 4 or 8 tiles of 64 outputs (gated: gates and ups of half as many columns) of up to 32
+// A workgroup of eight wavefronts takes 1, 2, 4 or 8 tiles of 64 outputs (gated: gates and ups of half as many columns) of up to 16
 // operand rows of an expert, K cut into 8, 4, 2 or 1 slices of whole 128 k over its wavefronts.  X goes through LDS as f16 (rows of two parts if it is fp32),
 // in the order in which the codes come out of their words; the weights go from memory into registers, in a ring of a few times 128 k that no register leaves by a
 // copy (which would wait for it), and into the 16 x 16 x 32 matrix instruction as q - z.  fp32 sums of a group (or 128 k of it) are multiplied by its scale; slices meet in LDS.
@@ -12,12 +12,11 @@
 #include "qg_experts_codes.h"
 
 constexpr int FEW_LDS = (64 << 10) - 256;      // for rows of X; and 35 KB at the end
-constexpr int FEW_ROWS = 64;                   // operand rows, at most
+constexpr int FEW_ROWS = 16;                   // operand rows
 constexpr int FEW_PAD = 68;                    // floats from one row of sums to the next: rows 4 apart on other banks
 
 struct QgFewArgs {
     QgExpertsArgs e;
-    int most;                  // operand rows of a workgroup, 16 or FEW_ROWS
     int tile_rows;             // rows of X a workgroup takes
     int tiles, tile_shift;     // tiles of 64 outputs a workgroup takes: 1, 2, 4 or 8, and its logarithm
     int g32, gshift;           // group / 32, its logarithm or -1
@@ -37,8 +36,8 @@ struct FewWeights {
     int shift[FOLDS];
 };
 
-// MB: blocks of 16 operand rows; RING: how many times 128 k are under way.
-template <int BITS, int GP, int MB, int RING>
+// RING: how many times 128 k are under way.
+template <int BITS, int GP, int RING>
 __device__ inline void few_rows(const QgFewArgs &f, const ExpertTile &t, int64_t column0, char *smem, uint32_t *most, int rows, int parts)
 {
     using F = Fmt<BITS>;
@@ -77,13 +76,11 @@ __device__ inline void few_rows(const QgFewArgs &f, const ExpertTile &t, int64_t
         }
     };
 
-    float4v y[MB][4];
+    float4v y[4];
 #pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) y[m][b] = 0.0f;
+    for (int b = 0; b < 4; ++b) y[b] = 0.0f;
     const HalfConst hc = half_constants<BITS>();
-    int up_y[MB][4];                                         // powers of two that y's rows are multiplied by
+    int up_y[4];                                             // powers of two that y's rows are multiplied by
 
     for (int c0 = 0; c0 < f.quanta; c0 += chunk) {
         const int here = f.quanta - c0 < chunk ? f.quanta - c0 : chunk;
@@ -154,22 +151,15 @@ __device__ inline void few_rows(const QgFewArgs &f, const ExpertTile &t, int64_t
 
         // y of the chunks before goes over to this one's powers of two, which are not above theirs
 #pragma unroll
-        for (int m = 0; m < MB; ++m)
+        for (int e = 0; e < 4; ++e) {
+            const int v = 4 * (lane >> 4) + e;
+            const int up = a.x_type == QG_F16 || v >= vrows ? 0 : row_exponent(most[parts == 2 ? v >> 1 : v]);
+            if (c0 > 0)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int v = 16 * m + 4 * (lane >> 4) + e;
-                const int up = a.x_type == QG_F16 || v >= vrows ? 0 : row_exponent(most[parts == 2 ? v >> 1 : v]);
-                if (c0 > 0)
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) y[m][b][e] = __builtin_amdgcn_ldexpf(y[m][b][e], up - up_y[m][e]);
-                up_y[m][e] = up;
-            }
-        const char *xa[MB];
-#pragma unroll
-        for (int m = 0; m < MB; ++m) {
-            const int v = 16 * m + (lane & 15);
-            xa[m] = smem + (v < vrows ? v : vrows - 1) * stride + (lane >> 4) * 16;
+                for (int b = 0; b < 4; ++b) y[b][e] = __builtin_amdgcn_ldexpf(y[b][e], up - up_y[e]);
+            up_y[e] = up;
         }
+        const char *xa = smem + ((lane & 15) < vrows ? lane & 15 : vrows - 1) * stride + (lane >> 4) * 16;
         for (int q = q0; q < q1; q += RING) {
 #pragma unroll
             for (int at = 0; at < RING; ++at) {
@@ -186,35 +176,30 @@ __device__ inline void few_rows(const QgFewArgs &f, const ExpertTile &t, int64_t
                     spread_16(w.s[i], s);
                     spread_16((w.z[i < Weights::ZEROS ? i : 0] >> w.shift[i]) & ((1u << F::ZBITS) - 1), zw);
                     uint32_t zc[4][zero_constants<BITS>()];
-                    float4v sum[4][MB];
+                    float4v sum[4];
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
                         zero_operands<BITS>(zw[b], zc[b]);
-#pragma unroll
-                        for (int m = 0; m < MB; ++m) sum[b][m] = 0.0f;
+                        sum[b] = 0.0f;
                     }
 #pragma unroll
                     for (int g = 0; g < PER; ++g) {
                         uint32_t words[4], ops[4];
                         words_of<BITS>(w.v, i * PER + g, words);
                         words_16<BITS>(words, ops);
-                        HalfOperand x[MB];
-#pragma unroll
-                        for (int m = 0; m < MB; ++m) x[m].q = *(const uint4 *)(xa[m] + ((q + at - c0) * QK + (i * PER + g) * 32) * 2);
+                        HalfOperand x;
+                        x.q = *(const uint4 *)(xa + ((q + at - c0) * QK + (i * PER + g) * 32) * 2);
 #pragma unroll
                         for (int b = 0; b < 4; ++b) {
                             HalfOperand o;
                             unpack_halves<BITS>(ops[b], hc, zc[b], o);
-#pragma unroll
-                            for (int m = 0; m < MB; ++m) sum[b][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[m].v, o.v, sum[b][m], 0, 0, 0);
+                            sum[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.v, o.v, sum[b], 0, 0, 0);
                         }
                     }
 #pragma unroll
                     for (int b = 0; b < 4; ++b)
 #pragma unroll
-                        for (int m = 0; m < MB; ++m)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) y[m][b][e] = __builtin_fmaf(__uint_as_float(s[b]), sum[b][m][e], y[m][b][e]);
+                        for (int e = 0; e < 4; ++e) y[b][e] = __builtin_fmaf(__uint_as_float(s[b]), sum[b][e], y[b][e]);
                 }
                 if (q + at + RING < q1) load(q + at + RING, w);
             }
@@ -222,42 +207,34 @@ __device__ inline void few_rows(const QgFewArgs &f, const ExpertTile &t, int64_t
         __syncthreads();
     }
 
-    // slices meet, 16 operand rows at a time
+    // slices meet
     float *sums = (float *)smem;
 #pragma unroll
-    for (int m = 0; m < MB; ++m) {
-        if (m > 0) __syncthreads();
+    for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sums[(wave * 16 + 4 * (lane >> 4) + e) * FEW_PAD + 16 * b + (lane & 15)] = __builtin_amdgcn_ldexpf(y[m][b][e], -up_y[m][e]);
-        __syncthreads();
-        const int first = 16 * m / parts, here = min(16 / parts, rows - first);
-        const int wide_shift = 6 + f.tile_shift - a.gated, wide = 1 << wide_shift;
-        for (int i = threadIdx.x; i < here * wide; i += 512) {
-            const int r = i >> wide_shift, col = i & (wide - 1);
-            auto total = [&](int which) {
-                float v = 0.0f;
-                for (int sl = 0; sl < slices; ++sl) {
-                    const int w = sl * f.tiles + which;
-                    for (int p = 0; p < parts; ++p) v += sums[(w * 16 + r * parts + p) * FEW_PAD + (col & 63)];
-                }
-                return v;
-            };
-            const int64_t at = column0 + col;
-            if (at >= a.columns) continue;
-            const float v = a.gated ? silu(total(col >> 6 << 1)) * total((col >> 6 << 1) + 1) : total(col >> 6);
-            store_typed(a.y_type, a.y, (t.begin + first + r) * a.columns + at, v);
-        }
+        for (int e = 0; e < 4; ++e) sums[(wave * 16 + 4 * (lane >> 4) + e) * FEW_PAD + 16 * b + (lane & 15)] = __builtin_amdgcn_ldexpf(y[b][e], -up_y[e]);
+    __syncthreads();
+    const int wide_shift = 6 + f.tile_shift - a.gated, wide = 1 << wide_shift;
+    for (int i = threadIdx.x; i < rows * wide; i += 512) {
+        const int r = i >> wide_shift, col = i & (wide - 1);
+        auto total = [&](int which) {
+            float v = 0.0f;
+            for (int sl = 0; sl < slices; ++sl)
+                for (int p = 0; p < parts; ++p) v += sums[((sl * f.tiles + which) * 16 + r * parts + p) * FEW_PAD + (col & 63)];
+            return v;
+        };
+        const int64_t at = column0 + col;
+        if (at >= a.columns) continue;
+        const float v = a.gated ? silu(total(col >> 6 << 1)) * total((col >> 6 << 1) + 1) : total(col >> 6);
+        store_typed(a.y_type, a.y, (t.begin + r) * a.columns + at, v);
     }
 }
 
-// MOST: 16 operand rows, or up to 64 in twice the registers.
-template <int BITS, int GP, int MOST>
-__global__ __launch_bounds__(512, MOST == 16 ? 4 : 2) void experts_few(const QgFewArgs f)
+template <int BITS, int GP>
+__global__ __launch_bounds__(512, 4) void experts_few(const QgFewArgs f)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ uint32_t most[MOST];
+    __shared__ uint32_t most[FEW_ROWS];
     // workgroup i runs on die i % 8: a die's workgroups take neighbouring pieces, so that an expert's tiles of rows share its weights
     int block = blockIdx.x;
     {
@@ -267,35 +244,22 @@ __global__ __launch_bounds__(512, MOST == 16 ? 4 : 2) void experts_few(const QgF
     const int columns = block / f.e.row_tiles;
     const ExpertTile t = expert_tile(f.e, block - columns * f.e.row_tiles, f.tile_rows);
     if (t.rows == 0) return;
-    if (threadIdx.x < MOST) most[threadIdx.x] = 0;
+    if (threadIdx.x < FEW_ROWS) most[threadIdx.x] = 0;
     __syncthreads();
     const int expert = __builtin_amdgcn_readfirstlane(t.expert), rows = __builtin_amdgcn_readfirstlane(t.rows);
     const ExpertTile u = {expert, rows, (int64_t)__builtin_amdgcn_readfirstlane((int)t.begin)};
     const int64_t column0 = (int64_t)columns << (6 + f.tile_shift - f.e.gated);
     const int parts = f.e.x_type == QG_F32 ? 2 : 1;
-    if constexpr (MOST == 16) {
-        few_rows<BITS, GP, 1, BITS == 4 ? 2 : 3>(f, u, column0, smem, most, rows, parts);
-    } else {
-        if (rows * parts <= 16) few_rows<BITS, GP, 1, 4>(f, u, column0, smem, most, rows, parts);
-        else if (rows * parts <= 32) few_rows<BITS, GP, 2, 3>(f, u, column0, smem, most, rows, parts);
-        else few_rows<BITS, GP, 4, 2>(f, u, column0, smem, most, rows, parts);
-    }
-}
-
-template <int BITS, int GP>
-void few_typed(const QgFewArgs &f, hipStream_t st)
-{
-    if (f.most == 16) experts_few<BITS, GP, 16><<<f.blocks, 512, FEW_LDS, st>>>(f);
-    else experts_few<BITS, GP, FEW_ROWS><<<f.blocks, 512, FEW_LDS, st>>>(f);
+    few_rows<BITS, GP, BITS == 4 ? 2 : 3>(f, u, column0, smem, most, rows, parts);
 }
 
 template <int BITS>
 void few_launch(const QgFewArgs &f, hipStream_t st)
 {
-    if (f.gshift < 0) few_typed<BITS, 0>(f, st);
-    else if (f.g32 % 4 == 0) few_typed<BITS, 4>(f, st);
-    else if (f.g32 == 2) few_typed<BITS, 2>(f, st);
-    else few_typed<BITS, 1>(f, st);
+    if (f.gshift < 0) experts_few<BITS, 0><<<f.blocks, 512, FEW_LDS, st>>>(f);
+    else if (f.g32 % 4 == 0) experts_few<BITS, 4><<<f.blocks, 512, FEW_LDS, st>>>(f);
+    else if (f.g32 == 2) experts_few<BITS, 2><<<f.blocks, 512, FEW_LDS, st>>>(f);
+    else experts_few<BITS, 1><<<f.blocks, 512, FEW_LDS, st>>>(f);
 }
 
 }  // namespace

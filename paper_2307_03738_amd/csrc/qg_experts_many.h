@@ -120,10 +120,7 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
     const int64_t wave_column = column0 + wave * (a.gated ? 32 : 64);
     const int64_t column = wave_column + (a.gated ? lane & 31 : lane);
     const int64_t n = (column < a.columns ? column : a.columns - 1) + (a.gated && half ? (int64_t)a.columns : 0);
-    const char *blob = a.packed + t.expert * a.expert_stride;
-    const char *codes = blob + (n >> 6) * a.tile_codes + (n & 63) * 16;
-    const char *scales = blob + a.scales_off + (n >> 6) * a.tile_scales + (n & 63) * 4;
-    const char *zeros = blob + a.zeros_off + (n >> 6) * a.tile_zeros + (n & 63) * 4;
+    const OutputWeights at_n = output_weights(a, t.expert, n);
     const int last_group = a.K / a.group - 1;
     const int steps = (a.K + 127) / 128;
 
@@ -157,14 +154,14 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
     };
     auto load = [&](int step, Weights &w) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) w.v[i] = *(const uint4 *)(codes + ((int64_t)step * LOADS + i) * 1024);
+        for (int i = 0; i < LOADS; ++i) w.v[i] = *(const uint4 *)(at_n.codes + ((int64_t)step * LOADS + i) * 1024 + at_n.codes_lane);
 #pragma unroll
         for (int i = 0; i < FOLDS; ++i) {
             const int k32 = step * 4 + i * GP;
             int g = f.gshift >= 0 ? k32 >> f.gshift : k32 / f.g32;
             g = g < last_group ? g : last_group;
-            w.s[i] = *(const uint32_t *)(scales + (int64_t)g * 256);
-            w.z[i] = *(const uint32_t *)(zeros + (int64_t)(g / ZPER) * 256);
+            w.s[i] = *(const uint32_t *)(at_n.scales + (int64_t)g * 256 + at_n.scales_lane);
+            w.z[i] = *(const uint32_t *)(at_n.zeros + (int64_t)(g / ZPER) * 256 + at_n.zeros_lane);
             w.shift[i] = g % ZPER * F::ZBITS;
         }
     };
