@@ -101,29 +101,6 @@ __global__ __launch_bounds__(256) void experts_any(QgExpertsArgs a)
     }
 }
 
-int few_plan(const QgExpertsArgs &a, int bits, hipStream_t st)
-{
-    QgFewArgs f = {};
-    f.e = a;
-    const int parts = a.x_type == QG_F32 ? 2 : 1;
-    f.tile_rows = FEW_ROWS / parts;
-    f.e.row_tiles = (int)qg_most_tiles(a.slots, a.experts, f.tile_rows);
-    const int64_t used = a.experts < a.slots ? a.experts : a.slots;
-    // as few tiles as leave one round of workgroups, two on a compute unit
-    f.tile_shift = a.gated;
-    while (f.tile_shift < 3 && used * ((a.columns + (64 << (f.tile_shift - a.gated)) - 1) >> (6 + f.tile_shift - a.gated)) > 2 * qg_compute_units()) ++f.tile_shift;
-    f.tiles = 1 << f.tile_shift;
-    const int width = 64 << (f.tile_shift - a.gated);
-    f.g32 = a.group / 32;
-    f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);
-    f.quanta = (a.K + 127) / 128;
-    const int64_t blocks = (int64_t)f.e.row_tiles * ((a.columns + width - 1) / width);
-    if (blocks > QG_MOST_GROUPS / 2) return QG_ERR_SHAPE;
-    f.blocks = (int)blocks;
-    (bits == 4 ? qg_few_launch_b4 : bits == 3 ? qg_few_launch_b3 : qg_few_launch_b2)(f, st);
-    return QG_OK;
-}
-
 // Of the rows of X as f16, and their powers of two.
 struct RowsSpace {
     int64_t padded, bytes, total;
@@ -147,14 +124,45 @@ bool many_of(int64_t slots, int experts, int x_type)
     return slots * (x_type == QG_F32 ? 2 : 1) > (int64_t)8 * experts;
 }
 
-int many_plan(const QgExpertsArgs &a, int bits, void *workspace, hipStream_t st)
+int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)
 {
-    const RowsSpace s = rows_space(a.x_rows, a.K, a.x_type);
+    QgFewArgs f = {};
+    f.e = a;
+    f.xh = p.xh;
+    f.up = p.up;
+    f.padded = s.padded;
+    f.parts = s.parts;
+    f.tile_rows = FEW_ROWS / s.parts;
+    // about one row for each expert that is used, and room for two of them: without prepare_rows
+    const int64_t row_bytes = s.parts * (s.padded * 2 + 16);
+    if (a.slots * 2 <= a.experts && 2 * row_bytes <= FEW_LDS) {
+        f.stride = (int)(s.padded * 2 + 16);
+        if (f.tile_rows * row_bytes > FEW_LDS) f.tile_rows = (int)(FEW_LDS / row_bytes);
+    }
+    f.e.row_tiles = (int)qg_most_tiles(a.slots, a.experts, f.tile_rows);
+    const int64_t used = a.experts < a.slots ? a.experts : a.slots;
+    // as few tiles as leave one round of workgroups, four on a compute unit
+    const int shift = a.gated ? 5 : 6;
+    f.tile_shift = 0;
+    while (f.tile_shift < 2 && used * ((a.columns + (1 << (shift + f.tile_shift)) - 1) >> (shift + f.tile_shift)) > 4 * qg_compute_units()) ++f.tile_shift;
+    const int width = 1 << (shift + f.tile_shift);
+    f.g32 = a.group / 32;
+    f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);
+    f.quanta = (a.K + 127) / 128;
+    const int64_t blocks = (int64_t)f.e.row_tiles * ((a.columns + width - 1) / width);
+    if (blocks > QG_MOST_GROUPS / 2) return QG_ERR_SHAPE;
+    f.blocks = (int)blocks;
+    (bits == 4 ? qg_few_launch_b4 : bits == 3 ? qg_few_launch_b3 : qg_few_launch_b2)(f, p, st);
+    return QG_OK;
+}
+
+int many_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)
+{
     QgManyArgs f = {};
     f.e = a;
     f.e.row_tiles = (int)qg_most_tiles(a.slots, a.experts, MANY_ROWS);
-    f.xh = (const char *)workspace;
-    f.up = (const int32_t *)((const char *)workspace + s.bytes);
+    f.xh = p.xh;
+    f.up = p.up;
     f.padded = s.padded;
     f.parts = s.parts;
     f.g32 = a.group / 32;
@@ -164,7 +172,6 @@ int many_plan(const QgExpertsArgs &a, int bits, void *workspace, hipStream_t st)
     const int64_t blocks = (int64_t)f.e.row_tiles * f.column_blocks;
     if (blocks > QG_MOST_GROUPS) return QG_ERR_SHAPE;
     f.blocks = (int)blocks;
-    const QgPrepareArgs p = {a.x, (char *)workspace, (int32_t *)((char *)workspace + s.bytes), a.x_rows, a.x_stride, s.padded, a.K, a.x_type};
     return (bits == 4 ? qg_many_launch_b4 : bits == 3 ? qg_many_launch_b3 : qg_many_launch_b2)(f, p, st);
 }
 
@@ -185,7 +192,7 @@ extern "C" size_t qg_experts_workspace_bytes(int64_t x_rows, int64_t slots, int6
 {
     if (x_rows < 0 || x_rows > 0x7fffffff || slots < 0 || slots > 0x7fffffff || K <= 0 || K > (int64_t)1 << 24 || experts <= 0 || experts > QG_MAX_EXPERTS ||
         !qg_float_type(x_type)) return 0;
-    return many_of(slots, experts, x_type) ? (size_t)rows_space(x_rows, K, x_type).total : 0;
+    return (size_t)rows_space(x_rows, K, x_type).total;
 }
 
 extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
@@ -228,7 +235,9 @@ extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
     a.y_type = d->y_type;
     const hipStream_t st = (hipStream_t)stream;
     if (d->group % 32 == 0) {
-        const int launched = many_of(d->slots, d->experts, d->x_type) ? many_plan(a, d->bits, d->workspace, st) : few_plan(a, d->bits, st);
+        const RowsSpace s = rows_space(a.x_rows, a.K, a.x_type);
+        const QgPrepareArgs p = {a.x, (char *)d->workspace, (int32_t *)((char *)d->workspace + s.bytes), a.x_rows, a.x_stride, s.padded, a.K, a.x_type};
+        const int launched = many_of(d->slots, d->experts, d->x_type) ? many_plan(a, d->bits, s, p, st) : few_plan(a, d->bits, s, p, st);
         return launched != QG_OK ? launched : qg_launch_status();
     }
     a.row_tiles = (int)qg_most_tiles(d->slots, d->experts, ANY_ROWS);

@@ -5,5 +5,5 @@
 #include "qg_experts_few.h"
 #include "qg_experts_many.h"
 
-void qg_few_launch_b4(const QgFewArgs &f, hipStream_t st) { few_launch<4>(f, st); }
+void qg_few_launch_b4(const QgFewArgs &f, const QgPrepareArgs &p, hipStream_t st) { few_launch<4>(f, p, st); }
 int qg_many_launch_b4(const QgManyArgs &f, const QgPrepareArgs &p, hipStream_t st) { return many_launch<4>(f, p, st); }

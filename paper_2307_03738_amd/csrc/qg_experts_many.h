@@ -1,14 +1,13 @@
 // The experts' products where an expert has many rows: bound by the matrix cores and by what turns codes into operands.
 //
-// prepare_rows converts each row of X once: f16 in the order in which codes come out of their words, one part or, fp32, two, and the
-// row's power of two.  experts_many: a workgroup of four wavefronts takes up to 64 slots of an expert and 256 outputs, a wavefront all of the
+// Rows of X come as prepare_rows leaves them.  A workgroup of four wavefronts takes up to 64 slots of an expert and 256 outputs, a wavefront all of the
 // slots and 64 outputs of its own (gated: gate and up of 32 columns), so that every weight is unpacked once per workgroup.  X's rows, gathered
 // by slot, go from memory to LDS without passing through registers, 128 k ahead, codes to registers; a wavefront reads each operand
 // of X for two 32 x 32 x 16 matrix instructions (half of LDS's rate at full speed of the matrix cores).  Two workgroups share a compute unit: with 128
 // slots and one wavefront a SIMD nothing covers what a wavefront waits for (a prompt of 4096 tokens, 22016 x 4096 4-bit, two of eight: 2.55 ms against 1.71).
 #pragma once
 
-#include "qg_experts_codes.h"
+#include "qg_experts_rows.h"
 
 constexpr int MANY_ROWS = 64;
 
@@ -23,86 +22,8 @@ struct QgManyArgs {
     int blocks;
 };
 
-struct QgPrepareArgs {
-    const char *x;
-    char *xh;
-    int32_t *up;
-    int64_t x_rows, x_stride, padded;
-    int K, type;
-};
-
 #ifdef QG_EXPERTS_KERNELS
 namespace {
-
-// Position of k (0 ... 31) in two operands of 16 k: operand position / 16, lanes of half position / 8 % 2, element position % 8.
-template <int BITS>
-__device__ inline int k_position_32(int k)
-{
-    if constexpr (BITS == 2) {
-        const int w = k >> 4, r = k & 15;
-        return ((r & 7) >> 2) * 16 + w * 8 + 2 * (r & 3) + (r >> 3);
-    } else {
-        return k_position<BITS>(k);
-    }
-}
-
-// A wavefront a row; a lane takes 32 k at a time, whose order is all in its registers then.
-template <int BITS>
-__global__ __launch_bounds__(256) void prepare_rows(const QgPrepareArgs a)
-{
-    const int lane = threadIdx.x & 63;
-    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (row > a.x_rows) return;
-    const int parts = a.type == QG_F32 ? 2 : 1;
-    char *to = a.xh + row * parts * a.padded * 2;
-    if (row == a.x_rows) {
-        for (int64_t k = lane * 8; k < parts * a.padded; k += 512) *(uint4 *)(to + k * 2) = make_uint4(0, 0, 0, 0);
-        if (lane == 0) a.up[row] = 0;
-        return;
-    }
-    const int64_t from = row * a.x_stride;
-    auto eight = [&](int64_t k, float *v) {
-        if (k < a.K) {
-            if (a.type == QG_F32) load_eight<QG_F32>(a.x, from + k, v);
-            else if (a.type == QG_BF16) load_eight<QG_BF16>(a.x, from + k, v);
-            else load_eight<QG_F16>(a.x, from + k, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-        }
-    };
-    int up = 0;
-    if (a.type != QG_F16) {
-        uint32_t most = 0;
-        for (int64_t k = lane * 8; k < a.K; k += 512) {
-            float v[8];
-            eight(k, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = max(most, magnitude_bits(v[e]));
-        }
-        up = row_exponent(most_of(most, 64));
-    }
-    if (lane == 0) a.up[row] = up;
-    constexpr int OCT = BITS == 2 ? 32 : 8;
-    for (int64_t k = lane * OCT; k < a.padded; k += 64 * OCT) {
-        float v[OCT], p[OCT];
-#pragma unroll
-        for (int o = 0; o < OCT; o += 8) eight(k + o, v + o);
-#pragma unroll
-        for (int e = 0; e < OCT; ++e) p[k_position_32<BITS>(e)] = a.type == QG_F16 ? v[e] : __builtin_amdgcn_ldexpf(v[e], up);
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            if (part < parts) {
-#pragma unroll
-                for (int o = 0; o < OCT; o += 8)
-                    *(uint4 *)(to + (part * a.padded + k + o) * 2) =
-                        make_uint4(two_halves(p[o], p[o + 1]), two_halves(p[o + 2], p[o + 3]), two_halves(p[o + 4], p[o + 5]), two_halves(p[o + 6], p[o + 7]));
-#pragma unroll
-                for (int e = 0; e < OCT; ++e) p[e] = left_over(p[e]);
-            }
-        }
-    }
-}
 
 // MB: blocks of 32 slots.
 template <int BITS, int GP, int PARTS, int MB>
@@ -313,9 +234,7 @@ int many_typed(const QgManyArgs &f, hipStream_t st)
 template <int BITS>
 int many_launch(const QgManyArgs &f, const QgPrepareArgs &p, hipStream_t st)
 {
-    const int64_t blocks = (p.x_rows + 4) / 4;
-    const unsigned across = (unsigned)(blocks < QG_MOST_GROUPS ? blocks : QG_MOST_GROUPS);
-    prepare_rows<BITS><<<dim3(across, (unsigned)((blocks + across - 1) / across)), 256, 0, st>>>(p);
+    prepare_launch<BITS>(p, st);
     if (f.parts == 2) return f.g32 % 4 == 0 ? many_typed<BITS, 4, 2>(f, st) : f.g32 % 2 == 0 ? many_typed<BITS, 2, 2>(f, st) : many_typed<BITS, 1, 2>(f, st);
     return f.g32 % 4 == 0 ? many_typed<BITS, 4, 1>(f, st) : f.g32 % 2 == 0 ? many_typed<BITS, 2, 1>(f, st) : many_typed<BITS, 1, 1>(f, st);
 }
