@@ -16,7 +16,7 @@
 constexpr int FEW_ROWS = 16;                   // operand rows
 constexpr int FEW_WAVES = 4;
 constexpr int FEW_LDS = 39 << 10;              // four workgroups a compute unit
-constexpr int FEW_PAD = 68;                    // floats from one row of sums to the next: rows 4 apart on other banks
+constexpr int FEW_PAD = 80;                    // floats from one row of sums to the next: four rows on other banks
 
 struct QgFewArgs {
     QgExpertsArgs e;
@@ -35,11 +35,11 @@ struct QgFewArgs {
 #ifdef QG_EXPERTS_KERNELS
 namespace {
 
-// Weights of 128 k, as loaded, and X's: GP times 32 k share a scale; GP 0: groups of an odd number of 32 k (or of pairs), a scale for each 32 k.
-template <int BITS, int GP, bool SELF>
+// Weights of 128 k, as loaded: GP times 32 k share a scale; GP 0: groups of an odd number of 32 k (or of pairs), a scale for each 32 k.
+template <int BITS, int GP>
 struct FewWeights {
     static constexpr int FOLDS = GP ? 4 / GP : 4, ZEROS = GP ? 1 : FOLDS;
-    uint4 v[BITS], x[SELF ? 1 : 4];
+    uint4 v[BITS];
     uint32_t s[FOLDS], z[ZEROS];               // scales, and the words with the zero-points (shifted where they are used: a shift here would wait)
     int shift[FOLDS];
 };
@@ -49,7 +49,7 @@ template <int BITS, int GP, int RING, bool SELF>
 __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs f)
 {
     using F = Fmt<BITS>;
-    using Weights = FewWeights<BITS, GP, SELF>;
+    using Weights = FewWeights<BITS, GP>;
     constexpr int FOLDS = Weights::FOLDS, PER = 4 / FOLDS, ZPER = 32 / F::ZBITS;
     extern __shared__ __attribute__((aligned(16))) char smem[];      // SELF: rows of X; then sums
     const QgExpertsArgs &a = f.e;
@@ -75,8 +75,9 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
     const OutputWeights at_n = output_weights(a, expert, n);
     const int last_group = a.K / a.group - 1;
 
-    // this lane's operand row (row and part of it), and its quarter of every 32 k
-    const int v = lane & 15, quarter = lane >> 4, row_of = f.parts == 2 ? v >> 1 : v;
+    // this lane's operand row (row and part of it), and its quarter of every 32 k.  Row v is the instruction's row 4 (v % 4) + v / 4, so that the first
+    // four come out in one register of every lane, the next four in the second, and only as many are added up as there are.
+    const int v = (lane & 3) * 4 + (lane >> 2 & 3), quarter = lane >> 4, row_of = f.parts == 2 ? v >> 1 : v;
     int64_t row = a.x_rows;
     if (row_of < rows) {
         row = a.rows ? a.rows[begin + row_of] : begin + row_of;
@@ -104,21 +105,23 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
             if (i < Weights::ZEROS) w.z[i] = *(const uint32_t *)(at_n.zeros + (int64_t)(g / ZPER) * 256 + at_n.zeros_lane);
             w.shift[i] = g % ZPER * F::ZBITS;
         }
-        if constexpr (!SELF) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w.x[i] = *(const uint4 *)(x + ((int64_t)q * 4 + i) * 64);
-        }
     };
 
     float4v y[4];
 #pragma unroll
     for (int b = 0; b < 4; ++b) y[b] = 0.0f;
     const HalfConst hc = half_constants<BITS>();
+    const int vrows = rows * f.parts;
     const int q0 = f.quanta * slice / slices, q1 = f.quanta * (slice + 1) / slices;
     Weights ring[RING];
 #pragma unroll
     for (int i = 0; i < RING; ++i)
         if (q0 + i < q1) load(q0 + i, ring[i]);
+    uint4 xs[SELF ? 1 : 4];                    // X of 128 k
+    if constexpr (!SELF) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xs[i] = *(const uint4 *)(x + ((int64_t)min(q0, f.quanta - 1) * 4 + i) * 64);
+    }
     if constexpr (SELF) {
         __shared__ uint32_t mosts[FEW_WAVES];
         for (int r = 0; r < rows; ++r) {
@@ -198,18 +201,25 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
                     words_16<BITS>(words, ops);
                     HalfOperand xo;
                     if constexpr (SELF) xo.q = *(const uint4 *)(x + ((q + at) * 4 + i * PER + g) * 64);
-                    else xo.q = w.x[i * PER + g];
+                    else xo.q = xs[i * PER + g];
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
                         HalfOperand o;
                         unpack_halves<BITS>(ops[b], hc, zc[b], o);
                         sum[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xo.v, o.v, sum[b], 0, 0, 0);
                     }
+                    if constexpr (!SELF) xs[i * PER + g] = *(const uint4 *)(x + ((int64_t)min(q + at + 1, f.quanta - 1) * 4 + i * PER + g) * 64);
                 }
+                auto fold = [&](int e) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[b][e] = __builtin_fmaf(__uint_as_float(s[b]), sum[b][e], y[b][e]);
+                    for (int b = 0; b < 4; ++b) y[b][e] = __builtin_fmaf(__uint_as_float(s[b]), sum[b][e], y[b][e]);
+                };
+                fold(0);
+                if (vrows > 4) fold(1);
+                if (vrows > 8) {
+                    fold(2);
+                    fold(3);
+                }
             }
             if (q + at + RING < q1) load(q + at + RING, w);
         }
@@ -222,7 +232,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
     for (int e = 0; e < 4; ++e) {
         const int down = -__shfl(up, 4 * quarter + e);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) sums[(wave * 16 + 4 * quarter + e) * FEW_PAD + 16 * b + (lane & 15)] = __builtin_amdgcn_ldexpf(y[b][e], down);
+        for (int b = 0; b < 4; ++b) sums[(wave * 16 + 4 * e + quarter) * FEW_PAD + 16 * b + (lane & 15)] = __builtin_amdgcn_ldexpf(y[b][e], down);
     }
     __syncthreads();
     const int wide_shift = width_shift + f.tile_shift, wide = 1 << wide_shift;
