@@ -116,12 +116,12 @@ RowsSpace rows_space(int64_t x_rows, int64_t K, int x_type)
     return s;
 }
 
-// Whether an expert has rows enough, on average, for the kernel of many rows: more than half of the 16 operand rows of the other's tiles, of
-// which a second one reads the matrix again.  4 a piece of 32 experts' 4096 x 4096 4-bit matrices, fp32 (8 operand rows): 88.7 us against 106; 8 a piece:
-// 179 against 123; bf16, 4 a piece 76 against 92, 8 98 against 99, 12 206 against 102.
+// Whether an expert has rows enough, on average, for the kernel of many rows: more than two tiles of the other's 16 operand rows, each of which reads the
+// matrix again (from cache).  32 experts' 4096 x 4096 4-bit matrices, 12, 16 and 24 rows each: fp32 (8 rows a tile) 101, 120 and 163 us against 127, 134 and 166; bf16, 24, 32
+// and 48 rows: 108, 122 and 163 against 114, 127 and 149; 64 experts' 5632 x 2048, bf16 with 40 rows 202 against 172, fp32 with 20 199 against 178.
 bool many_of(int64_t slots, int experts, int x_type)
 {
-    return slots * (x_type == QG_F32 ? 2 : 1) > (int64_t)8 * experts;
+    return slots * (x_type == QG_F32 ? 2 : 1) > (int64_t)32 * experts;
 }
 
 int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)
@@ -141,10 +141,11 @@ int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepa
     }
     f.e.row_tiles = (int)qg_most_tiles(a.slots, a.experts, f.tile_rows);
     const int64_t used = a.experts < a.slots ? a.experts : a.slots;
-    // as few tiles as leave one round of workgroups, four on a compute unit
+    // as few tiles as leave one and a half rounds of workgroups, four on a compute unit (61 tokens' 2816 x 2048 matrices 59.2 us, with one round at most 68.2; 24 tokens'
+    // 4096 x 1408 28.2, with two 31.3)
     const int shift = a.gated ? 5 : 6;
     f.tile_shift = 0;
-    while (f.tile_shift < 2 && used * ((a.columns + (1 << (shift + f.tile_shift)) - 1) >> (shift + f.tile_shift)) > 4 * qg_compute_units()) ++f.tile_shift;
+    while (f.tile_shift < 2 && used * ((a.columns + (1 << (shift + f.tile_shift)) - 1) >> (shift + f.tile_shift)) > 6 * qg_compute_units()) ++f.tile_shift;
     const int width = 1 << (shift + f.tile_shift);
     f.g32 = a.group / 32;
     f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);

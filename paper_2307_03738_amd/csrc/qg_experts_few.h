@@ -128,7 +128,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
             int64_t from = a.rows ? a.rows[begin + r] : begin + r;
             const bool real = from >= 0 && from < a.x_rows;
             from *= a.x_stride;
-            constexpr int OCT = BITS == 2 ? 16 : 8;           // as many values as decide an operand's eight
+            constexpr int OCT = row_piece<BITS>();
             float p[OCT];
             auto take = [&](int k) {
 #pragma unroll
@@ -151,23 +151,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
             if (row_of == r) up = row_up;
             for (int k = threadIdx.x * OCT; k < f.quanta * 128; k += 64 * FEW_WAVES * OCT) {
                 take(k);
-                // position of the first eight; 2 bits: 16 values are eights 2 j + (their half of 32 k)
-                char *to = smem + r * f.parts * f.stride + (BITS == 2 ? (k & ~31) + (k >> 1 & 8) : k) * 2;
-                float h[2 * OCT];
-#pragma unroll
-                for (int e = 0; e < OCT; ++e) h[k_position_32<BITS>(e)] = a.x_type == QG_F16 ? p[e] : __builtin_amdgcn_ldexpf(p[e], row_up);
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    if (part < f.parts) {
-#pragma unroll
-                        for (int j = 0; j < OCT / 8; ++j) {
-                            float *o = h + 16 * j;
-                            *(uint4 *)(to + part * f.stride + j * 32) = make_uint4(two_halves(o[0], o[1]), two_halves(o[2], o[3]), two_halves(o[4], o[5]), two_halves(o[6], o[7]));
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) o[e] = left_over(o[e]);
-                        }
-                    }
-                }
+                store_piece<BITS>(p, a.x_type, row_up, smem + r * f.parts * f.stride, f.stride, k);
             }
         }
         __syncthreads();

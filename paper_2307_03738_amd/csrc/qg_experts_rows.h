@@ -40,11 +40,37 @@ __device__ inline void eight_of_row(const char *x, int type, int64_t from, int64
     }
 }
 
-// LANES lanes a row, a wavefront or a workgroup; a lane takes 32 k at a time, which it keeps where K ends there (a workgroup: 8192).  Bound by memory where rows are many
-// (read once, from cache a second time where K is longer; written once), by one load and a meeting where they are few.
+// Values of a row that a lane takes together, as many as decide an operand's eight, from k on, and where they go: 2 bits, two eights 16 positions apart.
+template <int BITS> constexpr int row_piece() { return BITS == 2 ? 16 : 8; }
+
+template <int BITS>
+__device__ inline void store_piece(const float *v, int type, int up, char *row, int64_t apart, int64_t k)
+{
+    constexpr int OCT = row_piece<BITS>();
+    char *to = row + (BITS == 2 ? (k & ~31) + (k >> 1 & 8) : k) * 2;
+    float h[2 * OCT];
+#pragma unroll
+    for (int e = 0; e < OCT; ++e) h[k_position_32<BITS>(e)] = type == QG_F16 ? v[e] : __builtin_amdgcn_ldexpf(v[e], up);
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+        if (part == 0 || type == QG_F32) {
+#pragma unroll
+            for (int j = 0; j < OCT / 8; ++j) {
+                float *o = h + 16 * j;
+                *(uint4 *)(to + part * apart + j * 32) = make_uint4(two_halves(o[0], o[1]), two_halves(o[2], o[3]), two_halves(o[4], o[5]), two_halves(o[6], o[7]));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = left_over(o[e]);
+            }
+        }
+    }
+}
+
+// LANES lanes a row, a wavefront or a workgroup, which keep 32 values each (a workgroup: rows up to 8192 are read once).  Bound by memory where rows are many,
+// by one load and a meeting where they are few.
 template <int BITS, int LANES>
 __global__ __launch_bounds__(256) void prepare_rows(const QgPrepareArgs a)
 {
+    constexpr int OCT = row_piece<BITS>(), KEPT = 32 / OCT;
     __shared__ uint32_t mosts[4];
     const int lane = threadIdx.x % LANES;
     const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
@@ -53,22 +79,25 @@ __global__ __launch_bounds__(256) void prepare_rows(const QgPrepareArgs a)
     char *to = a.xh + row * parts * a.padded * 2;
     const bool real = row < a.x_rows;
     const int64_t from = row * a.x_stride;
-    float v[32];
-    auto take = [&](int64_t k, float *to) {
+    auto take = [&](int64_t k, float *v) {
 #pragma unroll
-        for (int o = 0; o < 32; o += 8) eight_of_row(a.x, a.type, from, k + o, a.K, real, to + o);
+        for (int o = 0; o < OCT; o += 8) eight_of_row(a.x, a.type, from, k + o, a.K, real, v + o);
     };
-    take(lane * 32, v);
+    float v[KEPT][OCT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) take((i * LANES + lane) * OCT, v[i]);
     int up = 0;
     if (a.type != QG_F16) {
         uint32_t most = 0;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) most = max(most, magnitude_bits(v[e]));
-        for (int64_t k = (LANES + lane) * 32; k < a.K; k += LANES * 32) {
-            float u[32];
+        for (int i = 0; i < KEPT; ++i)
+#pragma unroll
+            for (int e = 0; e < OCT; ++e) most = max(most, magnitude_bits(v[i][e]));
+        for (int64_t k = (KEPT * LANES + lane) * OCT; k < a.K; k += LANES * OCT) {
+            float u[OCT];
             take(k, u);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) most = max(most, magnitude_bits(u[e]));
+            for (int e = 0; e < OCT; ++e) most = max(most, magnitude_bits(u[e]));
         }
         most = most_of(most, 64);
         if constexpr (LANES > 64) {
@@ -79,22 +108,14 @@ __global__ __launch_bounds__(256) void prepare_rows(const QgPrepareArgs a)
         up = row_exponent(most);
     }
     if (lane == 0) a.up[row] = up;
-    for (int64_t k = lane * 32; k < a.padded; k += LANES * 32) {
-        if (k != lane * 32) take(k, v);
-        float p[32];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) p[k_position_32<BITS>(e)] = a.type == QG_F16 ? v[e] : __builtin_amdgcn_ldexpf(v[e], up);
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            if (part < parts) {
-#pragma unroll
-                for (int o = 0; o < 32; o += 8)
-                    *(uint4 *)(to + (part * a.padded + k + o) * 2) =
-                        make_uint4(two_halves(p[o], p[o + 1]), two_halves(p[o + 2], p[o + 3]), two_halves(p[o + 4], p[o + 5]), two_halves(p[o + 6], p[o + 7]));
-#pragma unroll
-                for (int e = 0; e < 32; ++e) p[e] = left_over(p[e]);
-            }
-        }
+    for (int i = 0; i < KEPT; ++i) {
+        const int64_t k = (i * LANES + lane) * OCT;
+        if (k < a.padded) store_piece<BITS>(v[i], a.type, up, to, a.padded * 2, k);
+    }
+    for (int64_t k = (KEPT * LANES + lane) * OCT; k < a.padded; k += LANES * OCT) {
+        take(k, v[0]);
+        store_piece<BITS>(v[0], a.type, up, to, a.padded * 2, k);
     }
 }
 
