@@ -7,6 +7,8 @@
 // slots and one wavefront a SIMD nothing covers what a wavefront waits for (a prompt of 4096 tokens, 22016 x 4096 4-bit, two of eight: 2.55 ms against 1.71).
 #pragma once
 
+#include <type_traits>
+
 #include "qg_experts_rows.h"
 
 constexpr int MANY_ROWS = 64;
@@ -169,23 +171,30 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
         __builtin_amdgcn_s_barrier();
     }
 
+    // out: the type is asked for once; rows lie in scalar addresses, a lane's column and half beside them
     const int64_t c = wave_column + r0;
+    const bool first = c < a.columns, second = !a.gated && c + 32 < a.columns;
+    auto store = [&](auto type) {
+        constexpr int TYPE = decltype(type)::value, SIZE = TYPE == QG_F32 ? 4 : 2;
+        const uint32_t lane_at = ((uint32_t)(4 * half) * (uint32_t)a.columns + r0) * SIZE;
 #pragma unroll
-    for (int m = 0; m < MB; ++m)
+        for (int m = 0; m < MB; ++m)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int r = 32 * m + 8 * (e / 4) + 4 * half + e % 4;
-            const int down = -ups[r];
-            if (r >= t.rows) continue;
-            const float v0 = __builtin_amdgcn_ldexpf(y[m][0][e], down), v1 = __builtin_amdgcn_ldexpf(y[m][1][e], down);
-            const int64_t at = (t.begin + r) * a.columns + c;
-            if (a.gated) {
-                if (c < a.columns) store_typed(a.y_type, a.y, at, silu(v0) * v1);
-            } else {
-                if (c < a.columns) store_typed(a.y_type, a.y, at, v0);
-                if (c + 32 < a.columns) store_typed(a.y_type, a.y, at + 32, v1);
+            for (int e = 0; e < 16; ++e) {
+                const int r = 32 * m + 8 * (e / 4) + e % 4;
+                if (r >= t.rows) continue;
+                const int down = -ups[r + 4 * half];
+                const float v0 = __builtin_amdgcn_ldexpf(y[m][0][e], down), v1 = __builtin_amdgcn_ldexpf(y[m][1][e], down);
+                char *to = (char *)a.y + ((t.begin + r) * a.columns + wave_column) * SIZE + lane_at;
+                if (r + 4 * half < t.rows) {
+                    if (first) store_float<TYPE>(to, 0, a.gated ? silu(v0) * v1 : v0);
+                    if (second) store_float<TYPE>(to, 32, v1);
+                }
             }
-        }
+    };
+    if (a.y_type == QG_F32) store(std::integral_constant<int, QG_F32>());
+    else if (a.y_type == QG_BF16) store(std::integral_constant<int, QG_BF16>());
+    else store(std::integral_constant<int, QG_F16>());
 }
 
 template <int BITS, int GP, int PARTS>

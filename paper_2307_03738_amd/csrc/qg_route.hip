@@ -18,30 +18,64 @@ struct RouteArgs {
 
 template <typename T> __device__ inline T lowest() { return (T)-__builtin_inff(); }
 
+// What lane ^ OFF holds, once lanes that differ in lower bits hold the same: inside a row of 16 lanes by the vector ALU (pairs, quads, mirrored halves and
+// rows), across rows by swaps.  (By way of LDS each step takes five times as long, and a choice is little else but such steps.)
+template <int OFF>
+__device__ inline uint32_t partner(uint32_t v)
+{
+    if constexpr (OFF == 1) return dpp<0xb1, 0xf>(v);
+    else if constexpr (OFF == 2) return dpp<0x4e, 0xf>(v);
+    else if constexpr (OFF == 4) return dpp<0x141, 0xf>(v);
+    else if constexpr (OFF == 8) return dpp<0x140, 0xf>(v);
+    else if constexpr (OFF == 16) {
+        const auto x = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? x[0] : x[1];
+    } else {
+        const auto x = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? x[0] : x[1];
+    }
+}
+template <int OFF> __device__ inline float partner(float v) { return __uint_as_float(partner<OFF>(__float_as_uint(v))); }
+template <int OFF> __device__ inline int partner(int v) { return (int)partner<OFF>((uint32_t)v); }
+template <int OFF>
+__device__ inline double partner(double v)
+{
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const uint32_t low = partner<OFF>((uint32_t)bits), high = partner<OFF>((uint32_t)(bits >> 32));
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
+
+template <int L, int OFF, typename T, typename OP>
+__device__ inline T team_all(T v, OP op)
+{
+    if constexpr (OFF < L) return team_all<L, 2 * OFF>(op(v, partner<OFF>(v)), op);
+    else return v;
+}
 template <int L, typename T>
 __device__ inline T team_max(T v)
 {
-#pragma unroll
-    for (int off = 1; off < L; off *= 2) {
-        const T o = __shfl_xor(v, off);
-        v = o > v ? o : v;
-    }
-    return v;
+    return team_all<L, 1>(v, [](T a, T b) { return b > a ? b : a; });
 }
 template <int L>
 __device__ inline int team_min(int v)
 {
-#pragma unroll
-    for (int off = 1; off < L; off *= 2) v = min(v, __shfl_xor(v, off));
-    return v;
+    return team_all<L, 1>(v, [](int a, int b) { return min(a, b); });
 }
 template <int L, typename T>
 __device__ inline T team_sum(T v)
 {
-#pragma unroll
-    for (int off = 1; off < L; off *= 2) v += __shfl_xor(v, off);
-    return v;
+    return team_all<L, 1>(v, [](T a, T b) { return a + b; });
 }
+
+// 1 / d, to a unit of its last place, for d of 1 and more.
+__device__ inline double inverse_of(double d)
+{
+    double r = __builtin_amdgcn_rcp(d);
+    r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+    r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+    return d == __builtin_inf() ? 0.0 : r;
+}
+__device__ inline double sigmoid(float x) { return inverse_of(1.0 + exp(-(double)x)); }
 
 __device__ inline float logit_of(const RouteArgs &a, int64_t at)
 {
@@ -84,7 +118,7 @@ __global__ __launch_bounds__(256) void route(RouteArgs a)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         if constexpr (SCORES) {
-            const double p = a.sigmoid ? 1.0 / (1.0 + exp(-(double)l[v])) : raised(l[v]);
+            const double p = a.sigmoid ? sigmoid(l[v]) : raised(l[v]);
             part += p;
             key[v] = p;
         } else {
@@ -132,24 +166,33 @@ __global__ __launch_bounds__(256) void route(RouteArgs a)
             ranks[g] = a.two && second > lowest<KEY>() ? first + second : first;
         }
         __syncthreads();
-        // scores rank groups; without a bias experts rank by their logits all the same (sigmoids near 1 and far softmaxes tie)
-        bool kept[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = v * L + lane, g = size == 1 ? e : (int)__umulhi((uint32_t)e, a.group_magic);
+        // which groups take part, a bit each, over the first keys (which all have read)
+        uint32_t *takes = (uint32_t *)keys;
+        for (int g0 = 0; g0 < a.groups; g0 += L) {
+            const int g = g0 + lane;
             int before = 0;
-            if (e < a.experts) {
+            if (g < a.groups) {
                 const KEY mine = ranks[g];
                 for (int o = 0; o < a.groups; ++o) {
                     const KEY r = ranks[o];
                     before += r > mine || (r == mine && o < g);
                 }
             }
-            kept[v] = before < a.top_groups;
+            const uint64_t all = __ballot(g < a.groups && before < a.top_groups) >> (threadIdx.x % 64 / L * L);
+            if (lane == 0) {
+                if constexpr (L == 16) ((uint16_t *)takes)[g0 / 16] = (uint16_t)all;
+                else takes[g0 / 32] = (uint32_t)all;
+                if constexpr (L == 64) takes[g0 / 32 + 1] = (uint32_t)(all >> 32);
+            }
         }
+        __syncthreads();
+        // scores rank groups; without a bias experts rank by their logits all the same (sigmoids near 1 and far softmaxes tie)
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            key[v] = !kept[v] ? lowest<KEY>() : SCORES && !a.bias ? (KEY)l[v] : key[v];
+        for (int v = 0; v < V; ++v) {
+            const int e = v * L + lane, g = size == 1 ? e : (int)__umulhi((uint32_t)e, a.group_magic);
+            const bool kept = e < a.experts && (takes[g >> 5] >> (g & 31) & 1);
+            key[v] = !kept || key[v] == lowest<KEY>() ? lowest<KEY>() : SCORES && !a.bias ? (KEY)l[v] : key[v];
+        }
     }
 
     int mine = -1;                         // lane j: the token's choice j
@@ -175,7 +218,7 @@ __global__ __launch_bounds__(256) void route(RouteArgs a)
     double p = 0.0;
     if (mine >= 0) {
         const float x = logit_of(a, row + mine);
-        p = a.sigmoid ? 1.0 / (1.0 + exp(-(double)x)) : raised(x);
+        p = a.sigmoid ? sigmoid(x) : raised(x);
     }
     if (a.renormalise) {
         const double sum = team_sum<L>(p);
@@ -214,12 +257,42 @@ struct PlanArgs {
     int32_t *offsets, *slot_tokens, *slots;
     uint32_t pairs, part;      // choices in all, and of a workgroup
     int top_k, experts, bits;  // bits: of an expert's number
+    int32_t *counted;          // parts' choices of each expert, [parts][experts]; or NULL: they are counted where they are needed
+    int parts;
 };
 
 constexpr int PLAN_WAVES = 16;
 
-// A stable counting sort in one launch: every workgroup counts all choices, those before its own part apart, adds the counts up to where
+// Choices of each expert in a part.
+__global__ __launch_bounds__(64 * PLAN_WAVES) void plan_count(PlanArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    int32_t *all = (int32_t *)smem;
+    for (int e = threadIdx.x; e < a.experts; e += 64 * PLAN_WAVES) all[e] = 0;
+    __syncthreads();
+    const uint32_t begin = blockIdx.x * a.part, end = min(a.pairs, begin + a.part);
+    for (uint32_t i = begin + threadIdx.x; i < end; i += 64 * PLAN_WAVES) {
+        const uint32_t e = (uint32_t)a.ids[i];
+        if (e < (uint32_t)a.experts) atomicAdd(&all[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += 64 * PLAN_WAVES) a.counted[(int64_t)blockIdx.x * a.experts + e] = all[e];
+}
+
+// Slots' tokens, of choices' slots.
+__global__ __launch_bounds__(256) void plan_tokens(PlanArgs a)
+{
+    const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+    if (i >= a.pairs) return;
+    const int slot = a.slots[i];
+    if (slot >= 0) a.slot_tokens[slot] = (int32_t)(i / (uint32_t)a.top_k);
+    if (i >= (uint32_t)a.offsets[a.experts]) a.slot_tokens[i] = -1;
+}
+
+// A stable counting sort: every workgroup has the counts of all choices, those before its own part apart, adds the counts up to where
 // each expert begins, and places its part: wavefront by wavefront in order, inside a wavefront by the lanes with the same expert before it.
+// Up to 8 parts of 2048 choices each workgroup counts them all itself, in one launch.  Beyond, parts are counted by a launch before, into what will be slot_tokens, which
+// is therefore filled by a launch after (16383 tokens' eight choices of 192: 27.7 us in one launch).
 // LDS: counts of all choices [experts], where the next choice goes [wave][experts].
 __global__ __launch_bounds__(64 * PLAN_WAVES) void plan(PlanArgs a)
 {
@@ -232,11 +305,27 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void plan(PlanArgs a)
     const uint32_t begin = blockIdx.x * a.part, end = min(a.pairs, begin + a.part);
     const uint32_t per_wave = (a.part / PLAN_WAVES), w0 = min(end, begin + wave * per_wave), w1 = min(end, w0 + per_wave);
     // choices before the part count into the first wavefront's places, as do those of wavefronts before another's into its own
-    for (uint32_t i = threadIdx.x; i < a.pairs; i += 64 * PLAN_WAVES) {
-        const uint32_t e = (uint32_t)a.ids[i];
-        if (e < (uint32_t)E) {
-            atomicAdd(&all[e], 1);
-            if (i < begin) atomicAdd(&next[e], 1);
+    if (a.counted) {
+        // a quarter of the workgroup, at least, goes along the parts of 256 experts
+        for (int i = threadIdx.x; i < E * 4; i += 64 * PLAN_WAVES) {
+            const int e = i % E, quarter = i / E;
+            int sum = 0, before = 0;
+#pragma unroll 4
+            for (int p = quarter; p < a.parts; p += 4) {
+                const int n = a.counted[(int64_t)p * E + e];
+                sum += n;
+                if (p < (int)blockIdx.x) before += n;
+            }
+            atomicAdd(&all[e], sum);
+            atomicAdd(&next[e], before);
+        }
+    } else {
+        for (uint32_t i = threadIdx.x; i < a.pairs; i += 64 * PLAN_WAVES) {
+            const uint32_t e = (uint32_t)a.ids[i];
+            if (e < (uint32_t)E) {
+                atomicAdd(&all[e], 1);
+                if (i < begin) atomicAdd(&next[e], 1);
+            }
         }
     }
     for (uint32_t i = w0 + lane; i < w1; i += 64) {
@@ -269,7 +358,8 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void plan(PlanArgs a)
         }
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) a.offsets[E] = total;
-    for (uint32_t i = total + blockIdx.x * 64 * PLAN_WAVES + threadIdx.x; i < a.pairs; i += gridDim.x * 64 * PLAN_WAVES) a.slot_tokens[i] = -1;
+    if (!a.counted)
+        for (uint32_t i = total + blockIdx.x * 64 * PLAN_WAVES + threadIdx.x; i < a.pairs; i += gridDim.x * 64 * PLAN_WAVES) a.slot_tokens[i] = -1;
     __syncthreads();
     int32_t *places = next + wave * E;
     for (uint32_t i0 = w0; i0 < w1; i0 += 64) {
@@ -289,7 +379,7 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void plan(PlanArgs a)
         if (real && before == 0) places[id] += __popcll(same);
         __builtin_amdgcn_wave_barrier();
         if (i < w1) a.slots[i] = slot;
-        if (real) a.slot_tokens[slot] = (int32_t)(i / (uint32_t)a.top_k);
+        if (real && !a.counted) a.slot_tokens[slot] = (int32_t)(i / (uint32_t)a.top_k);
     }
 }
 
@@ -306,42 +396,106 @@ struct CombineArgs {
     uint32_t chunks;           // workgroups of a token
 };
 
-// A lane takes VEC neighbouring columns of a token.
-template <int TYPE, int OUT, int VEC>
+// Eight neighbouring elements that begin anywhere (rows of odd widths): the hardware takes vectors at any element's address.
+template <int TYPE>
+__device__ inline void load_eight_anywhere(const void *p, int64_t i, float *v)
+{
+    if constexpr (TYPE == QG_F32) {
+        __builtin_memcpy(v, (const float *)p + i, 32);
+    } else {
+        uint32_t w[4];
+        __builtin_memcpy(w, (const uint16_t *)p + i, 16);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t bits = e % 2 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu;
+            v[e] = TYPE == QG_BF16 ? bf16_to_float(bits) : f16_to_float(bits);
+        }
+    }
+}
+template <int TYPE>
+__device__ inline void store_eight_anywhere(void *p, int64_t i, const float *v)
+{
+    if constexpr (TYPE == QG_F32) {
+        __builtin_memcpy((float *)p + i, v, 32);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] = TYPE == QG_BF16 ? float_to_bf16(v[2 * e]) | float_to_bf16(v[2 * e + 1]) << 16 : float_to_f16(v[2 * e]) | float_to_f16(v[2 * e + 1]) << 16;
+        __builtin_memcpy((uint16_t *)p + i, w, 16);
+    }
+}
+
+// A lane takes eight neighbouring columns of a token, the last one of a row as many as there are.  The token's slots and weights are loaded by a lane each
+// (64 choices at most); four choices' rows are under way at once.
+template <int TYPE, int OUT>
 __global__ __launch_bounds__(256) void combine(CombineArgs a)
 {
     const uint32_t token = blockIdx.x / a.chunks;
-    const int64_t n = ((int64_t)(blockIdx.x - token * a.chunks) * 256 + threadIdx.x) * VEC;
-    if (n >= a.N) return;
-    float sum[VEC];
+    const int64_t n = ((int64_t)(blockIdx.x - token * a.chunks) * 256 + threadIdx.x) * 8;
+    const int choice = threadIdx.x & 63;
+    int slot = -1;
+    float weight = 0.0f;
+    if (choice < a.top_k) {
+        slot = a.slots[(int64_t)token * a.top_k + choice];
+        weight = a.weights[(int64_t)token * a.top_k + choice];
+    }
+    if (slot >= a.y_rows) slot = -1;
+    const int64_t left = a.N - n;
+    if (__ballot(left > 0) == 0) return;
+    const bool whole = left >= 8;
+    float sum[8];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) sum[v] = 0.0f;
+    for (int v = 0; v < 8; ++v) sum[v] = 0.0f;
+    auto take = [&](int64_t row, float *v) {
+        if (whole) {
+            load_eight_anywhere<TYPE>(a.y, row * a.N + n, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < left ? load_as_float<TYPE>(a.y, row * a.N + n + i) : 0.0f;
+        }
+    };
     if (a.residual) {
         const int64_t at = (int64_t)token * a.residual_stride + n;
-        if constexpr (VEC == 8) load_eight<OUT>(a.residual, at, sum);
-        else sum[0] = load_as_float<OUT>(a.residual, at);
-    }
-    for (int j = 0; j < a.top_k; ++j) {
-        const int64_t pair = (int64_t)token * a.top_k + j;
-        const int32_t slot = a.slots[pair];
-        const float w = a.weights[pair];
-        if (slot < 0 || slot >= a.y_rows) continue;
-        float v[VEC];
-        if constexpr (VEC == 8) load_eight<TYPE>(a.y, slot * a.N + n, v);
-        else v[0] = load_as_float<TYPE>(a.y, slot * a.N + n);
+        if (whole) {
+            load_eight_anywhere<OUT>(a.residual, at, sum);
+        } else {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) sum[i] = __builtin_fmaf(w, v[i], sum[i]);
+            for (int i = 0; i < 8; ++i)
+                if (i < left) sum[i] = load_as_float<OUT>(a.residual, at + i);
+        }
     }
-    if constexpr (VEC == 8) store_eight<OUT>(a.out, (int64_t)token * a.N + n, sum);
-    else store_float<OUT>(a.out, (int64_t)token * a.N + n, sum[0]);
+    for (int j = 0; j < a.top_k; j += 4) {
+        float v[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int row = __builtin_amdgcn_readlane(slot, min(j + u, 63));
+            if (j + u < a.top_k && row >= 0) take(row, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int row = __builtin_amdgcn_readlane(slot, min(j + u, 63));
+            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), min(j + u, 63)));
+            if (j + u < a.top_k && row >= 0)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(w, v[u][i], sum[i]);
+        }
+    }
+    const int64_t at = (int64_t)token * a.N + n;
+    if (whole) {
+        store_eight_anywhere<OUT>(a.out, at, sum);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) store_float<OUT>(a.out, at + i, sum[i]);
+    }
 }
 
 template <int TYPE, int OUT>
-void combine_launch(const CombineArgs &a, bool eights, hipStream_t st)
+void combine_launch(const CombineArgs &a, hipStream_t st)
 {
     CombineArgs b = a;
-    const int64_t per = 256 * (eights ? 8 : 1);
-    b.chunks = (uint32_t)((a.N + per - 1) / per);
+    b.chunks = (uint32_t)((a.N + 2047) / 2048);
     const int64_t turn = QG_MOST_GROUPS / b.chunks > 0 ? QG_MOST_GROUPS / b.chunks : 1;
     for (int64_t done = 0; done < a.tokens; done += turn) {
         b.tokens = a.tokens - done < turn ? a.tokens - done : turn;
@@ -350,17 +504,16 @@ void combine_launch(const CombineArgs &a, bool eights, hipStream_t st)
         if (a.residual) b.residual = (const char *)a.residual + done * a.residual_stride * qg_type_bytes(OUT);
         b.out = (char *)a.out + done * a.N * qg_type_bytes(OUT);
         const unsigned blocks = (unsigned)(b.tokens * b.chunks);
-        if (eights) combine<TYPE, OUT, 8><<<blocks, 256, 0, st>>>(b);
-        else combine<TYPE, OUT, 1><<<blocks, 256, 0, st>>>(b);
+        combine<TYPE, OUT><<<blocks, 256, 0, st>>>(b);
     }
 }
 
 template <int TYPE>
-void combine_typed(const CombineArgs &a, int out, bool eights, hipStream_t st)
+void combine_typed(const CombineArgs &a, int out, hipStream_t st)
 {
-    if (out == QG_F32) combine_launch<TYPE, QG_F32>(a, eights, st);
-    else if (out == QG_BF16) combine_launch<TYPE, QG_BF16>(a, eights, st);
-    else combine_launch<TYPE, QG_F16>(a, eights, st);
+    if (out == QG_F32) combine_launch<TYPE, QG_F32>(a, st);
+    else if (out == QG_BF16) combine_launch<TYPE, QG_BF16>(a, st);
+    else combine_launch<TYPE, QG_F16>(a, st);
 }
 
 }  // namespace
@@ -397,7 +550,7 @@ extern "C" int qg_expert_plan(const int32_t *ids, int64_t tokens, int top_k, int
     if (tokens < 0 || top_k <= 0 || experts <= 0 || tokens > 0x3fffffff / top_k) return QG_ERR_SHAPE;
     if (!offsets || (tokens && (!ids || !slot_tokens || !slots))) return QG_ERR_NULL;
     if (!qg_aligned_to(ids, 4) || !qg_aligned_to(offsets, 4) || !qg_aligned_to(slot_tokens, 4) || !qg_aligned_to(slots, 4)) return QG_ERR_ALIGN;
-    PlanArgs a = {ids, offsets, slot_tokens, slots, (uint32_t)(tokens * top_k), 64 * PLAN_WAVES, top_k, experts, 0};
+    PlanArgs a = {ids, offsets, slot_tokens, slots, (uint32_t)(tokens * top_k), 64 * PLAN_WAVES, top_k, experts, 0, nullptr, 0};
     while (a.bits < 10 && (experts - 1) >> a.bits) ++a.bits;
     // parts of 2048 choices, of more where that would take more workgroups than compute units
     const uint32_t blocks = (uint32_t)qg_compute_units();
@@ -409,7 +562,15 @@ extern "C" int qg_expert_plan(const int32_t *ids, int64_t tokens, int top_k, int
         (void)hipGetLastError();
         return QG_ERR_DEVICE;
     }
-    plan<<<grid, 64 * PLAN_WAVES, lds, (hipStream_t)stream>>>(a);
+    const hipStream_t st = (hipStream_t)stream;
+    // (parts have 2048 choices at least, experts are 1024 at most: the counts fit)
+    if (grid > 8) {
+        a.counted = slot_tokens;
+        a.parts = (int)grid;
+        plan_count<<<grid, 64 * PLAN_WAVES, (size_t)experts * 4, st>>>(a);
+    }
+    plan<<<grid, 64 * PLAN_WAVES, lds, st>>>(a);
+    if (grid > 8) plan_tokens<<<(a.pairs + 255) / 256, 256, 0, st>>>(a);
     return qg_launch_status();
 }
 
@@ -426,10 +587,9 @@ extern "C" int qg_experts_combine(const qg_combine_desc *d, void *stream)
     if (!qg_aligned_to(d->y, in) || !qg_aligned_to(d->residual, out) || !qg_aligned_to(d->out, out) || !qg_aligned_to(d->slots, 4) || !qg_aligned_to(d->weights, 4))
         return QG_ERR_ALIGN;
     const CombineArgs a = {d->y, d->slots, d->weights, d->residual, d->out, d->y_rows, d->tokens, d->N, d->residual_stride, d->top_k, 0};
-    const bool eights = d->N % 8 == 0 && qg_aligned16(d->y) && qg_aligned16(d->out) && (!d->residual || (qg_aligned16(d->residual) && d->residual_stride % 8 == 0));
     const hipStream_t st = (hipStream_t)stream;
-    if (d->type == QG_F32) combine_typed<QG_F32>(a, d->out_type, eights, st);
-    else if (d->type == QG_BF16) combine_typed<QG_BF16>(a, d->out_type, eights, st);
-    else combine_typed<QG_F16>(a, d->out_type, eights, st);
+    if (d->type == QG_F32) combine_typed<QG_F32>(a, d->out_type, st);
+    else if (d->type == QG_BF16) combine_typed<QG_BF16>(a, d->out_type, st);
+    else combine_typed<QG_F16>(a, d->out_type, st);
     return qg_launch_status();
 }
