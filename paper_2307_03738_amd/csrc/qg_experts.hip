@@ -116,12 +116,23 @@ RowsSpace rows_space(int64_t x_rows, int64_t K, int x_type)
     return s;
 }
 
-// Whether an expert has rows enough, on average, for the kernel of many rows: more than two tiles of the other's 16 operand rows, each of which reads the
-// matrix again (from cache).  32 experts' 4096 x 4096 4-bit matrices, 12, 16 and 24 rows each: fp32 (8 rows a tile) 101, 120 and 163 us against 127, 134 and 166; bf16, 24, 32
-// and 48 rows: 108, 122 and 163 against 114, 127 and 149; 64 experts' 5632 x 2048, bf16 with 40 rows 202 against 172, fp32 with 20 199 against 178.
-bool many_of(int64_t slots, int experts, int x_type)
+// Slots of a workgroup of the kernel of many rows, 64 or 32, or 0: the kernel of few rows.
+//
+// By the rows of an expert, on average: few rows up to 20 operand rows (two of fp32 each); beyond, tiles of 32 slots, three workgroups a compute unit, up to
+// 64 rows (128 of fp32, whose two parts make as much of a weight unpacked).  Each side measured, us: 32 experts' 4096 x 4096 4-bit matrices, groups of 64: 8 rows fp32
+// 81 by few against 96, 12 rows 101 against 99, 16 rows bf16 81 against 82, 24 rows 108 against 104; tiles of 32 against 64, bf16 48 rows 132, 142; fp32 48 rows
+// 179, 240; 100 rows fp32 (5632 x 2048) 416, 458; 512 rows: bf16, 8192 x 4096, groups of 32, 497, 418, fp32 groups of 128 547, 526.
+//
+// And by workgroups: with fewer than one a compute unit tiles of 32, and where those are not 9 to 16 units the wavefronts of few rows, which also divide K.  2 experts, 300 rows, 1000 x 8192:
+// 98 (64), 77 (32), 36 (few); 2, 400 rows, 4096 x 4096: 55, 44, 50; 4, 2000 rows, 400 x 4096: 60, 51, 40; 3, 6000 rows, 1000 x 1024: 36, 37, 63.
+int many_rows_of(const QgExpertsArgs &a, int parts)
 {
-    return slots * (x_type == QG_F32 ? 2 : 1) > (int64_t)32 * experts;
+    if (a.slots * parts <= (int64_t)20 * a.experts) return 0;
+    const int width = a.gated ? 128 : 256;
+    const int64_t across = (a.columns + width - 1) / width;
+    if (qg_most_tiles(a.slots, a.experts, 32) * across * 16 <= (int64_t)9 * qg_compute_units()) return 0;
+    if (a.slots <= (int64_t)64 * parts * a.experts || qg_most_tiles(a.slots, a.experts, 64) * across < qg_compute_units()) return 32;
+    return 64;
 }
 
 int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)
@@ -157,11 +168,12 @@ int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepa
     return QG_OK;
 }
 
-int many_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)
+int many_plan(const QgExpertsArgs &a, int bits, int tile_rows, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)
 {
     QgManyArgs f = {};
     f.e = a;
-    f.e.row_tiles = (int)qg_most_tiles(a.slots, a.experts, MANY_ROWS);
+    f.tile_rows = tile_rows;
+    f.e.row_tiles = (int)qg_most_tiles(a.slots, a.experts, f.tile_rows);
     f.xh = p.xh;
     f.up = p.up;
     f.padded = s.padded;
@@ -238,7 +250,8 @@ extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
     if (d->group % 32 == 0) {
         const RowsSpace s = rows_space(a.x_rows, a.K, a.x_type);
         const QgPrepareArgs p = {a.x, (char *)d->workspace, (int32_t *)((char *)d->workspace + s.bytes), a.x_rows, a.x_stride, s.padded, a.K, a.x_type};
-        const int launched = many_of(d->slots, d->experts, d->x_type) ? many_plan(a, d->bits, s, p, st) : few_plan(a, d->bits, s, p, st);
+        const int many = many_rows_of(a, s.parts);
+        const int launched = many ? many_plan(a, d->bits, many, s, p, st) : few_plan(a, d->bits, s, p, st);
         return launched != QG_OK ? launched : qg_launch_status();
     }
     a.row_tiles = (int)qg_most_tiles(d->slots, d->experts, ANY_ROWS);

@@ -1,6 +1,6 @@
 // The experts' products where an expert has many rows: bound by the matrix cores and by what turns codes into operands.
 //
-// Rows of X come as prepare_rows leaves them.  A workgroup of four wavefronts takes up to 64 slots of an expert and 256 outputs, a wavefront all of the
+// Rows of X come as prepare_rows leaves them.  A workgroup of four wavefronts takes up to 64 slots of an expert (or 32: many_rows_of) and 256 outputs, a wavefront all of the
 // slots and 64 outputs of its own (gated: gate and up of 32 columns), so that every weight is unpacked once per workgroup.  X's rows, gathered
 // by slot, go from memory to LDS without passing through registers, 128 k ahead, codes to registers; a wavefront reads each operand
 // of X for two 32 x 32 x 16 matrix instructions (half of LDS's rate at full speed of the matrix cores).  Two workgroups share a compute unit: with 128
@@ -11,8 +11,6 @@
 
 #include "qg_experts_rows.h"
 
-constexpr int MANY_ROWS = 64;
-
 struct QgManyArgs {
     QgExpertsArgs e;
     const char *xh;            // rows of f16, [x_rows + 1][parts][padded]: the last one zeros
@@ -20,6 +18,7 @@ struct QgManyArgs {
     int64_t padded;            // k a row is filled up to: a multiple of 128
     int parts;
     int g32, gshift;
+    int tile_rows;             // slots of a workgroup: 32 or 64
     int column_blocks;         // of 256 outputs
     int blocks;
 };
@@ -197,11 +196,12 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
     else store(std::integral_constant<int, QG_F16>());
 }
 
-template <int BITS, int GP, int PARTS>
-__global__ __launch_bounds__(256, 2) void experts_many(const QgManyArgs f)
+// MOST: 32 slots in registers for three workgroups a compute unit, or 64 for two.
+template <int BITS, int GP, int PARTS, int MOST>
+__global__ __launch_bounds__(256, MOST == 1 ? 3 : 2) void experts_many(const QgManyArgs f)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ int32_t ups[MANY_ROWS];
+    __shared__ int32_t ups[32 * MOST];
     // A die's workgroups (i % 8) take neighbouring pieces, eight blocks of columns by as many tiles of slots: they share X's rows and weights in its L2.
     int block = blockIdx.x;
     {
@@ -210,34 +210,40 @@ __global__ __launch_bounds__(256, 2) void experts_many(const QgManyArgs f)
     }
     const int band = block / (8 * f.e.row_tiles), across = min(8, f.column_blocks - 8 * band);
     const int rest = block - band * 8 * f.e.row_tiles;
-    const ExpertTile t = expert_tile(f.e, rest / across, MANY_ROWS);
+    const ExpertTile t = expert_tile(f.e, rest / across, 32 * MOST);
     if (t.rows == 0) return;
     const int expert = __builtin_amdgcn_readfirstlane(t.expert), rows = __builtin_amdgcn_readfirstlane(t.rows);
     const ExpertTile u = {expert, rows, (int64_t)__builtin_amdgcn_readfirstlane((int)t.begin)};
     const int64_t column0 = (int64_t)(8 * band + rest % across) * (f.e.gated ? 128 : 256);
     if (rows <= 32) many_rows<BITS, GP, PARTS, 1>(f, u, column0, smem, ups);
-    else many_rows<BITS, GP, PARTS, 2>(f, u, column0, smem, ups);
+    else if constexpr (MOST == 2) many_rows<BITS, GP, PARTS, 2>(f, u, column0, smem, ups);
 
 }
 
-template <int BITS, int GP, int PARTS>
-int many_typed(const QgManyArgs &f, hipStream_t st)
+template <int BITS, int GP, int PARTS, int MOST>
+int many_sized(const QgManyArgs &f, hipStream_t st)
 {
-    constexpr size_t lds = (size_t)2 * MANY_ROWS * 256 * PARTS;
+    constexpr size_t lds = (size_t)2 * 32 * MOST * 256 * PARTS;
     if (lds > 63 << 10) {
         static std::atomic<bool> prepared[64];      // once per device (devices past the table: every time)
         int dev = -1;
         if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = -1;
         if (dev < 0 || !prepared[dev].load(std::memory_order_acquire)) {
-            if (hipFuncSetAttribute((const void *)experts_many<BITS, GP, PARTS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
+            if (hipFuncSetAttribute((const void *)experts_many<BITS, GP, PARTS, MOST>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
                 (void)hipGetLastError();
                 return QG_ERR_DEVICE;
             }
             if (dev >= 0) prepared[dev].store(true, std::memory_order_release);
         }
     }
-    experts_many<BITS, GP, PARTS><<<f.blocks, 256, lds, st>>>(f);
+    experts_many<BITS, GP, PARTS, MOST><<<f.blocks, 256, lds, st>>>(f);
     return QG_OK;
+}
+
+template <int BITS, int GP, int PARTS>
+int many_typed(const QgManyArgs &f, hipStream_t st)
+{
+    return f.tile_rows == 32 ? many_sized<BITS, GP, PARTS, 1>(f, st) : many_sized<BITS, GP, PARTS, 2>(f, st);
 }
 
 template <int BITS>

@@ -262,8 +262,37 @@ PRODUCTS = [
     (2050, 160, 4, 32, [200], False, F32, BF16, True, 0),
 ]
 
+# wide matrices and rows enough for the tiles of 64 and of 32 slots, every width, scales for 32, 64, 128 k and odd numbers of 32, K that ends inside 128
+WIDE = [
+    (5130, 160, 4, 32, [300, 419], False, F32, F32, True, 0),
+    (2570 * 2, 352, 4, 32, [419, 300, 1], True, BF16, BF16, True, 8),
+    (5130, 320, 4, 64, [419, 300], False, F16, F32, False, 0),
+    (2562 * 2, 192, 4, 64, [300, 419], True, F32, F32, True, 0),
+    (5130, 384, 4, 128, [129, 600], False, BF16, F32, True, 0),
+    (5130, 256, 4, 256, [129, 600], False, F32, F16, True, 0),
+    (5130, 288, 4, 96, [129, 600], False, F16, F16, True, 0),
+    (5130, 384, 4, 192, [129, 600], False, BF16, BF16, True, 0),
+    (5130, 160, 3, 32, [300, 419], False, F32, F32, True, 0),
+    (5130, 320, 3, 64, [300, 419], False, BF16, F32, True, 0),
+    (2562 * 2, 384, 3, 128, [300, 419], True, F16, F16, True, 0),
+    (5130, 160, 2, 32, [300, 419], False, F16, F32, True, 0),
+    (5130, 320, 2, 64, [300, 419], False, F32, BF16, True, 0),
+    (2562 * 2, 384, 2, 128, [300, 419], True, BF16, F32, True, 0),
+    (5130, 288, 2, 96, [300, 419], False, F32, F32, False, 0),
+    (7170, 160, 4, 32, [40, 33, 0, 64, 31], False, F32, F32, True, 0),
+    (3590 * 2, 192, 4, 64, [40, 33, 0, 64, 31], True, BF16, BF16, True, 0),
+    (7170, 384, 4, 128, [40, 33, 2, 64, 31], False, F16, F32, True, 0),
+    (7170, 192, 4, 96, [40, 33, 2, 64, 31], False, BF16, F32, True, 0),
+    (7170, 160, 3, 32, [40, 33, 2, 64, 31], False, BF16, F16, True, 0),
+    (7170, 192, 3, 64, [40, 33, 2, 64, 31], False, F32, F32, True, 0),
+    (7170, 384, 3, 384, [40, 33, 2, 64, 31], False, F16, F32, True, 0),
+    (7170, 160, 2, 32, [40, 33, 2, 64, 31], False, F32, F32, True, 0),
+    (3590 * 2, 192, 2, 64, [40, 33, 2, 64, 31], True, F16, F16, True, 0),
+    (7170, 256, 2, 128, [40, 33, 2, 64, 31], False, BF16, F32, True, 0),
+]
 
-@pytest.mark.parametrize("N,K,bits,group,counts,gated,xt,yt,given,gap", PRODUCTS)
+
+@pytest.mark.parametrize("N,K,bits,group,counts,gated,xt,yt,given,gap", PRODUCTS + WIDE)
 def test_products_match_64_bits(qg, N, K, bits, group, counts, gated, xt, yt, given, gap):
     case("product", N, K, bits, group, counts[:6], gated, xt, yt, given)
     g = gen(N + K + len(counts))
@@ -291,12 +320,12 @@ def test_products_match_64_bits(qg, N, K, bits, group, counts, gated, xt, yt, gi
         assert (y[[3, 5]] == 0).all()
 
 
-@pytest.mark.parametrize("counts", [[2, 3], [40, 3], [300, 9]])
+@pytest.mark.parametrize("N,counts", [(96, [1, 0, 0, 2, 0, 0, 0, 0]), (96, [2, 3]), (96, [40, 3]), (96, [300, 9]), (7168, [64, 90]), (5120, [400, 300])])
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
-def test_values_that_are_no_numbers_stay_in_their_rows(qg, counts, dt):
-    case("nan", counts, dt)
-    N, K, group = 96, 256, 64
-    packed, W = blobs(qg, 2, N, K, 4, group, 5)
+def test_values_that_are_no_numbers_stay_in_their_rows(qg, N, counts, dt):
+    case("nan", N, counts, dt)
+    K, group = 256, 64
+    packed, W = blobs(qg, len(counts), N, K, 4, group, 5)
     offsets = offsets_of(counts)
     x = torch.randn(offsets[-1], K, generator=gen(1)).to(dt)
     x[1, 5], x[2, 250] = math.nan, INF
@@ -306,11 +335,11 @@ def test_values_that_are_no_numbers_stay_in_their_rows(qg, counts, dt):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
-@pytest.mark.parametrize("count", [1, 20, 200])
-def test_rows_of_every_magnitude(qg, dt, count):
+@pytest.mark.parametrize("N,count", [(70, 1), (70, 20), (70, 200), (5120, 700)])
+def test_rows_of_every_magnitude(qg, dt, N, count):
     # the largest and smallest numbers that leave the result's terms within fp32's range, rows of zeros
-    case("magnitudes", dt, count)
-    N, K, group = 70, 384, 128
+    case("magnitudes", dt, N, count)
+    K, group = 384, 128
     packed, W = blobs(qg, 1, N, K, 4, group, 9)
     x = torch.randn(count, K, generator=gen(2))
     x *= torch.tensor([2.0 ** e for e in (0, 100, -100, 60, -60, -110)])[torch.arange(count) % 6, None]
