@@ -440,7 +440,7 @@ size_t qg_pages_workspace_bytes(int rows, int max_pages, int64_t pages);
 /* ---------------------------------------------------------------------------------------------
  * Experts: a layer whose matrices are chosen by token.  A token's router gives a logit for each expert; qg_route chooses and
  * weighs, qg_expert_plan orders the choices by expert, qg_experts_product multiplies each expert's tokens with its packed matrix,
- * qg_experts_combine adds a token's results up.  The conventions above hold; an empty batch is QG_OK and nothing about the choices
+ * qg_experts_combine adds a token's results up.  The conventions above hold; an empty batch is QG_OK, and nothing about the choices
  * is asked of the host (the calls can be captured and replayed).  Forward only, as all of this library.
  * --------------------------------------------------------------------------------------------- */
 typedef enum { QG_SOFTMAX = 0, QG_SIGMOID = 1 } qg_score;
@@ -472,14 +472,18 @@ int qg_route(const qg_route_desc *d /* HOST */, void *stream);
 /* Slots for all choices, ordered by expert, those of one expert by token and choice:
  *   offsets [experts + 1]: expert e has the slots offsets[e] ... offsets[e + 1] - 1
  *   slot_tokens [tokens * top_k]: each slot's token, -1 from offsets[experts] on
- *   slots [tokens][top_k]: each choice's slot; -1 for an id outside 0 ... experts - 1, which gets none */
+ *   slots [tokens][top_k]: each choice's slot; -1 for an id outside 0 ... experts - 1, which gets none
+ * An expert that a token names twice has a slot for each.  ids overlaps no output; an empty batch writes offsets. */
 int qg_expert_plan(const int32_t *ids, int64_t tokens, int top_k, int experts, int32_t *offsets, int32_t *slot_tokens, int32_t *slots, void *stream);
 
 /* For each slot p of expert e, with x the row rows[p] of X (row p, if rows is NULL):
  *   y[p][n] = sum_k What_e[n][k] x[k]                  (N columns), or, gated, with gate and up side by side as in qg_gemv_swiglu,
  *   y[p][n] = silu(gate[n]) * up[n]                    (N / 2 columns: What_e rows [0, N / 2) are gate, the others up)
- * per group as s * sum (q - z) x, sums in fp32.  A row outside 0 ... x_rows - 1 counts as zeros.  Rows of y past offsets[experts] are left
- * as they were.  NaN and infinity in X reach their own rows of y alone.  y overlaps no input. */
+ * per group as s * sum (q - z) x, sums in fp32.  Groups of whole 32 k: on the matrix cores, q - z as it is, each row of X times a power of two as f16 (bf16, fp32:
+ * the one that brings its largest |x| to [2^14, 2^15)), fp32 in two parts: 2^-22 of an x is left out, and what lies below 2^-39 of its row's largest.  Other groups, and gated matrices of
+ * 8 GB and more: fp32 multiply-adds (slow from a few rows on).  A call enqueues one kernel or two.
+ * A row outside 0 ... x_rows - 1 counts as zeros.  Rows of y past offsets[experts] are left as they were.  NaN and infinity in X
+ * make their own rows of y NaN or infinite, and no others.  y overlaps no input. */
 typedef struct qg_experts_desc {
     const void *packed;       /* [experts] blobs of QG_LAYOUT_DEVICE (qg_pack), expert_stride bytes apart; 16-byte aligned */
     const void *x;            /* [x_rows][K] of x_type, rows x_stride elements apart (a multiple of 8); 16-byte aligned */
@@ -491,10 +495,10 @@ typedef struct qg_experts_desc {
     int x_type, y_type;       /* QG_F32, QG_BF16 or QG_F16 */
     int gated;
     void *workspace;          /* 16-byte aligned, needs no preparation; calls that overlap in time must not share one */
-    size_t workspace_bytes;   /* qg_experts_workspace_bytes() */
+    size_t workspace_bytes;   /* qg_experts_workspace_bytes(): rows of X as f16 parts */
 } qg_experts_desc;
 int qg_experts_product(const qg_experts_desc *d /* HOST */, void *stream);
-size_t qg_experts_workspace_bytes(int64_t x_rows, int64_t slots, int64_t K, int experts, int x_type);
+size_t qg_experts_workspace_bytes(int64_t x_rows, int64_t K, int x_type);
 
 /* out[t][n] = residual[t][n] + sum_j weights[t][j] * y[slots[t][j]][n], in fp32 in the order of j, rounded once.  A slot outside 0 ... y_rows - 1 adds nothing. */
 typedef struct qg_combine_desc {

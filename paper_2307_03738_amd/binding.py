@@ -134,7 +134,7 @@ def lib():
         L.qg_experts_product.restype = i32
         L.qg_experts_product.argtypes = [cp, vp]
         L.qg_experts_workspace_bytes.restype = sz
-        L.qg_experts_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+        L.qg_experts_workspace_bytes.argtypes = [i64, i64, i32]
         L.qg_experts_combine.restype = i32
         L.qg_experts_combine.argtypes = [cp, vp]
         _LIB = L
@@ -884,8 +884,8 @@ def qg_expert_plan(ids: torch.Tensor, experts: int, out=None):
     return offsets, slot_tokens, slots
 
 
-def qg_experts_workspace_bytes(x_rows: int, slots: int, K: int, experts: int, dtype: torch.dtype = torch.float32) -> int:
-    return int(lib().qg_experts_workspace_bytes(x_rows, slots, K, experts, _FLOATS[dtype]))
+def qg_experts_workspace_bytes(x_rows: int, K: int, dtype: torch.dtype = torch.float32) -> int:
+    return int(lib().qg_experts_workspace_bytes(x_rows, K, _FLOATS[dtype]))
 
 
 def qg_experts_product(packed: torch.Tensor, N: int, K: int, bits: int, group: int, x: torch.Tensor, offsets: torch.Tensor,
@@ -915,15 +915,10 @@ def qg_experts_product(packed: torch.Tensor, N: int, K: int, bits: int, group: i
     ykind = _type(y, "y")
     L = _LIB or lib()
     if workspace is None:
-        size = L.qg_experts_workspace_bytes(x_rows, slots, K, experts, kind)
-        wp = 0
-        if size:
-            workspace = _bytes(size, x.device)
-            wp = workspace.data_ptr()
-    else:
-        wp, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        workspace = _bytes(max(256, L.qg_experts_workspace_bytes(x_rows, K, kind)), x.device)
     rc = L.qg_experts_product(_EXPERTS(packed.data_ptr(), xp, op, rp, y.data_ptr(), N, K, packed.stride(0), x_rows, xs, slots,
-                                       bits, group, experts, kind, ykind, 1 if gated else 0, wp, size), _stream())
+                                       bits, group, experts, kind, ykind, 1 if gated else 0,
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size()), _stream())
     if rc != 0:
         _check(rc, "qg_experts_product")
     return y

@@ -201,10 +201,9 @@ int any_launch(const QgExpertsArgs &a, int64_t blocks, hipStream_t st)
 
 }  // namespace
 
-extern "C" size_t qg_experts_workspace_bytes(int64_t x_rows, int64_t slots, int64_t K, int experts, int x_type)
+extern "C" size_t qg_experts_workspace_bytes(int64_t x_rows, int64_t K, int x_type)
 {
-    if (x_rows < 0 || x_rows > 0x7fffffff || slots < 0 || slots > 0x7fffffff || K <= 0 || K > (int64_t)1 << 24 || experts <= 0 || experts > QG_MAX_EXPERTS ||
-        !qg_float_type(x_type)) return 0;
+    if (x_rows < 0 || x_rows > 0x7fffffff || K <= 0 || K > (int64_t)1 << 24 || !qg_float_type(x_type)) return 0;
     return (size_t)rows_space(x_rows, K, x_type).total;
 }
 
@@ -221,8 +220,7 @@ extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
     if (!d->packed || (!d->x && d->x_rows) || !d->offsets || !d->y) return QG_ERR_NULL;
     if (!qg_aligned16(d->packed) || d->expert_stride % 16 || !qg_aligned16(d->x) || (d->x_rows > 1 && d->x_stride % 8) || !qg_aligned_to(d->offsets, 4) ||
         !qg_aligned_to(d->rows, 4) || !qg_aligned_to(d->y, qg_type_bytes(d->y_type)) || !qg_aligned16(d->workspace)) return QG_ERR_ALIGN;
-    const size_t space = qg_experts_workspace_bytes(d->x_rows, d->slots, d->K, d->experts, d->x_type);
-    if (space && (!d->workspace || d->workspace_bytes < space)) return QG_ERR_WORKSPACE;
+    if (!d->workspace || d->workspace_bytes < qg_experts_workspace_bytes(d->x_rows, d->K, d->x_type)) return QG_ERR_WORKSPACE;
     QgExpertsArgs a = {};
     a.packed = (const char *)d->packed;
     a.x = (const char *)d->x;
@@ -247,7 +245,9 @@ extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
     a.x_type = d->x_type;
     a.y_type = d->y_type;
     const hipStream_t st = (hipStream_t)stream;
-    if (d->group % 32 == 0) {
+    // (the lanes of a wavefront that take ups lie up to so far behind the gates, in 32 bits)
+    const bool near = !a.gated || ((a.columns + 63) / 64 + 2) * a.tile_codes < (int64_t)1 << 32;
+    if (d->group % 32 == 0 && near) {
         const RowsSpace s = rows_space(a.x_rows, a.K, a.x_type);
         const QgPrepareArgs p = {a.x, (char *)d->workspace, (int32_t *)((char *)d->workspace + s.bytes), a.x_rows, a.x_stride, s.padded, a.K, a.x_type};
         const int many = many_rows_of(a, s.parts);

@@ -558,7 +558,7 @@ extern "C" int qg_expert_plan(const int32_t *ids, int64_t tokens, int top_k, int
     while ((uint64_t)a.part * blocks < a.pairs) a.part *= 2;
     const unsigned grid = a.pairs ? (a.pairs + a.part - 1) / a.part : 1;
     const size_t lds = (size_t)experts * (PLAN_WAVES + 1) * 4;
-    if (lds > 65536 && hipFuncSetAttribute((const void *)plan, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
+    if (lds > 65536 - 1024 && hipFuncSetAttribute((const void *)plan, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
         (void)hipGetLastError();
         return QG_ERR_DEVICE;
     }

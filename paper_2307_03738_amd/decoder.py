@@ -4,7 +4,8 @@
 
 runs a small batch with random weights: sequences begin, grow token by token, branch, end, and the pool is packed.
 Every layer is norm -> q/k/v product -> rotate and store -> attention -> output product -> norm -> gate/up product -> down
-product on 2-, 3- or 4-bit weights; hidden states come in and go out (no vocabulary: embedding and sampling are the caller's).
+product on 2-, 3- or 4-bit weights, where a layer may have experts in the place of its gate/up and down matrices: router product -> choice -> order by
+expert -> their gate/up and down products -> weighted sum; hidden states come in and go out (no vocabulary: embedding and sampling are the caller's).
 """
 import math
 from typing import Dict, List, Sequence
@@ -18,11 +19,14 @@ class Decoder:
     """Layers of packed weights, a paged cache for all of them, and the book of a batch of `rows` sequences (at most 128).
 
     weights: for each layer a dict of qkv, out, gate_up, down -- (codes, scales, zero-points) of qg_quantize, q, k and v
-    and gate and up stacked along the outputs -- and norm, norm2 (fp32 [hidden]); final_norm (fp32 [hidden])."""
+    and gate and up stacked along the outputs -- and norm, norm2 (fp32 [hidden]); final_norm (fp32 [hidden]).  A layer of experts has, instead of
+    gate_up and down, router (outputs: the experts) and experts_gate_up, experts_down: a list of such triples, one for each expert, of which
+    every token takes top_k."""
 
     def __init__(self, weights: Sequence[Dict], final_norm: torch.Tensor, heads: int, kv_heads: int, head_dim: int, bits: int, group: int,
                  rows: int, pages: int, max_pages: int, page: int = 16, cache: torch.dtype = torch.bfloat16, base: float = 10000.0,
-                 eps: float = 1e-5):
+                 eps: float = 1e-5, top_k: int = 2):
+        self.top_k = top_k
         self.heads, self.kv_heads, self.head_dim, self.bits, self.group, self.eps = heads, kv_heads, head_dim, bits, group, eps
         self.rows, self.page, self.final_norm = rows, page, final_norm
         device = final_norm.device
@@ -30,12 +34,15 @@ class Decoder:
         spaces: Dict = {}
         for w in weights:
             layer = {"norm": w["norm"], "norm2": w["norm2"]}
-            for name in ("qkv", "out", "gate_up", "down"):
+            for name in ("qkv", "out", "router") if "router" in w else ("qkv", "out", "gate_up", "down"):
                 codes, scales, zeros = w[name]
                 N, K = codes.shape
                 if (N, K) not in spaces:              # one for each shape: products of a stream do not overlap
                     spaces[N, K] = qg.new_workspace(qg.qg_workspace_bytes(N, K, bits, group, rows), device)
                 layer[name] = (qg.qg_pack(codes, scales, zeros, bits, group), N, K, spaces[N, K])
+            for name in ("experts_gate_up", "experts_down") if "router" in w else ():
+                N, K = w[name][0][0].shape
+                layer[name] = (torch.stack([qg.qg_pack(*triple, bits, group) for triple in w[name]]), N, K)
             self.layers.append(layer)
         # a page has the same id in all layers
         shape = (len(self.layers), pages, kv_heads, page, head_dim)
@@ -72,6 +79,14 @@ class Decoder:
         blob, N, K, space = packed
         return qg.qg_gemm_small(blob, N, K, self.bits, self.group, x, workspace=space)
 
+    def _experts(self, layer: Dict, y: torch.Tensor, live: torch.Tensor) -> torch.Tensor:
+        logits = self._product(layer["router"], y).masked_fill(~live[:, None], -math.inf)          # rows that are passed over choose nothing
+        ids, weights = qg.qg_route(logits, self.top_k)
+        (up, N, K), (down, hidden, inner) = layer["experts_gate_up"], layer["experts_down"]
+        offsets, tokens, slots = qg.qg_expert_plan(ids, up.shape[0])
+        h = qg.qg_experts_product(up, N, K, self.bits, self.group, y, offsets, rows=tokens, gated=True)
+        return qg.qg_experts_combine(qg.qg_experts_product(down, hidden, inner, self.bits, self.group, h, offsets), slots, weights)
+
     def step(self, x: torch.Tensor, live: torch.Tensor) -> torch.Tensor:
         """Hidden states after the last layer of one new token for each row of x [rows][hidden] (fp32) that `live` (bool) marks; its
         place, the last cell of its row, has been made by resize().  The other rows are passed over: nothing is stored
@@ -92,13 +107,16 @@ class Decoder:
             seen, _ = qg.qg_paged_attention(q, self.k[i], self.v[i], self.tables, lens, 1 / math.sqrt(D), workspace=self.workspace, **scales)
             update = self._product(layer["out"], seen.view(rows, H * D))
             y, stream, _ = qg.qg_rms_norm(update, layer["norm2"], self.eps, residual=stream)
+            if "router" in layer:
+                update = self._experts(layer, y, live)
+                continue
             gate, up = self._product(layer["gate_up"], y).chunk(2, 1)
             update = self._product(layer["down"], torch.nn.functional.silu(gate) * up)
         return qg.qg_rms_norm(update, self.final_norm, self.eps, residual=stream)[0]
 
 
-def random_weights(layers: int, hidden: int, inner: int, heads: int, kv_heads: int, head_dim: int, bits: int, group: int, seed: int = 0):
-    """Quantized random weights of the right shapes, and the final norm's."""
+def random_weights(layers: int, hidden: int, inner: int, heads: int, kv_heads: int, head_dim: int, bits: int, group: int, seed: int = 0, experts: int = 0):
+    """Quantized random weights of the right shapes, and the final norm's.  experts: every second layer has so many."""
     g = torch.Generator(device="cuda").manual_seed(seed)
 
     def matrix(N, K):
@@ -107,13 +125,19 @@ def random_weights(layers: int, hidden: int, inner: int, heads: int, kv_heads: i
     def norm():
         return 1 + 0.1 * torch.randn(hidden, generator=g, device="cuda")
 
-    return [{"qkv": matrix((heads + 2 * kv_heads) * head_dim, hidden), "out": matrix(hidden, heads * head_dim),
-             "gate_up": matrix(2 * inner, hidden), "down": matrix(hidden, inner), "norm": norm(), "norm2": norm()} for _ in range(layers)], norm()
+    def rest(layer):
+        if not experts or layer % 2 == 0:
+            return {"gate_up": matrix(2 * inner, hidden), "down": matrix(hidden, inner)}
+        return {"router": matrix(experts, hidden), "experts_gate_up": [matrix(2 * inner, hidden) for _ in range(experts)],
+                "experts_down": [matrix(hidden, inner) for _ in range(experts)]}
+
+    return [{"qkv": matrix((heads + 2 * kv_heads) * head_dim, hidden), "out": matrix(hidden, heads * head_dim), **rest(layer),
+             "norm": norm(), "norm2": norm()} for layer in range(layers)], norm()
 
 
 def main() -> None:
     hidden, inner, heads, kv_heads, head_dim, bits, group, rows = 1024, 2816, 8, 2, 128, 4, 128, 6
-    weights, final = random_weights(2, hidden, inner, heads, kv_heads, head_dim, bits, group)
+    weights, final = random_weights(2, hidden, inner, heads, kv_heads, head_dim, bits, group, experts=8)
     model = Decoder(weights, final, heads, kv_heads, head_dim, bits, group, rows, pages=96, max_pages=16, cache=torch.float8_e4m3fn)
     ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
     g = torch.Generator(device="cuda").manual_seed(1)

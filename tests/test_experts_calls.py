@@ -68,7 +68,7 @@ def test_plan_refuses(qg):
     (dict(experts=1025), UNSUPPORTED), (dict(experts=0), SHAPE), (dict(N=0), SHAPE), (dict(K=250), SHAPE), (dict(group=12), SHAPE), (dict(slots=-1), SHAPE), (dict(slots=1 << 31), SHAPE),
     (dict(x_rows=-1), SHAPE), (dict(x_rows=1 << 31), SHAPE), (dict(x_stride=248), SHAPE), (dict(expert_stride=1024), SHAPE), (dict(N=127, gated=1), SHAPE), (dict(packed=72), ALIGN),
     (dict(x=72), ALIGN), (dict(x_stride=260), ALIGN), (dict(expert_stride=(1 << 20) + 8), ALIGN), (dict(offsets=66), ALIGN), (dict(rows=66), ALIGN), (dict(y=130), ALIGN),
-    (dict(workspace=72), ALIGN), (dict(slots=0, x=0, packed=0), OK)])
+    (dict(workspace=72), ALIGN), (dict(workspace=0), WORKSPACE), (dict(workspace_bytes=6 * (2 * 256 * 2 + 4) - 1), WORKSPACE), (dict(slots=0, x=0, packed=0), OK)])
 def test_product_refuses(qg, change, status):
     assert qg.lib().qg_experts_product(qg._EXPERTS(*{**EXPERTS, **change}.values()), None) == status
 
@@ -79,3 +79,11 @@ def test_product_refuses(qg, change, status):
     (dict(y=66), ALIGN), (dict(out=130), ALIGN), (dict(slots=66), ALIGN), (dict(weights=65), ALIGN), (dict(residual=66, residual_stride=64), ALIGN), (dict(tokens=0, y=0, out=0), OK)])
 def test_combine_refuses(qg, change, status):
     assert qg.lib().qg_experts_combine(qg._COMBINE(*{**COMBINE, **change}.values()), None) == status
+
+
+def test_workspace_sizes(qg):
+    import torch
+    size = qg.qg_experts_workspace_bytes
+    assert size(5, 256) == 6 * (2 * 256 * 2 + 4) and size(0, 32, torch.bfloat16) == 128 * 2 + 4          # rows of whole 128 k, and one of zeros
+    assert size(-1, 256) == 0 and size(4, 0) == 0 and qg.lib().qg_experts_workspace_bytes(4, 256, 3) == 0
+    assert size(1 << 30, 1 << 20) == ((1 << 30) + 1) * (4 * (1 << 20) + 4)

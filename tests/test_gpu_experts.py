@@ -160,7 +160,7 @@ def test_sigmoids_that_tie_rank_by_their_logits(qg):
 
 # --- order ------------------------------------------------------------------------------------------------------
 
-@pytest.mark.parametrize("tokens,k,experts", [(1, 1, 1), (1, 8, 8), (48, 4, 32), (1000, 3, 7), (2049, 1, 192), (5000, 8, 1024), (40000, 2, 3), (70001, 8, 100)])
+@pytest.mark.parametrize("tokens,k,experts", [(1, 1, 1), (1, 8, 8), (48, 4, 32), (1000, 3, 7), (2049, 1, 192), (5000, 8, 1024), (3000, 4, 963), (1100, 15, 1000), (40000, 2, 3), (70001, 8, 100)])
 def test_plan_is_a_stable_sort(qg, tokens, k, experts):
     case("plan", tokens, k, experts)
     g = gen(tokens + k)
