@@ -157,6 +157,9 @@ int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepa
     const int shift = a.gated ? 5 : 6;
     f.tile_shift = 0;
     while (f.tile_shift < 2 && used * ((a.columns + (1 << (shift + f.tile_shift)) - 1) >> (shift + f.tile_shift)) > 6 * qg_compute_units()) ++f.tile_shift;
+    // where not even the tiles that could be needed make two and a half workgroups a compute unit, K goes to twice as many wavefronts (8 experts' 4096 x 4096 4-bit matrices, 2 rows
+    // each: fp32 24.7 us, 21.4 so, bf16 4 rows 26.4, 23.0; beyond, fp32 4 rows 27.0, 29.2)
+    f.waves = 2 * (int64_t)f.e.row_tiles * ((a.columns + (1 << shift) - 1) >> shift) <= 5 * qg_compute_units() ? 8 : 4;
     const int width = 1 << (shift + f.tile_shift);
     f.g32 = a.group / 32;
     f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);

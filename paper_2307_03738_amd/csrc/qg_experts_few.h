@@ -1,7 +1,8 @@
 // The experts' products where an expert has few rows: bound by reading the packed matrices once.
 //
 // A wavefront takes a tile of 64 outputs (gated: gates and ups of 32 columns) of up to 16 operand rows of an expert (8 of fp32, in two parts
-// each) and a slice of K; a workgroup of four wavefronts is 1, 2 or 4 tiles by 4, 2 or 1 slices, which meet in LDS.  Rows of X come as prepare_rows
+// each) and a slice of K; a workgroup of four wavefronts is 1, 2 or 4 tiles by 4, 2 or 1 slices, which meet in LDS (of eight: one tile by
+// eight slices).  Rows of X come as prepare_rows
 // leaves them, from cache straight into the operands; the weights go from memory into registers, in a ring of a few times 128 k that no
 // register leaves by a copy (which would wait for it), and into the 16 x 16 x 32 matrix instruction as q - z.  fp32 sums of a group (or 128 k of it) are
 // multiplied by its scale.
@@ -14,7 +15,6 @@
 #include "qg_experts_rows.h"
 
 constexpr int FEW_ROWS = 16;                   // operand rows
-constexpr int FEW_WAVES = 4;
 constexpr int FEW_LDS = 39 << 10;              // four workgroups a compute unit
 constexpr int FEW_PAD = 80;                    // floats from one row of sums to the next: four rows on other banks
 
@@ -26,6 +26,7 @@ struct QgFewArgs {
     int parts;
     int tile_rows;             // rows of X a workgroup takes
     int stride;                // SELF: bytes from one operand row to the next
+    int waves;                 // of a workgroup: 4, or 8
     int tile_shift;            // logarithm of a workgroup's tiles
     int g32, gshift;           // group / 32, its logarithm or -1
     int quanta;                // times 128 k
@@ -45,8 +46,8 @@ struct FewWeights {
 };
 
 // RING: how many times 128 k are under way.
-template <int BITS, int GP, int RING, bool SELF>
-__global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs f)
+template <int BITS, int GP, int RING, int WAVES, bool SELF>
+__global__ __launch_bounds__(64 * WAVES, 4) void experts_few(const QgFewArgs f)
 {
     using F = Fmt<BITS>;
     using Weights = FewWeights<BITS, GP>;
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
     const int expert = __builtin_amdgcn_readfirstlane(t.expert), rows = __builtin_amdgcn_readfirstlane(t.rows);
     const int64_t begin = __builtin_amdgcn_readfirstlane((int)t.begin);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tiles = 1 << f.tile_shift, tile = wave & (tiles - 1), slices = FEW_WAVES >> f.tile_shift, slice = wave >> f.tile_shift;
+    const int tiles = 1 << f.tile_shift, tile = wave & (tiles - 1), slices = WAVES >> f.tile_shift, slice = wave >> f.tile_shift;
 
     // this lane's output
     const int width_shift = 6 - a.gated, tile_columns = 1 << width_shift;
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
         for (int i = 0; i < 4; ++i) xs[i] = *(const uint4 *)(x + ((int64_t)min(q0, f.quanta - 1) * 4 + i) * 64);
     }
     if constexpr (SELF) {
-        __shared__ uint32_t mosts[FEW_WAVES];
+        __shared__ uint32_t mosts[WAVES];
         for (int r = 0; r < rows; ++r) {
             int64_t from = a.rows ? a.rows[begin + r] : begin + r;
             const bool real = from >= 0 && from < a.x_rows;
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
             };
             uint32_t most = 0;
             if (a.x_type != QG_F16) {
-                for (int k = threadIdx.x * OCT; k < a.K; k += 64 * FEW_WAVES * OCT) {
+                for (int k = threadIdx.x * OCT; k < a.K; k += 64 * WAVES * OCT) {
                     take(k);
 #pragma unroll
                     for (int e = 0; e < OCT; ++e) most = max(most, magnitude_bits(p[e]));
@@ -145,11 +146,13 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
                 if (r > 0) __syncthreads();
                 if (lane == 0) mosts[wave] = most;
                 __syncthreads();
-                most = max(max(mosts[0], mosts[1]), max(mosts[2], mosts[3]));
+                most = mosts[0];
+#pragma unroll
+                for (int w = 1; w < WAVES; ++w) most = max(most, mosts[w]);
             }
             const int row_up = a.x_type == QG_F16 ? 0 : row_exponent(most);
             if (row_of == r) up = row_up;
-            for (int k = threadIdx.x * OCT; k < f.quanta * 128; k += 64 * FEW_WAVES * OCT) {
+            for (int k = threadIdx.x * OCT; k < f.quanta * 128; k += 64 * WAVES * OCT) {
                 take(k);
                 store_piece<BITS>(p, a.x_type, row_up, smem + r * f.parts * f.stride, f.stride, k);
             }
@@ -220,7 +223,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
     }
     __syncthreads();
     const int wide_shift = width_shift + f.tile_shift, wide = 1 << wide_shift;
-    for (int i = threadIdx.x; i < rows * wide; i += 64 * FEW_WAVES) {
+    for (int i = threadIdx.x; i < rows * wide; i += 64 * WAVES) {
         const int r = i >> wide_shift, col = i & (wide - 1);
         auto total = [&](int output) {
             float sum = 0.0f;
@@ -235,26 +238,28 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 4) void experts_few(const QgFewArgs
     }
 }
 
-template <int BITS, bool SELF>
+template <int BITS, int WAVES, bool SELF>
 void few_typed(const QgFewArgs &f, hipStream_t st)
 {
     constexpr int RING = 2;
-    constexpr size_t of_sums = FEW_WAVES * 16 * FEW_PAD * 4;
+    constexpr size_t of_sums = WAVES * 16 * FEW_PAD * 4;
     const size_t of_rows = (size_t)f.tile_rows * f.parts * f.stride, lds = SELF && of_rows > of_sums ? of_rows : of_sums;
-    if (f.gshift < 0) experts_few<BITS, 0, RING, SELF><<<f.blocks, 64 * FEW_WAVES, lds, st>>>(f);
-    else if (f.g32 % 4 == 0) experts_few<BITS, 4, RING, SELF><<<f.blocks, 64 * FEW_WAVES, lds, st>>>(f);
-    else if (f.g32 == 2) experts_few<BITS, 2, RING, SELF><<<f.blocks, 64 * FEW_WAVES, lds, st>>>(f);
-    else experts_few<BITS, 1, RING, SELF><<<f.blocks, 64 * FEW_WAVES, lds, st>>>(f);
+    if (f.gshift < 0) experts_few<BITS, 0, RING, WAVES, SELF><<<f.blocks, 64 * WAVES, lds, st>>>(f);
+    else if (f.g32 % 4 == 0) experts_few<BITS, 4, RING, WAVES, SELF><<<f.blocks, 64 * WAVES, lds, st>>>(f);
+    else if (f.g32 == 2) experts_few<BITS, 2, RING, WAVES, SELF><<<f.blocks, 64 * WAVES, lds, st>>>(f);
+    else experts_few<BITS, 1, RING, WAVES, SELF><<<f.blocks, 64 * WAVES, lds, st>>>(f);
 }
 
 template <int BITS>
 void few_launch(const QgFewArgs &f, const QgPrepareArgs &p, hipStream_t st)
 {
     if (f.stride) {
-        few_typed<BITS, true>(f, st);
+        if (f.waves == 4) few_typed<BITS, 4, true>(f, st);
+        else few_typed<BITS, 8, true>(f, st);
     } else {
         prepare_launch<BITS>(p, st);
-        few_typed<BITS, false>(f, st);
+        if (f.waves == 4) few_typed<BITS, 4, false>(f, st);
+        else few_typed<BITS, 8, false>(f, st);
     }
 }
 

@@ -63,17 +63,19 @@ def most_tiles(slots, experts, rows):
 
 PRODUCTS = [
     # slots, experts, N, K, bits, group, type, gated: kernels, slots of a tile, columns of a workgroup
-    (2, 8, 22016, 4096, 4, 128, F32, 1, [("experts_few", [4, 4, 2, 1])], None),                           # a row for each expert that is used
-    (2, 8, 22016, 1 << 16, 4, 128, F32, 1, [("prepare_rows", [4, 256]), ("experts_few", [4, 4, 2, 0])], None),
-    (96, 32, 4096, 1408, 3, 64, F32, 0, [("prepare_rows", [3, 256]), ("experts_few", [3, 2, 2, 0])], 8),
-    (96, 32, 4096, 1440, 2, 96, BF16, 0, [("prepare_rows", [2, 256]), ("experts_few", [2, 0, 2, 0])], 16),
-    (366, 64, 2816, 2048, 4, 32, BF16, 1, [("prepare_rows", [4, 256]), ("experts_few", [4, 1, 2, 0])], 16),
+    (2, 8, 22016, 4096, 4, 128, F32, 1, [("experts_few", [4, 4, 2, 4, 1])], None),                           # a row for each expert that is used
+    (2, 8, 22016, 1 << 16, 4, 128, F32, 1, [("prepare_rows", [4, 256]), ("experts_few", [4, 4, 2, 4, 0])], None),
+    (96, 32, 4096, 1408, 3, 64, F32, 0, [("prepare_rows", [3, 256]), ("experts_few", [3, 2, 2, 4, 0])], 8),
+    (96, 32, 4096, 1440, 2, 96, BF16, 0, [("prepare_rows", [2, 256]), ("experts_few", [2, 0, 2, 4, 0])], 16),
+    (366, 64, 2816, 2048, 4, 32, BF16, 1, [("prepare_rows", [4, 256]), ("experts_few", [4, 1, 2, 4, 0])], 16),
     (8192, 8, 22016, 4096, 4, 128, BF16, 1, [("prepare_rows", [4, 64]), ("experts_many", [4, 4, 1, 2])], 64),
     (1280, 32, 4096, 4096, 4, 64, F32, 1, [("prepare_rows", [4, 256]), ("experts_many", [4, 2, 2, 1])], 32),
     (8184, 60, 5120, 1792, 2, 64, F16, 0, [("prepare_rows", [2, 64]), ("experts_many", [2, 2, 1, 2])], 64),
     (719, 2, 5130, 160, 4, 32, F32, 0, [("prepare_rows", [4, 256]), ("experts_many", [4, 1, 2, 2])], 64),
     (173, 5, 7170, 192, 3, 64, F32, 0, [("prepare_rows", [3, 256]), ("experts_many", [3, 2, 2, 1])], 32),
-    (300, 2, 1000, 8192, 4, 128, BF16, 0, [("prepare_rows", [4, 256]), ("experts_few", [4, 4, 2, 0])], 16),
+    (300, 2, 1000, 8192, 4, 128, BF16, 0, [("prepare_rows", [4, 256]), ("experts_few", [4, 4, 2, 8, 0])], 16),
+    (4, 32, 2816, 4096, 4, 64, F32, 1, [("experts_few", [4, 2, 2, 8, 1])], 2),                              # not many workgroups: eight wavefronts each
+    (16, 8, 4096, 4096, 4, 128, BF16, 0, [("prepare_rows", [4, 256]), ("experts_few", [4, 4, 2, 8, 0])], 16),
     (9, 4, 128, 320, 4, 40, F32, 0, [("experts_any", [4, 0])], 4),
     (9, 4, 1 << 24, 1 << 16, 4, 128, F32, 1, [("experts_any", [4, 0])], 4),                               # ups too far behind the gates
 ]
@@ -91,7 +93,8 @@ def test_products_take_the_kernels_that_are_meant(tmp_path, slots, experts, N, K
             assert x * y >= most_tiles(slots, experts, tile) * -(-columns // across)
         else:                                  # 1, 2 or 4 tiles of 64 outputs
             assert x % most_tiles(slots, experts, tile) == 0
-            assert x // most_tiles(slots, experts, tile) in [-(-columns // (w * (32 if gated else 64))) for w in (1, 2, 4)]
+            wide = [-(-columns // (w * (32 if gated else 64))) for w in (1, 2, 4)]
+            assert x // most_tiles(slots, experts, tile) in wide and lanes == 64 * template[3]
 
 
 @pytest.mark.parametrize("tokens,top_k,experts,kernels", [(1, 1, 1, ["plan"]), (48, 4, 32, ["plan"]), (2048, 8, 1024, ["plan"]), (16383, 8, 192, ["plan_count", "plan", "plan_tokens"]),

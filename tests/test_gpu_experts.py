@@ -290,9 +290,35 @@ WIDE = [
     (3590 * 2, 192, 2, 64, [40, 33, 2, 64, 31], True, F16, F16, True, 0),
     (7170, 256, 2, 128, [40, 33, 2, 64, 31], False, BF16, F32, True, 0),
 ]
+# many experts of few rows: workgroups of four wavefronts, one, two and four tiles of outputs each, with and without a conversion of rows of its own
+def some(E, often, most):
+    return [(7 * e * e + e) % (most + 1) if e % often == 0 else 0 for e in range(E)]
 
 
-@pytest.mark.parametrize("N,K,bits,group,counts,gated,xt,yt,given,gap", PRODUCTS + WIDE)
+FEW = [
+    (2050, 160, 4, 32, some(24, 1, 7), False, F32, F32, True, 0),
+    (2050 * 2, 192, 4, 64, some(24, 1, 12), True, BF16, BF16, True, 8),
+    (2050, 288, 4, 96, some(24, 1, 9), False, F16, F32, True, 0),
+    (2050, 256, 4, 128, some(60, 1, 5), False, F32, F32, True, 0),
+    (2050, 96, 3, 32, some(60, 1, 5), False, BF16, F32, True, 0),
+    (1030 * 2, 192, 3, 64, some(60, 1, 5), True, F32, F32, True, 0),
+    (2050, 128, 3, 128, some(100, 1, 5), False, F16, F16, False, 0),
+    (1030 * 2, 96, 2, 32, some(100, 1, 5), True, F32, F32, True, 0),
+    (2050, 192, 2, 64, some(100, 1, 5), False, BF16, F32, True, 0),
+    (2050, 96, 2, 96, some(24, 1, 9), False, F32, F32, True, 0),
+    (2050, 352, 4, 32, some(60, 3, 2), False, F32, F32, True, 8),
+    (1030 * 2, 192, 4, 64, some(60, 3, 2), True, BF16, F32, True, 8),
+    (2050, 256, 4, 128, some(60, 4, 3), False, F16, F32, True, 0),
+    (2050, 160, 3, 32, some(60, 4, 3), False, F32, BF16, True, 0),
+    (2050, 288, 3, 96, some(60, 4, 3), False, BF16, F32, False, 0),
+    (2050, 160, 2, 32, some(60, 4, 3), False, F32, F32, True, 0),
+    (1030 * 2, 320, 2, 64, some(60, 4, 3), True, F16, F16, True, 0),
+    (64, 9600, 4, 128, [0, 1, 0, 0, 2, 0, 0, 0], False, F32, F32, True, 0),       # rows too long for a workgroup's own conversion of two
+    (64, 4992, 2, 64, [0, 1, 0, 0, 2, 0, 0, 1], False, F32, F32, True, 0),        # ... of three
+]
+
+
+@pytest.mark.parametrize("N,K,bits,group,counts,gated,xt,yt,given,gap", PRODUCTS + WIDE + FEW)
 def test_products_match_64_bits(qg, N, K, bits, group, counts, gated, xt, yt, given, gap):
     case("product", N, K, bits, group, counts[:6], gated, xt, yt, given)
     g = gen(N + K + len(counts))
