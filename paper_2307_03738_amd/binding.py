@@ -832,6 +832,15 @@ def _matrix_rows(t: torch.Tensor, name: str, shape=None, types=_FLOATS):
     return t.data_ptr(), stride, kind
 
 
+def _stream_of(*tensors) -> int:
+    """The current stream of the current device, which all of a call's tensors have to lie on."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"expected tensors on the current device ({device}), got one on {t.device}")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def qg_route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = None, score: str = "softmax", groups: int = 1,
              top_groups: Optional[int] = None, group_best: int = 1, renormalise: bool = True, scale: float = 1.0,
              ids: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None):
@@ -855,7 +864,7 @@ def qg_route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = No
     else:
         _whole(weights, torch.float32, "weights", shape)
     rc = (_LIB or lib()).qg_route(_ROUTE(lp, bp, ids.data_ptr(), weights.data_ptr(), tokens, stride, kind, experts, top_k, _SCORES[score],
-                                         groups, groups if top_groups is None else top_groups, group_best, 1 if renormalise else 0, scale), _stream())
+                                         groups, groups if top_groups is None else top_groups, group_best, 1 if renormalise else 0, scale), _stream_of(logits, bias, ids, weights))
     if rc != 0:
         _check(rc, "qg_route")
     return ids, weights
@@ -878,7 +887,8 @@ def qg_expert_plan(ids: torch.Tensor, experts: int, out=None):
         _whole(offsets, torch.int32, "offsets", (experts + 1,))
         _whole(slot_tokens, torch.int32, "slot_tokens", (tokens * top_k,))
         _whole(slots, torch.int32, "slots", shape)
-    rc = (_LIB or lib()).qg_expert_plan(ip, tokens, top_k, experts, offsets.data_ptr(), slot_tokens.data_ptr(), slots.data_ptr(), _stream())
+    rc = (_LIB or lib()).qg_expert_plan(ip, tokens, top_k, experts, offsets.data_ptr(), slot_tokens.data_ptr(), slots.data_ptr(),
+                                       _stream_of(ids, offsets, slot_tokens, slots))
     if rc != 0:
         _check(rc, "qg_expert_plan")
     return offsets, slot_tokens, slots
@@ -916,9 +926,12 @@ def qg_experts_product(packed: torch.Tensor, N: int, K: int, bits: int, group: i
     L = _LIB or lib()
     if workspace is None:
         workspace = _bytes(max(256, L.qg_experts_workspace_bytes(x_rows, K, kind)), x.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor")
     rc = L.qg_experts_product(_EXPERTS(packed.data_ptr(), xp, op, rp, y.data_ptr(), N, K, packed.stride(0), x_rows, xs, slots,
                                        bits, group, experts, kind, ykind, 1 if gated else 0,
-                                       workspace.data_ptr(), workspace.numel() * workspace.element_size()), _stream())
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size()),
+                              _stream_of(packed, x, offsets, rows, y, workspace))
     if rc != 0:
         _check(rc, "qg_experts_product")
     return y
@@ -949,7 +962,8 @@ def qg_experts_combine(y: torch.Tensor, slots: torch.Tensor, weights: torch.Tens
         if residual.dtype is not dtype:
             raise ValueError(f"residual: expected a {dtype} tensor")
         rp, rs, _ = _matrix_rows(residual, "residual", (tokens, N))
-    rc = (_LIB or lib()).qg_experts_combine(_COMBINE(y.data_ptr(), sp, wp, rp, out.data_ptr(), y_rows, tokens, N, rs, kind, okind, top_k), _stream())
+    rc = (_LIB or lib()).qg_experts_combine(_COMBINE(y.data_ptr(), sp, wp, rp, out.data_ptr(), y_rows, tokens, N, rs, kind, okind, top_k),
+                                           _stream_of(y, slots, weights, residual, out))
     if rc != 0:
         _check(rc, "qg_experts_combine")
     return out

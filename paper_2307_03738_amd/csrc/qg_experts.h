@@ -63,6 +63,7 @@ __device__ inline ExpertTile expert_tile(const QgExpertsArgs &a, int64_t tile, i
             const int b = __shfl((int)begin, at), n = __shfl((int)count, at);
             t.begin = b + (tile - first) * most;
             const int64_t left = n - (tile - first) * most;
+            if (left <= 0 || left > n) return {0, 0, 0};         // (offsets that decrease, whose tiles do not add up in 32 bits)
             t.rows = (int)(left < most ? left : most);
             return t;
         }

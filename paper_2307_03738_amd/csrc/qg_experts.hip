@@ -6,9 +6,6 @@ namespace {
 
 constexpr int ANY_ROWS = 4;
 
-template <int TYPE>
-__device__ inline void eight_of(const char *x, int64_t at, float *v) { load_eight<TYPE>(x, at, v); }
-
 // Codes of a cell less its zero-point, exact.
 template <int BITS>
 __device__ inline void cell_weights(const uint4 (&v)[Fmt<BITS>::PLANES], int j, float zero, float *w)
@@ -75,7 +72,7 @@ __global__ __launch_bounds__(256) void experts_any(QgExpertsArgs a)
 #pragma unroll
                     for (int o = 0; o < CELL; o += 8) {
                         float x[8];
-                        eight_of<TYPE>(a.x, from[r] + k + o, x);
+                        load_eight<TYPE>(a.x, from[r] + k + o, x);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(w[o + i], x[i], sum);
                     }

@@ -27,21 +27,6 @@ template <int BITS> constexpr int words_of_32() { return BITS == 2 ? 2 : 4; }
 // fields of a 16-bit half that a word, shifted by 8 or not, is read with
 template <int BITS> constexpr int zero_constants() { return BITS == 2 ? 4 : 2; }
 
-// Position of k (0 ... 31) in the operands of 32 k: lanes of quarter position / 8, their element position % 8.
-template <int BITS>
-__device__ inline int k_position(int k)
-{
-    if constexpr (BITS == 2) {                 // quarter = word and upper or lower four fields of its bytes 0, 2 or 1, 3
-        const int w = k >> 4, r = k & 15;
-        return (2 * w + ((r & 7) >> 2)) * 8 + 2 * (r & 3) + (r >> 3);
-    } else if constexpr (BITS == 4) {
-        return (k & 24) + 2 * (k & 3) + ((k >> 2) & 1);
-    } else {                                   // byte b: code b below, code 4 + b above
-        const int c = k & 7;
-        return (k & 24) + 4 * (c & 1) + 2 * (c >> 2) + ((c & 3) >> 1);
-    }
-}
-
 struct HalfConst {
     uint32_t mask[4], magic;
 };

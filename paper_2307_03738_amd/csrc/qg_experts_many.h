@@ -217,7 +217,6 @@ __global__ __launch_bounds__(256, MOST == 1 ? 3 : 2) void experts_many(const QgM
     const int64_t column0 = (int64_t)(8 * band + rest % across) * (f.e.gated ? 128 : 256);
     if (rows <= 32) many_rows<BITS, GP, PARTS, 1>(f, u, column0, smem, ups);
     else if constexpr (MOST == 2) many_rows<BITS, GP, PARTS, 2>(f, u, column0, smem, ups);
-
 }
 
 template <int BITS, int GP, int PARTS, int MOST>

@@ -17,13 +17,16 @@ namespace {
 
 // Position of k (0 ... 31) in two operands of 16 k: operand position / 16, lanes of half position / 8 % 2, element position % 8.
 template <int BITS>
-__device__ inline int k_position_32(int k)
+__device__ inline int k_position(int k)
 {
-    if constexpr (BITS == 2) {
+    if constexpr (BITS == 2) {                 // word, and upper or lower four fields of its bytes 0, 2 or 1, 3
         const int w = k >> 4, r = k & 15;
         return ((r & 7) >> 2) * 16 + w * 8 + 2 * (r & 3) + (r >> 3);
-    } else {
-        return k_position<BITS>(k);
+    } else if constexpr (BITS == 4) {
+        return (k & 24) + 2 * (k & 3) + ((k >> 2) & 1);
+    } else {                                   // byte b: code b below, code 4 + b above
+        const int c = k & 7;
+        return (k & 24) + 4 * (c & 1) + 2 * (c >> 2) + ((c & 3) >> 1);
     }
 }
 
@@ -50,7 +53,7 @@ __device__ inline void store_piece(const float *v, int type, int up, char *row, 
     char *to = row + (BITS == 2 ? (k & ~31) + (k >> 1 & 8) : k) * 2;
     float h[2 * OCT];
 #pragma unroll
-    for (int e = 0; e < OCT; ++e) h[k_position_32<BITS>(e)] = type == QG_F16 ? v[e] : __builtin_amdgcn_ldexpf(v[e], up);
+    for (int e = 0; e < OCT; ++e) h[k_position<BITS>(e)] = type == QG_F16 ? v[e] : __builtin_amdgcn_ldexpf(v[e], up);
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
         if (part == 0 || type == QG_F32) {

@@ -375,8 +375,11 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void plan(PlanArgs a)
         const int before = __popcll(same & ((1ull << lane) - 1));
         int slot = -1;
         if (real) slot = places[id] + before;
+        // all of the wavefront have read before the first of each expert writes, and it has written before the next 64 read
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         if (real && before == 0) places[id] += __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         if (i < w1) a.slots[i] = slot;
         if (real && !a.counted) a.slot_tokens[slot] = (int32_t)(i / (uint32_t)a.top_k);

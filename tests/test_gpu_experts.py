@@ -542,3 +542,21 @@ def test_refused_tensors(qg):
         qg.qg_expert_plan(torch.zeros(2, 2, dtype=torch.int64, device="cuda"), 4)
     with pytest.raises(ValueError):
         qg.qg_experts_combine(x, torch.zeros(2, 2, dtype=torch.int32, device="cuda"), torch.ones(2, 3, device="cuda"))
+
+
+def test_tensors_that_the_current_device_does_not_hold_are_refused(qg, monkeypatch):
+    packed, _ = blobs(qg, 2, 64, 128, 4, 64, 1)
+    x, offsets = torch.randn(4, 128).cuda(), torch.tensor([0, 2, 4], dtype=torch.int32).cuda()
+    need = qg.qg_experts_workspace_bytes(4, 128)
+    for workspace in (torch.empty(need, dtype=torch.uint8), torch.empty(1, dtype=torch.uint8, device="cuda").expand(need)):
+        with pytest.raises(ValueError):
+            qg.qg_experts_product(packed, 64, 128, 4, 64, x, offsets, workspace=workspace)
+    ids, weights = qg.qg_route(torch.randn(4, 2).cuda(), 1)
+    _, rows, slots = qg.qg_expert_plan(ids, 2)
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)          # the calls see a current device that none of the tensors is on
+    calls = (lambda: qg.qg_route(x, 1), lambda: qg.qg_expert_plan(ids, 2), lambda: qg.qg_experts_product(packed, 64, 128, 4, 64, x, offsets, rows=rows),
+             lambda: qg.qg_experts_combine(x, slots, weights))
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()
