@@ -102,6 +102,8 @@ ROUTES = [
     (9, 511, 33, BF16, "softmax", False, 1, 1, 1, False, 1.0, 0),
     (5, 1024, 64, F32, "sigmoid", True, 128, 9, 2, True, 1.0, 0),
     (4, 1000, 12, F16, "softmax", False, 1000, 12, 1, True, 1.0, 8),
+    (6, 1024, 5, F32, "softmax", True, 1024, 9, 2, True, 1.0, 0),
+    (7, 256, 32, BF16, "sigmoid", True, 256, 40, 1, False, 1.0, 0),
     (300, 8, 8, F16, "softmax", False, 1, 1, 1, True, 1.0, 0),
     (65, 16, 4, F32, "sigmoid", False, 4, 4, 2, False, 3.0, 0),
 ]
@@ -560,3 +562,64 @@ def test_tensors_that_the_current_device_does_not_hold_are_refused(qg, monkeypat
     for call in calls:
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+# --- distances past 32 bits -------------------------------------------------------------------------------------
+
+def test_route_past_32_bits(qg):
+    case("route far", 1200001, 1900)
+    logits = torch.zeros(1200001, 1900, dtype=BF16, device="cuda")
+    last = torch.randn(5, 64, generator=gen(1)).to(BF16)
+    logits[-5:, :64] = last.cuda()
+    ids, weights = qg.qg_route(logits[:, :64], 6)
+    want, w = plain_route(last, 6, None, "softmax", 1, 1, 1, True, 1.0)
+    assert torch.equal(ids[-5:].cpu(), want)
+    near(weights[-5:].cpu(), w, 2 * U * w.abs(), F32)
+    assert (ids[:-5] == torch.arange(6, device="cuda")).all()
+
+
+@pytest.mark.parametrize("counts", [[2], [40]])
+def test_experts_past_32_bits(qg, counts):
+    case("experts far", counts)
+    N, K, group, E = 96, 256, 64, 700
+    one, W = blobs(qg, 1, N, K, 4, group, 4)
+    packed = torch.empty(E, 7 << 20, dtype=torch.uint8, device="cuda")
+    packed[E - 1, : one.shape[1]] = one[0]
+    x = torch.randn(counts[0], K, generator=gen(5))
+    offsets = [0] * E + counts
+    y = qg.qg_experts_product(packed, N, K, 4, group, x.cuda(), torch.tensor(offsets, dtype=torch.int32).cuda())
+    want, slack = product_want(W, x, [0] + counts, None, False, group)
+    near(y.cpu(), want, slack, F32)
+
+
+@pytest.mark.parametrize("E,N,slots", [(2, 4096, 600000), (1024, 220000, 10240)])
+def test_rows_past_32_bits(qg, E, N, slots):
+    # X's rows, those of its f16 parts and those of y: by the kernel of many rows and by that of few
+    case("rows far", E, N, slots)
+    K, group, stride, tokens = 32, 32, 8192, 300000
+    one, W = blobs(qg, 1, N, K, 4, group, 6)
+    packed = one.expand(E, one.shape[1]).contiguous()
+    x = torch.zeros(tokens, stride, dtype=BF16, device="cuda")[:, :K]
+    x[-1] = torch.randn(K, generator=gen(7)).to(BF16).cuda()
+    rows = torch.zeros(slots, dtype=torch.int32)
+    rows[-3:] = torch.tensor([tokens - 1, 0, tokens - 1])
+    offsets = torch.arange(E + 1) * slots // E
+    y = qg.qg_experts_product(packed, N, K, 4, group, x, offsets.int().cuda(), rows=rows.cuda())
+    want, slack = product_want(W, x[-1:].cpu(), [0, 1], None, False, group)
+    for at in (-3, -1):
+        near(y[at:][:1].cpu(), want, slack, BF16)
+    assert (y[-2] == 0).all() and not y[:-3].any()
+
+
+def test_sum_past_32_bits(qg):
+    case("sum far", 600000, 4096)
+    y = torch.empty(600000, 4096, dtype=BF16, device="cuda")
+    last = torch.randn(4, 4096, generator=gen(8)).to(BF16)
+    y[-4:] = last.cuda()
+    slots = torch.full((540000, 2), -1, dtype=torch.int32, device="cuda")
+    slots[-1], slots[-3] = torch.tensor([599999, 599996]), torch.tensor([599997, 599998])
+    out = qg.qg_experts_combine(y, slots, torch.tensor([0.25, 2.0], device="cuda").expand(540000, 2).contiguous())
+    for at, (a, b) in ((-1, (3, 0)), (-3, (1, 2))):
+        want, size = 0.25 * last[a].double() + 2 * last[b].double(), 0.25 * last[a].double().abs() + 2 * last[b].double().abs()
+        near(out[at].cpu(), want, 4 * U * size, BF16)
+    assert not out[:-3].any() and not out[-2].any()
