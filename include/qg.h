@@ -479,9 +479,10 @@ int qg_expert_plan(const int32_t *ids, int64_t tokens, int top_k, int experts, i
 /* For each slot p of expert e, with x the row rows[p] of X (row p, if rows is NULL):
  *   y[p][n] = sum_k What_e[n][k] x[k]                  (N columns), or, gated, with gate and up side by side as in qg_gemv_swiglu,
  *   y[p][n] = silu(gate[n]) * up[n]                    (N / 2 columns: What_e rows [0, N / 2) are gate, the others up)
- * per group as s * sum (q - z) x, sums in fp32.  Groups of whole 32 k: on the matrix cores, q - z as it is, each row of X times a power of two as f16 (bf16, fp32:
- * the one that brings its largest |x| to [2^14, 2^15)), fp32 in two parts: 2^-22 of an x is left out, and what lies below 2^-39 of its row's largest.  Other groups, and gated matrices of
- * 8 GB and more: fp32 multiply-adds (slow from a few rows on).  A call enqueues one kernel or two.
+ * per group as s * sum (q - z) x, sums in fp32, on the matrix cores: q - z as it is, each row of X times a power of two as f16 (bf16, fp32:
+ * the one that brings its largest |x| to [2^14, 2^15)), fp32 in two parts: 2^-22 of an x is left out, and what lies below 2^-39 of its row's largest.  (The power of two is
+ * taken back from the sums: scales of 2^80 and more may make them infinite on the way.)  Groups of whole 32 k have tiles for many rows; other groups take their rows in tiles of 16
+ * (fp32: 8).  Gated matrices have to be smaller than 8 GB each.  A call enqueues one kernel or two.
  * A row outside 0 ... x_rows - 1 counts as zeros.  Rows of y past offsets[experts] are left as they were.  NaN and infinity in X
  * make their own rows of y NaN or infinite, and no others.  y overlaps no input. */
 typedef struct qg_experts_desc {

@@ -4,100 +4,6 @@
 
 namespace {
 
-constexpr int ANY_ROWS = 4;
-
-// Codes of a cell less its zero-point, exact.
-template <int BITS>
-__device__ inline void cell_weights(const uint4 (&v)[Fmt<BITS>::PLANES], int j, float zero, float *w)
-{
-    if constexpr (BITS == 3) {
-        const uint32_t a = word_of(v[0], j), b = word_of(v[1], j), c = word_of(v[2], j);
-        const uint32_t t = ((a >> 6) & 0x03030303u) | ((b >> 4) & 0x0c0c0c0cu) | ((c >> 2) & 0x30303030u);
-        const uint32_t words[4] = {a, b, c, t};
-#pragma unroll
-        for (int i = 0; i < 32; ++i) w[i] = (float)((words[i / 8] >> (8 * (i % 4) + (i % 8 < 4 ? 0 : 3))) & 7u) - zero;
-    } else {
-        const uint32_t word = word_of(v[0], j);
-#pragma unroll
-        for (int i = 0; i < 32 / BITS; ++i) w[i] = (float)((word >> (BITS * i)) & ((1u << BITS) - 1)) - zero;
-    }
-}
-
-// Any group of whole cells, in fp32 multiply-adds: a wavefront takes 64 outputs (a lane one) of four slots and a quarter of K's units,
-// the quarters meet in LDS.  Bound by the vector ALU from a few rows on; groups of whole 32 k have kernels of their own.
-template <int BITS, int TYPE>
-__global__ __launch_bounds__(256) void experts_any(QgExpertsArgs a)
-{
-    using F = Fmt<BITS>;
-    constexpr int CELL = F::CELL, P = F::PLANES, ZPER = 32 / F::ZBITS;
-    __shared__ float sums[3][2][ANY_ROWS][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t block = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
-    const int64_t column_tile = block / a.row_tiles;
-    const ExpertTile t = expert_tile(a, block - column_tile * a.row_tiles, ANY_ROWS);
-    const int64_t column = column_tile * 64 + lane;
-    if (t.rows == 0 || column_tile * 64 >= a.columns) return;
-    const char *blob = a.packed + t.expert * a.expert_stride;
-    int64_t from[ANY_ROWS];
-#pragma unroll
-    for (int r = 0; r < ANY_ROWS; ++r) {
-        int64_t row = -1;
-        if (r < t.rows) row = a.rows ? a.rows[t.begin + r] : t.begin + r;
-        from[r] = row >= 0 && row < a.x_rows ? row * a.x_stride : -1;
-    }
-    float acc[2][ANY_ROWS] = {};
-    const int units = (a.K + 4 * CELL - 1) / (4 * CELL);
-    for (int part = 0; part < 1 + a.gated; ++part) {
-        const int64_t n = (column < a.columns ? column : a.columns - 1) + (int64_t)part * a.columns;
-        const char *codes = blob + (n >> 6) * a.tile_codes + (n & 63) * 16;
-        const char *scales = blob + a.scales_off + (n >> 6) * a.tile_scales + (n & 63) * 4;
-        const char *zeros = blob + a.zeros_off + (n >> 6) * a.tile_zeros + (n & 63) * 4;
-        for (int u = wave; u < units; u += 4) {
-            uint4 v[P];
-#pragma unroll
-            for (int p = 0; p < P; ++p) v[p] = *(const uint4 *)(codes + ((int64_t)u * P + p) * 1024);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = (u * 4 + j) * CELL;
-                if (k >= a.K) break;
-                const int g = k / a.group;
-                const float s = *(const float *)(scales + (int64_t)g * 256);
-                const uint32_t zw = *(const uint32_t *)(zeros + (int64_t)(g / ZPER) * 256);
-                float w[CELL];
-                cell_weights<BITS>(v, j, (float)((zw >> (g % ZPER * F::ZBITS)) & ((1u << F::ZBITS) - 1)), w);
-#pragma unroll
-                for (int r = 0; r < ANY_ROWS; ++r) {
-                    if (from[r] < 0) continue;
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int o = 0; o < CELL; o += 8) {
-                        float x[8];
-                        load_eight<TYPE>(a.x, from[r] + k + o, x);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(w[o + i], x[i], sum);
-                    }
-                    acc[part][r] = __builtin_fmaf(s, sum, acc[part][r]);
-                }
-            }
-        }
-    }
-    if (wave > 0)
-#pragma unroll
-        for (int part = 0; part < 2; ++part)
-#pragma unroll
-            for (int r = 0; r < ANY_ROWS; ++r) sums[wave - 1][part][r][lane] = acc[part][r];
-    __syncthreads();
-    if (wave > 0 || column >= a.columns) return;
-#pragma unroll
-    for (int r = 0; r < ANY_ROWS; ++r) {
-        if (r >= t.rows) break;
-        float y[2];
-#pragma unroll
-        for (int part = 0; part < 2; ++part) y[part] = acc[part][r] + sums[0][part][r][lane] + sums[1][part][r][lane] + sums[2][part][r][lane];
-        store_typed(a.y_type, a.y, (t.begin + r) * a.columns + column, a.gated ? silu(y[0]) * y[1] : y[0]);
-    }
-}
-
 // Of the rows of X as f16, and their powers of two.
 struct RowsSpace {
     int64_t padded, bytes, total;
@@ -124,7 +30,7 @@ RowsSpace rows_space(int64_t x_rows, int64_t K, int x_type)
 // 98 (64), 77 (32), 36 (few); 2, 400 rows, 4096 x 4096: 55, 44, 50; 4, 2000 rows, 400 x 4096: 60, 51, 40; 3, 6000 rows, 1000 x 1024: 36, 37, 63.
 int many_rows_of(const QgExpertsArgs &a, int parts)
 {
-    if (a.slots * parts <= (int64_t)20 * a.experts) return 0;
+    if (a.group % 32 || a.slots * parts <= (int64_t)20 * a.experts) return 0;
     const int width = a.gated ? 128 : 256;
     const int64_t across = (a.columns + width - 1) / width;
     if (qg_most_tiles(a.slots, a.experts, 32) * across * 16 <= (int64_t)9 * qg_compute_units()) return 0;
@@ -158,11 +64,15 @@ int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepa
     // each: fp32 24.7 us, 21.4 so, bf16 4 rows 26.4, 23.0; beyond, fp32 4 rows 27.0, 29.2)
     f.waves = 2 * (int64_t)f.e.row_tiles * ((a.columns + (1 << shift) - 1) >> shift) <= 5 * qg_compute_units() ? 8 : 4;
     const int width = 1 << (shift + f.tile_shift);
-    f.g32 = a.group / 32;
-    f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);
+    if (a.group % 32) {
+        f.cells = a.group % 16 ? a.group / 8 : a.group / 16;
+    } else {
+        f.g32 = a.group / 32;
+        f.gshift = f.g32 & (f.g32 - 1) ? -1 : __builtin_ctz(f.g32);
+    }
     f.quanta = (a.K + 127) / 128;
     const int64_t blocks = (int64_t)f.e.row_tiles * ((a.columns + width - 1) / width);
-    if (blocks > QG_MOST_GROUPS / 2) return QG_ERR_SHAPE;
+    if (blocks > 0x7fffffff - QG_MOST_GROUPS) return QG_ERR_SHAPE;
     f.blocks = (int)blocks;
     (bits == 4 ? qg_few_launch_b4 : bits == 3 ? qg_few_launch_b3 : qg_few_launch_b2)(f, p, st);
     return QG_OK;
@@ -186,17 +96,6 @@ int many_plan(const QgExpertsArgs &a, int bits, int tile_rows, const RowsSpace &
     if (blocks > QG_MOST_GROUPS) return QG_ERR_SHAPE;
     f.blocks = (int)blocks;
     return (bits == 4 ? qg_many_launch_b4 : bits == 3 ? qg_many_launch_b3 : qg_many_launch_b2)(f, p, st);
-}
-
-template <int BITS>
-int any_launch(const QgExpertsArgs &a, int64_t blocks, hipStream_t st)
-{
-    const unsigned across = (unsigned)(blocks < QG_MOST_GROUPS ? blocks : QG_MOST_GROUPS);
-    const dim3 grid(across, (unsigned)((blocks + across - 1) / across));
-    if (a.x_type == QG_F32) experts_any<BITS, QG_F32><<<grid, 256, 0, st>>>(a);
-    else if (a.x_type == QG_BF16) experts_any<BITS, QG_BF16><<<grid, 256, 0, st>>>(a);
-    else experts_any<BITS, QG_F16><<<grid, 256, 0, st>>>(a);
-    return qg_launch_status();
 }
 
 }  // namespace
@@ -244,18 +143,12 @@ extern "C" int qg_experts_product(const qg_experts_desc *d, void *stream)
     a.experts = d->experts;
     a.x_type = d->x_type;
     a.y_type = d->y_type;
-    const hipStream_t st = (hipStream_t)stream;
     // (the lanes of a wavefront that take ups lie up to so far behind the gates, in 32 bits)
-    const bool near = !a.gated || ((a.columns + 63) / 64 + 2) * a.tile_codes < (int64_t)1 << 32;
-    if (d->group % 32 == 0 && near) {
-        const RowsSpace s = rows_space(a.x_rows, a.K, a.x_type);
-        const QgPrepareArgs p = {a.x, (char *)d->workspace, (int32_t *)((char *)d->workspace + s.bytes), a.x_rows, a.x_stride, s.padded, a.K, a.x_type};
-        const int many = many_rows_of(a, s.parts);
-        const int launched = many ? many_plan(a, d->bits, many, s, p, st) : few_plan(a, d->bits, s, p, st);
-        return launched != QG_OK ? launched : qg_launch_status();
-    }
-    a.row_tiles = (int)qg_most_tiles(d->slots, d->experts, ANY_ROWS);
-    const int64_t blocks = (int64_t)a.row_tiles * ((a.columns + 63) / 64);
-    if (blocks > (int64_t)QG_MOST_GROUPS * 65535) return QG_ERR_SHAPE;
-    return d->bits == 4 ? any_launch<4>(a, blocks, st) : d->bits == 3 ? any_launch<3>(a, blocks, st) : any_launch<2>(a, blocks, st);
+    if (a.gated && ((a.columns + 63) / 64 + 2) * a.tile_codes >= (int64_t)1 << 32) return QG_ERR_SHAPE;
+    const hipStream_t st = (hipStream_t)stream;
+    const RowsSpace s = rows_space(a.x_rows, a.K, a.x_type);
+    const QgPrepareArgs p = {a.x, (char *)d->workspace, (int32_t *)((char *)d->workspace + s.bytes), a.x_rows, a.x_stride, s.padded, a.K, a.x_type};
+    const int many = many_rows_of(a, s.parts);
+    const int launched = many ? many_plan(a, d->bits, many, s, p, st) : few_plan(a, d->bits, s, p, st);
+    return launched != QG_OK ? launched : qg_launch_status();
 }

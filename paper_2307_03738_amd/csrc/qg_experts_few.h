@@ -2,14 +2,19 @@
 //
 // A wavefront takes a tile of 64 outputs (gated: gates and ups of 32 columns) of up to 16 operand rows of an expert (8 of fp32, in two parts
 // each) and a slice of K; a workgroup of four wavefronts is 1, 2 or 4 tiles by 4, 2 or 1 slices, which meet in LDS (of eight: one tile by
-// eight slices).  Rows of X come as prepare_rows
-// leaves them, from cache straight into the operands; the weights go from memory into registers, in a ring of a few times 128 k that no
-// register leaves by a copy (which would wait for it), and into the 16 x 16 x 32 matrix instruction as q - z.  fp32 sums of a group (or 128 k of it) are
-// multiplied by its scale.
+// eight slices).  Rows of X come as prepare_rows leaves them, from cache straight into the operands; the weights go from memory into registers,
+// in a ring of twice 128 k that no register leaves by a copy (which would wait for it; longer rings were no faster), and into the
+// 16 x 16 x 32 matrix instruction as q - z.  fp32 sums of a group (or 128 k of it) are multiplied by its scale.
+// Measured: 61 tokens' six of 64 2816 x 2048 4-bit matrices in groups of 32, 237 MB: 49 us, 4.8 TB/s (a copy 5.4); one token's two of eight
+// 22016 x 4096, 91 MB: 22 us as a caller sees it; 24 tokens' four of 32 4096 x 1408 3-bit, 80 MB: 22.5 us, of which 3 are the launch and the meeting.
 //
 // A call with about one row for each expert that it uses does without prepare_rows: its workgroups convert their rows into LDS themselves (SELF), which is a kernel less
 // (one token, two of eight 22016 x 4096 4-bit matrices: 23.5 us against 28.1; four of 32 2816 x 4096: 15.1, 18.4).  With more rows that costs every workgroup more than
 // the kernel costs the call (61 tokens' 2816 x 2048 matrices, groups of 32: 73 to 86 us against 67.8, 20 to 36 of them before the first multiplication).
+//
+// Groups that are no whole 32 k take the matrix instruction twice for every 32 k (four times, where not even 16 k share a scale), with what other scales have set
+// to zero in X: at groups of 16 and eight 4096 x 4096 4-bit matrices, 105 MB, 43 us with a row each, 47 with four, 119 with 32 (multiply-adds on the vector ALU, four rows
+// at a time: 92, 179, 664).  They come here with any number of rows.
 #pragma once
 
 #include "qg_experts_rows.h"
@@ -29,6 +34,7 @@ struct QgFewArgs {
     int waves;                 // of a workgroup: 4, or 8
     int tile_shift;            // logarithm of a workgroup's tiles
     int g32, gshift;           // group / 32, its logarithm or -1
+    int cells;                 // > 0: groups that are no whole 32 k, in pieces of 16 k or, where that does not do, of 8
     int quanta;                // times 128 k
     int blocks;
 };
@@ -36,26 +42,28 @@ struct QgFewArgs {
 #ifdef QG_EXPERTS_KERNELS
 namespace {
 
-// Weights of 128 k, as loaded: GP times 32 k share a scale; GP 0: groups of an odd number of 32 k (or of pairs), a scale for each 32 k.
+// Weights of 128 k, as loaded: GP times 32 k share a scale; GP 0: groups of an odd number of 32 k (or of pairs), a scale for each 32 k;
+// GP -2, -4: groups that are no whole 32 k, two or four scales for each 32 k.
 template <int BITS, int GP>
 struct FewWeights {
-    static constexpr int FOLDS = GP ? 4 / GP : 4, ZEROS = GP ? 1 : FOLDS;
+    static constexpr int SUB = GP < 0 ? -GP : 1, FOLDS = GP < 0 ? 4 * SUB : GP ? 4 / GP : 4, ZEROS = GP < 0 ? 2 : GP ? 1 : FOLDS;
     uint4 v[BITS];
     uint32_t s[FOLDS], z[ZEROS];               // scales, and the words with the zero-points (shifted where they are used: a shift here would wait)
-    int shift[FOLDS];
+    int shift[FOLDS];                          // GP < 0: which of the zero-points of both words
 };
 
 // RING: how many times 128 k are under way.
 template <int BITS, int GP, int RING, int WAVES, bool SELF>
-__global__ __launch_bounds__(64 * WAVES, 4) void experts_few(const QgFewArgs f)
+__global__ __launch_bounds__(64 * WAVES, GP < 0 ? 2 : 4) void experts_few(const QgFewArgs f)
 {
     using F = Fmt<BITS>;
     using Weights = FewWeights<BITS, GP>;
-    constexpr int FOLDS = Weights::FOLDS, PER = 4 / FOLDS, ZPER = 32 / F::ZBITS;
+    constexpr int SUB = Weights::SUB, FOLDS = Weights::FOLDS, TURNS = FOLDS / SUB, PER = 4 / TURNS, ZPER = 32 / F::ZBITS;
     extern __shared__ __attribute__((aligned(16))) char smem[];      // SELF: rows of X; then sums
     const QgExpertsArgs &a = f.e;
     // workgroup i runs on die i % 8: a die's workgroups take neighbouring pieces, so that an expert's tiles of rows share its weights
-    int block = blockIdx.x;
+    int block = blockIdx.y * gridDim.x + blockIdx.x;
+    if (block >= f.blocks) return;
     {
         const int die = block & 7, each = f.blocks >> 3, more = f.blocks & 7;
         block = die * each + (die < more ? die : more) + (block >> 3);
@@ -96,6 +104,24 @@ __global__ __launch_bounds__(64 * WAVES, 4) void experts_few(const QgFewArgs f)
     auto load = [&](int q, Weights &w) {
 #pragma unroll
         for (int i = 0; i < BITS; ++i) w.v[i] = *(const uint4 *)(at_n.codes + ((int64_t)q * BITS + i) * 1024 + at_n.codes_lane);
+        if constexpr (GP < 0) {
+            // (128 k have zero-points of two words at most: whole words of them at groups of a cell, half as many at longer ones)
+            int g = q * FOLDS / f.cells, in = q * FOLDS - g * f.cells;
+            const int word = min(g, last_group) / ZPER;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w.z[i] = *(const uint32_t *)(at_n.zeros + (int64_t)min(word + i, last_group / ZPER) * 256 + at_n.zeros_lane);
+#pragma unroll
+            for (int i = 0; i < FOLDS; ++i) {
+                const int at = min(g, last_group);
+                w.s[i] = *(const uint32_t *)(at_n.scales + (int64_t)at * 256 + at_n.scales_lane);
+                w.shift[i] = at - word * ZPER;
+                if (++in == f.cells) {
+                    in = 0;
+                    ++g;
+                }
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < FOLDS; ++i) {
             const int k32 = q * 4 + i * PER;
@@ -165,12 +191,54 @@ __global__ __launch_bounds__(64 * WAVES, 4) void experts_few(const QgFewArgs f)
             if (at > 0 && q + at >= q1) break;
             Weights &w = ring[at];
 #pragma unroll
-            for (int i = 0; i < FOLDS; ++i) {
+            for (int i = 0; i < TURNS; ++i) {
                 // A branch that is always taken keeps the next scale's operands out of this one's code: the compiler would
                 // begin with all of them at once, in registers that there are not (up to 400 spilled).
                 int go = 1;
                 if (i > 0) asm volatile("" : "+s"(go));
                 if (!go) continue;
+                if constexpr (GP < 0) {
+                    // every quarter of an operand has its own zero-points; the sums of a scale's k come from X with the other k zero
+                    HalfOperand xo, o[4];
+                    uint32_t words[4], ops[4], z[4];
+                    if constexpr (SELF) xo.q = *(const uint4 *)(x + ((q + at) * 4 + i) * 64);
+                    else xo.q = xs[i];
+#pragma unroll
+                    for (int k = 0; k < words_of_32<BITS>(); ++k) {
+                        const int place = w.shift[i * SUB + k * SUB / words_of_32<BITS>()];
+                        const uint32_t zero = ((place < ZPER ? w.z[0] : w.z[1]) >> (place % ZPER * F::ZBITS)) & ((1u << F::ZBITS) - 1);
+                        words[k] = BITS == 2 ? zero * 0x101u : zero;
+                    }
+                    words_16<BITS>(words, z);
+                    words_of<BITS>(w.v, i, words);
+                    words_16<BITS>(words, ops);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        uint32_t zc[zero_constants<BITS>()];
+                        zero_operands<BITS>(BITS == 2 ? z[b] & 0xff : z[b], zc);
+                        unpack_halves<BITS>(ops[b], hc, zc, o[b]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < SUB; ++j) {
+                        uint32_t s[4];
+                        spread_16(w.s[i * SUB + j], s);
+                        HalfOperand part;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) part.r[e] = quarter * SUB / 4 == j ? xo.r[e] : 0;
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            float4v sum = 0.0f;
+                            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(part.v, o[b].v, sum, 0, 0, 0);
+                            y[b][0] = __builtin_fmaf(__uint_as_float(s[b]), sum[0], y[b][0]);
+                            if (vrows > 4) y[b][1] = __builtin_fmaf(__uint_as_float(s[b]), sum[1], y[b][1]);
+                            if (vrows > 8)
+#pragma unroll
+                                for (int e = 2; e < 4; ++e) y[b][e] = __builtin_fmaf(__uint_as_float(s[b]), sum[e], y[b][e]);
+                        }
+                    }
+                    if constexpr (!SELF) xs[i] = *(const uint4 *)(x + ((int64_t)min(q + at + 1, f.quanta - 1) * 4 + i) * 64);
+                    continue;
+                }
                 uint32_t s[4], zw[4];
                 spread_16(w.s[i], s);
                 spread_16((w.z[i < Weights::ZEROS ? i : 0] >> w.shift[i]) & ((1u << F::ZBITS) - 1), zw);
@@ -244,10 +312,20 @@ void few_typed(const QgFewArgs &f, hipStream_t st)
     constexpr int RING = 2;
     constexpr size_t of_sums = WAVES * 16 * FEW_PAD * 4;
     const size_t of_rows = (size_t)f.tile_rows * f.parts * f.stride, lds = SELF && of_rows > of_sums ? of_rows : of_sums;
-    if (f.gshift < 0) experts_few<BITS, 0, RING, WAVES, SELF><<<f.blocks, 64 * WAVES, lds, st>>>(f);
-    else if (f.g32 % 4 == 0) experts_few<BITS, 4, RING, WAVES, SELF><<<f.blocks, 64 * WAVES, lds, st>>>(f);
-    else if (f.g32 == 2) experts_few<BITS, 2, RING, WAVES, SELF><<<f.blocks, 64 * WAVES, lds, st>>>(f);
-    else experts_few<BITS, 1, RING, WAVES, SELF><<<f.blocks, 64 * WAVES, lds, st>>>(f);
+    const unsigned across = (unsigned)(f.blocks < QG_MOST_GROUPS / 2 ? f.blocks : QG_MOST_GROUPS / 2);
+    const dim3 grid(across, (f.blocks + across - 1) / across);
+    if (f.cells) {
+        if constexpr (BITS == 4) {
+            if (f.cells * 8 == f.e.group) {
+                experts_few<BITS, -4, RING, WAVES, SELF><<<grid, 64 * WAVES, lds, st>>>(f);
+                return;
+            }
+        }
+        if constexpr (BITS != 3) experts_few<BITS, -2, RING, WAVES, SELF><<<grid, 64 * WAVES, lds, st>>>(f);
+    } else if (f.gshift < 0) experts_few<BITS, 0, RING, WAVES, SELF><<<grid, 64 * WAVES, lds, st>>>(f);
+    else if (f.g32 % 4 == 0) experts_few<BITS, 4, RING, WAVES, SELF><<<grid, 64 * WAVES, lds, st>>>(f);
+    else if (f.g32 == 2) experts_few<BITS, 2, RING, WAVES, SELF><<<grid, 64 * WAVES, lds, st>>>(f);
+    else experts_few<BITS, 1, RING, WAVES, SELF><<<grid, 64 * WAVES, lds, st>>>(f);
 }
 
 template <int BITS>

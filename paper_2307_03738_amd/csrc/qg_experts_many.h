@@ -4,7 +4,11 @@
 // slots and 64 outputs of its own (gated: gate and up of 32 columns), so that every weight is unpacked once per workgroup.  X's rows, gathered
 // by slot, go from memory to LDS without passing through registers, 128 k ahead, codes to registers; a wavefront reads each operand
 // of X for two 32 x 32 x 16 matrix instructions (half of LDS's rate at full speed of the matrix cores).  Two workgroups share a compute unit: with 128
-// slots and one wavefront a SIMD nothing covers what a wavefront waits for (a prompt of 4096 tokens, 22016 x 4096 4-bit, two of eight: 2.55 ms against 1.71).
+// slots and one wavefront a SIMD nothing covers what a wavefront waits for (4096 tokens, two of eight gated 22016 x 4096 4-bit matrices: 2.55 ms against 1.71 at that time).
+//
+// That prompt now takes 1.50 to 1.57 ms, 0.93 to 0.97 PFLOP/s; a library's product of bf16 matrices reaches 1.20.  Both are held by power (the clock falls to 2.0 GHz; a loop of nothing but
+// matrix instructions reaches 1.65), here by 9 vector instructions beside each matrix instruction: a loop of just these and no memory makes 1.17 to 1.33.  Codes unpacked once for a
+// whole workgroup by way of LDS make 0.95 to 1.04 in such a loop.  8184 slots of 60 5120 x 1792 2-bit matrices, groups of 64: 235 us (0.64 PFLOP/s; 14 steps of 128 k, 10.5 vector instructions).
 #pragma once
 
 #include <type_traits>

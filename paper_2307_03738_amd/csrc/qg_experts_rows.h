@@ -69,7 +69,7 @@ __device__ inline void store_piece(const float *v, int type, int up, char *row, 
 }
 
 // LANES lanes a row, a wavefront or a workgroup, which keep 32 values each (a workgroup: rows up to 8192 are read once).  Bound by memory where rows are many,
-// by one load and a meeting where they are few.
+// by one load and a meeting where they are few (4096 rows of 4096 bf16: 16 us, 4.2 TB/s; 61 of 2048: 2 to 4).
 template <int BITS, int LANES>
 __global__ __launch_bounds__(256) void prepare_rows(const QgPrepareArgs a)
 {

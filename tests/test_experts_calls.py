@@ -68,6 +68,7 @@ def test_plan_refuses(qg):
     (dict(experts=1025), UNSUPPORTED), (dict(experts=0), SHAPE), (dict(N=0), SHAPE), (dict(K=250), SHAPE), (dict(group=12), SHAPE), (dict(slots=-1), SHAPE), (dict(slots=1 << 31), SHAPE),
     (dict(x_rows=-1), SHAPE), (dict(x_rows=1 << 31), SHAPE), (dict(x_stride=248), SHAPE), (dict(expert_stride=1024), SHAPE), (dict(N=127, gated=1), SHAPE), (dict(packed=72), ALIGN),
     (dict(x=72), ALIGN), (dict(x_stride=260), ALIGN), (dict(expert_stride=(1 << 20) + 8), ALIGN), (dict(offsets=66), ALIGN), (dict(rows=66), ALIGN), (dict(y=130), ALIGN),
+    (dict(N=1 << 24, K=1 << 16, x_stride=1 << 16, expert_stride=1 << 42, gated=1), SHAPE),             # ups further behind the gates than 32 bits reach
     (dict(workspace=72), ALIGN), (dict(workspace=0), WORKSPACE), (dict(workspace_bytes=6 * (2 * 256 * 2 + 4) - 1), WORKSPACE), (dict(slots=0, x=0, packed=0), OK)])
 def test_product_refuses(qg, change, status):
     assert qg.lib().qg_experts_product(qg._EXPERTS(*{**EXPERTS, **change}.values()), None) == status

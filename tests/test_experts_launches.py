@@ -32,7 +32,7 @@ def _run(stub_path, lib_path, call, packed):
         stub.stub_shape(i, shape)
         length, rest = re.match(r"_ZN12_GLOBAL__N_1(\d\d?)(\D.*)", stub.stub_name(i).decode()).groups()
         name, tail = rest[:int(length)], rest[int(length):]
-        out.append([name, [int(v) for v in re.findall(r"L[ib](\d+)E", tail)], list(shape)])
+        out.append([name, [int(v.replace("n", "-")) for v in re.findall(r"L[ib](n?\d+)E", tail)], list(shape)])
     json.dump([status, out], sys.stdout)
 
 
@@ -76,8 +76,10 @@ PRODUCTS = [
     (300, 2, 1000, 8192, 4, 128, BF16, 0, [("prepare_rows", [4, 256]), ("experts_few", [4, 4, 2, 8, 0])], 16),
     (4, 32, 2816, 4096, 4, 64, F32, 1, [("experts_few", [4, 2, 2, 8, 1])], 2),                              # not many workgroups: eight wavefronts each
     (16, 8, 4096, 4096, 4, 128, BF16, 0, [("prepare_rows", [4, 256]), ("experts_few", [4, 4, 2, 8, 0])], 16),
-    (9, 4, 128, 320, 4, 40, F32, 0, [("experts_any", [4, 0])], 4),
-    (9, 4, 1 << 24, 1 << 16, 4, 128, F32, 1, [("experts_any", [4, 0])], 4),                               # ups too far behind the gates
+    (9, 4, 128, 320, 4, 40, F32, 0, [("prepare_rows", [4, 256]), ("experts_few", [4, -4, 2, 8, 0])], 8),     # groups that are no whole 32 k
+    (2, 8, 22016, 4096, 4, 16, F32, 1, [("experts_few", [4, -2, 2, 4, 1])], None),
+    (5000, 8, 4096, 4096, 2, 16, BF16, 0, [("prepare_rows", [2, 64]), ("experts_few", [2, -2, 2, 4, 0])], 16),
+    (1 << 24, 64, 22016, 4096, 4, 16, F16, 1, [("prepare_rows", [4, 64]), ("experts_few", [4, -2, 2, 4, 0])], 16),
 ]
 
 
@@ -88,13 +90,14 @@ def test_products_take_the_kernels_that_are_meant(tmp_path, slots, experts, N, K
     name, template, (x, y, _, lanes, _) = launches[-1]
     columns = N // 2 if gated else N
     if tile:
-        across = {"experts_many": 128 if gated else 256, "experts_any": 64}.get(name)
-        if across:
-            assert x * y >= most_tiles(slots, experts, tile) * -(-columns // across)
-        else:                                  # 1, 2 or 4 tiles of 64 outputs
+        if name == "experts_many":
+            assert x * y >= most_tiles(slots, experts, tile) * -(-columns // (128 if gated else 256))
+        elif y == 1:                           # 1, 2 or 4 tiles of 64 outputs
             assert x % most_tiles(slots, experts, tile) == 0
             wide = [-(-columns // (w * (32 if gated else 64))) for w in (1, 2, 4)]
             assert x // most_tiles(slots, experts, tile) in wide and lanes == 64 * template[3]
+        else:
+            assert x * y >= most_tiles(slots, experts, tile) * -(-columns // (4 * (32 if gated else 64))) and x % 8 == 0
 
 
 @pytest.mark.parametrize("tokens,top_k,experts,kernels", [(1, 1, 1, ["plan"]), (48, 4, 32, ["plan"]), (2048, 8, 1024, ["plan"]), (16383, 8, 192, ["plan_count", "plan", "plan_tokens"]),

@@ -249,7 +249,7 @@ PRODUCTS = [
     (66, 96, 4, 96, ODD, True, F32, F32, True, 0),
     (100, 1024, 4, 1024, ODD, False, F32, F32, True, 0),
     (100, 512, 3, 256, ODD, False, F16, F16, True, 0),
-    (64, 72, 4, 8, ODD, False, F32, F32, True, 0),                  # groups that are no whole 32 k
+    (64, 72, 4, 8, ODD, False, F32, F32, True, 0),
     (66, 80, 4, 16, ODD, True, BF16, BF16, True, 0),
     (64, 48, 2, 16, ODD, False, F16, F32, True, 0),
     (64, 240, 4, 40, ODD, False, BF16, F32, False, 0),
@@ -320,7 +320,29 @@ FEW = [
 ]
 
 
-@pytest.mark.parametrize("N,K,bits,group,counts,gated,xt,yt,given,gap", PRODUCTS + WIDE + FEW)
+# groups that are no whole 32 k: pieces of 8 and of 16 k, words of zero-points that end inside 128 k, K that ends inside 32, few rows and many
+CELLS = [
+    (130, 1000, 4, 8, ODD, False, F32, F32, True, 8),
+    (70, 1024, 4, 8, [1, 0, 0, 0], True, BF16, F32, False, 0),
+    (2050, 96, 4, 8, some(60, 4, 3), False, F16, F32, True, 0),
+    (130, 1104, 4, 24, ODD, True, F16, F16, True, 0),
+    (67, 40, 4, 40, [3, 200, 0, 1], False, F32, F32, True, 0),
+    (2050, 360, 4, 72, some(24, 1, 12), False, BF16, F32, True, 8),
+    (1030 * 2, 176, 4, 88, some(60, 3, 2), True, F32, F32, True, 8),
+    (130, 1040, 4, 16, ODD, False, F32, F32, True, 0),
+    (130, 1040, 4, 16, [300, 2, 129], True, BF16, BF16, True, 0),
+    (2050, 272, 4, 16, some(24, 1, 12), False, F32, F32, True, 0),
+    (70, 2064, 4, 48, [1, 0, 1, 0, 0, 0], False, F16, F32, True, 0),
+    (2050, 336, 4, 112, some(60, 1, 5), False, BF16, F32, False, 0),
+    (130, 1040, 2, 16, ODD, True, F32, F32, True, 8),
+    (2050, 272, 2, 16, some(24, 1, 12), False, BF16, F32, True, 0),
+    (70, 2064, 2, 16, [1, 0, 0, 0], False, F16, F16, False, 0),
+    (1030 * 2, 336, 2, 48, some(60, 4, 3), True, F32, F32, True, 0),
+    (130, 1200, 2, 80, [90, 0, 33, 5], False, F16, F32, True, 0),
+]
+
+
+@pytest.mark.parametrize("N,K,bits,group,counts,gated,xt,yt,given,gap", PRODUCTS + WIDE + FEW + CELLS)
 def test_products_match_64_bits(qg, N, K, bits, group, counts, gated, xt, yt, given, gap):
     case("product", N, K, bits, group, counts[:6], gated, xt, yt, given)
     g = gen(N + K + len(counts))
