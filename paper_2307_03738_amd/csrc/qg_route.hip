@@ -1,4 +1,6 @@
 // qg_route, qg_expert_plan, qg_experts_combine: what surrounds the experts' products.
+#include <type_traits>
+
 #include "qg_types.h"
 
 namespace {
@@ -18,48 +20,55 @@ struct RouteArgs {
 
 template <typename T> __device__ inline T lowest() { return (T)-__builtin_inff(); }
 
-// What lane ^ OFF holds, once lanes that differ in lower bits hold the same: inside a row of 16 lanes by the vector ALU (pairs, quads, mirrored halves and
-// rows), across rows by swaps.  (By way of LDS each step takes five times as long, and a choice is little else but such steps.)
+// v and what lane ^ OFF holds, in either order, once lanes that differ in lower bits hold the same: inside a row of 16 lanes by the vector ALU (pairs, quads, mirrored
+// halves and rows), across rows by swaps.  (By way of LDS each step takes five times as long, and a choice is little else but such steps.)
+template <typename T> struct Two { T a, b; };
 template <int OFF>
-__device__ inline uint32_t partner(uint32_t v)
+__device__ inline Two<uint32_t> both(uint32_t v)
 {
-    if constexpr (OFF == 1) return dpp<0xb1, 0xf>(v);
-    else if constexpr (OFF == 2) return dpp<0x4e, 0xf>(v);
-    else if constexpr (OFF == 4) return dpp<0x141, 0xf>(v);
-    else if constexpr (OFF == 8) return dpp<0x140, 0xf>(v);
+    if constexpr (OFF == 1) return {v, dpp<0xb1, 0xf>(v)};
+    else if constexpr (OFF == 2) return {v, dpp<0x4e, 0xf>(v)};
+    else if constexpr (OFF == 4) return {v, dpp<0x141, 0xf>(v)};
+    else if constexpr (OFF == 8) return {v, dpp<0x140, 0xf>(v)};
     else if constexpr (OFF == 16) {
         const auto x = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-        return threadIdx.x & 16 ? x[0] : x[1];
+        return {x[0], x[1]};
     } else {
         const auto x = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-        return threadIdx.x & 32 ? x[0] : x[1];
+        return {x[0], x[1]};
     }
 }
-template <int OFF> __device__ inline float partner(float v) { return __uint_as_float(partner<OFF>(__float_as_uint(v))); }
-template <int OFF> __device__ inline int partner(int v) { return (int)partner<OFF>((uint32_t)v); }
 template <int OFF>
-__device__ inline double partner(double v)
+__device__ inline Two<float> both(float v)
+{
+    const Two<uint32_t> t = both<OFF>(__float_as_uint(v));
+    return {__uint_as_float(t.a), __uint_as_float(t.b)};
+}
+template <int OFF>
+__device__ inline Two<double> both(double v)
 {
     const uint64_t bits = __builtin_bit_cast(uint64_t, v);
-    const uint32_t low = partner<OFF>((uint32_t)bits), high = partner<OFF>((uint32_t)(bits >> 32));
-    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+    const Two<uint32_t> low = both<OFF>((uint32_t)bits), high = both<OFF>((uint32_t)(bits >> 32));
+    return {__builtin_bit_cast(double, (uint64_t)high.a << 32 | low.a), __builtin_bit_cast(double, (uint64_t)high.b << 32 | low.b)};
 }
 
+// op is the same either way round
 template <int L, int OFF, typename T, typename OP>
 __device__ inline T team_all(T v, OP op)
 {
-    if constexpr (OFF < L) return team_all<L, 2 * OFF>(op(v, partner<OFF>(v)), op);
-    else return v;
+    if constexpr (OFF < L) {
+        const Two<T> t = both<OFF>(v);
+        return team_all<L, 2 * OFF>(op(t.a, t.b), op);
+    } else return v;
 }
+__device__ inline float larger(float a, float b) { return __builtin_fmaxf(a, b); }       // (neither is NaN)
+__device__ inline double larger(double a, double b) { return __builtin_fmax(a, b); }
+__device__ inline float smaller(float a, float b) { return __builtin_fminf(a, b); }
+__device__ inline double smaller(double a, double b) { return __builtin_fmin(a, b); }
 template <int L, typename T>
 __device__ inline T team_max(T v)
 {
-    return team_all<L, 1>(v, [](T a, T b) { return b > a ? b : a; });
-}
-template <int L>
-__device__ inline int team_min(int v)
-{
-    return team_all<L, 1>(v, [](int a, int b) { return min(a, b); });
+    return team_all<L, 1>(v, [](T a, T b) { return larger(a, b); });
 }
 template <int L, typename T>
 __device__ inline T team_sum(T v)
@@ -75,15 +84,45 @@ __device__ inline double inverse_of(double d)
     r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
     return d == __builtin_inf() ? 0.0 : r;
 }
-__device__ inline double sigmoid(float x) { return inverse_of(1.0 + exp(-(double)x)); }
+
+// e^y = 2^n e^r, r = y - n ln 2 of at most 0.347, by the series up to r^12 / 12! (what is left out is below 2e-16); y is not NaN.  Its coefficients
+// stay in scalar registers, one instruction each (as constants of the code they cost two moves more, and the choice of a prompt is bound by instructions).
+struct Series {
+    double c[11];
+    __device__ inline Series()
+    {
+        double f = 1.0;
+#pragma unroll
+        for (int i = 0; i < 11; ++i) {
+            f /= i + 2;
+            c[i] = f;
+            asm("" : "+s"(c[i]));
+        }
+    }
+    __device__ inline double exp(double y) const
+    {
+        y = __builtin_fmin(__builtin_fmax(y, -800.0), 800.0);
+        const double n = __builtin_rint(y * 1.4426950408889634);
+        double r = __builtin_fma(n, -0x1.62e42feep-1, y);              // ln 2 in two parts, of which the first times n is exact
+        r = __builtin_fma(n, -0x1.a39ef35793c76p-33, r);
+        double p = c[10];
+#pragma unroll
+        for (int i = 9; i >= 0; --i) p = __builtin_fma(p, r, c[i]);
+        p = __builtin_fma(p, r, 1.0);
+        p = __builtin_fma(p, r, 1.0);
+        return __builtin_amdgcn_ldexp(p, (int)n);
+    }
+    __device__ inline double sigmoid(float x) const { return inverse_of(1.0 + exp(-(double)x)); }
+};
 
 __device__ inline float logit_of(const RouteArgs &a, int64_t at)
 {
     return a.type == QG_F32 ? load_as_float<QG_F32>(a.logits, at) : a.type == QG_BF16 ? load_as_float<QG_BF16>(a.logits, at) : load_as_float<QG_F16>(a.logits, at);
 }
 
-// Bound by latency: a load, exponentials in fp64 where a weight or a rank needs them, and top_k steps of log2 L exchanges (one token, six of 64: 3.1 us, an empty launch 2.4;
-// 8190 tokens of bf16, seven of 192 in 12 groups, sigmoids and a bias: 15.3 us, 3.1 MB).  16 lanes a token where they suffice, so that four tokens share a wavefront's steps.
+// A few tokens are bound by latency: a load, exponentials in fp64 where a weight or a rank needs them, and top_k steps of log2 L exchanges (one token, six of 64: 3.0 us, an empty
+// launch 2.4).  Many are bound by instructions (8190 tokens of bf16, seven of 192 in 12 groups, sigmoids and a bias: 12.5 us, 1300 vector instructions a wavefront, 9 us of issue; 3.6 MB).  16 lanes a
+// token where they suffice, so that four tokens share a wavefront's steps.
 // L lanes take a token, V experts each: expert v * L + lane.  KEY: what experts rank by, fp32 logits, or, with a bias or
 // groups ranked by sums, scores in fp64 (two fp32 scores with a bias tie or swap in about one of 10^5 choices).
 template <int L, int V, typename KEY>
@@ -96,49 +135,69 @@ __global__ __launch_bounds__(256) void route(RouteArgs a)
     const int64_t token = wanted < a.tokens ? wanted : a.tokens - 1;      // lanes past the end work along and store nothing
     const int64_t row = token * a.stride;
 
-    float l[V];
+    // what a call asks for is asked once, not for each expert, and lanes past the last expert read it: all of a lane's experts are under way at once
+    int at[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) at[v] = min(v * L + lane, a.experts - 1);
+    float l[V], b[V];
+    auto read = [&](auto type) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) l[v] = load_as_float<decltype(type)::value>(a.logits, row + at[v]);
+    };
+    if (a.type == QG_F32) read(std::integral_constant<int, QG_F32>());
+    else if (a.type == QG_BF16) read(std::integral_constant<int, QG_BF16>());
+    else read(std::integral_constant<int, QG_F16>());
+    if constexpr (SCORES) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) b[v] = a.bias ? a.bias[at[v]] : 0.0f;
+    }
     bool nan = false;
     float most = lowest<float>();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int e = v * L + lane;
-        l[v] = e < a.experts ? logit_of(a, row + e) : lowest<float>();
-        if (l[v] != l[v]) {
-            nan = true;
-            l[v] = lowest<float>();
-        }
-        most = l[v] > most ? l[v] : most;
+        nan |= l[v] != l[v];
+        l[v] = l[v] != l[v] || v * L + lane >= a.experts ? lowest<float>() : l[v];
+        most = larger(most, l[v]);
     }
     // softmax: the largest logit and, where a weight needs it, the sum of exponentials; of infinite logits each counts 1 and the others 0
     const bool sums = !a.sigmoid && (SCORES || !a.renormalise);
     if (!a.sigmoid) most = team_max<L>(most);
-    const bool infinite = most == __builtin_inff();
-    auto raised = [&](float x) { return infinite ? (x == most ? 1.0 : 0.0) : x == lowest<float>() ? 0.0 : exp((double)x - (double)most); };
+    const float base = most == lowest<float>() ? 0.0f : most;
+    const Series series;
+    auto raised = [&](float x) { return series.exp(x == base ? 0.0 : (double)x - (double)base); };
     double total = 1.0;
     KEY key[V];
-    double part = 0.0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        if constexpr (SCORES) {
-            const double p = a.sigmoid ? sigmoid(l[v]) : raised(l[v]);
-            part += p;
-            key[v] = p;
-        } else {
-            key[v] = l[v];
-            if (sums) part += raised(l[v]);
-        }
-    }
-    if (sums) total = team_sum<L>(part);
     if constexpr (SCORES) {
+        if (a.sigmoid) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = series.sigmoid(l[v]);
+        } else {
+            double part = 0.0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                key[v] = raised(l[v]);
+                part += key[v];
+            }
+            total = team_sum<L>(part);
+            const double scale = inverse_of(total);     // (1 or more, or all are switched off)
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] *= scale;
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int e = v * L + lane;
-            if (!a.sigmoid) key[v] /= total;
-            if (a.bias && e < a.experts) key[v] += (double)a.bias[e];
-            if (l[v] == lowest<float>() || key[v] != key[v]) {
-                nan |= key[v] != key[v] && l[v] != lowest<float>();
-                key[v] = lowest<KEY>();
-            }
+            if (a.bias) key[v] += (double)b[v];
+            const bool off = l[v] == lowest<float>(), bad = key[v] != key[v];
+            nan |= bad && !off;
+            key[v] = off || bad ? lowest<KEY>() : key[v];
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = l[v];
+        if (sums) {
+            double part = 0.0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) part += raised(l[v]);
+            total = team_sum<L>(part);
         }
     }
     const uint64_t nans = __ballot(nan);
@@ -156,14 +215,11 @@ __global__ __launch_bounds__(256) void route(RouteArgs a)
         const int size = a.experts / a.groups;
         for (int g = lane; g < a.groups; g += L) {
             KEY first = lowest<KEY>(), second = lowest<KEY>();
+#pragma unroll 4
             for (int i = 0; i < size; ++i) {
                 const KEY k = keys[g * size + i];
-                if (k > first) {
-                    second = first;
-                    first = k;
-                } else if (k > second) {
-                    second = k;
-                }
+                second = larger(second, smaller(first, k));
+                first = larger(first, k);
             }
             ranks[g] = a.two && second > lowest<KEY>() ? first + second : first;
         }
@@ -201,26 +257,31 @@ __global__ __launch_bounds__(256) void route(RouteArgs a)
     for (int j = 0; j < a.top_k; ++j) {
         KEY best = key[0];
 #pragma unroll
-        for (int v = 1; v < V; ++v) best = key[v] > best ? key[v] : best;
-        best = team_max<L>(best);
-        if (!(best > lowest<KEY>())) {     // none is left for this token; others of the wavefront may go on
-            best = lowest<KEY>();
-        }
+        for (int v = 1; v < V; ++v) best = larger(best, key[v]);
+        best = team_max<L>(best);          // -infinity: none is left for this token; others of the wavefront may go on
+        // the first that has it: for a token of a whole wavefront by scalar instructions, a mask of lanes for each v (4000 tokens, 12 of 512: 9.3 us against 9.9); for two
+        // tokens that takes twice as many (8190 tokens, 7 of 192: 13.9 us against 12.8)
         int at = 0x7fffffff;
+        if constexpr (L == 64) {
 #pragma unroll
-        for (int v = V - 1; v >= 0; --v)
-            if (key[v] == best) at = v * L + lane;
-        at = team_min<L>(at);
+            for (int v = V - 1; v >= 0; --v) {
+                const uint64_t has = __ballot(key[v] == best);
+                at = has ? v * L + __builtin_ctzll(has) : at;
+            }
+        } else {
+#pragma unroll
+            for (int v = V - 1; v >= 0; --v) at = key[v] == best ? v * L + lane : at;
+            at = (int)team_all<L, 1>((uint32_t)at, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+        }
         const bool real = best > lowest<KEY>();
         if (lane == j) mine = real ? at : -1;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v * L + lane == at) key[v] = lowest<KEY>();
+        for (int v = 0; v < V; ++v) key[v] = v * L + lane == at ? lowest<KEY>() : key[v];
     }
     double p = 0.0;
     if (mine >= 0) {
         const float x = logit_of(a, row + mine);
-        p = a.sigmoid ? sigmoid(x) : raised(x);
+        p = a.sigmoid ? series.sigmoid(x) : raised(x);
     }
     if (a.renormalise) {
         const double sum = team_sum<L>(p);
@@ -545,6 +606,7 @@ extern "C" int qg_route(const qg_route_desc *d, void *stream)
     // as few lanes a token as eight experts a lane allow, and one a choice at least
     if (E <= 64 && k <= 16) route_launch<16, 4>(a, scores, st);
     else if (E <= 128 && k <= 16) route_launch<16, 8>(a, scores, st);
+    else if (E <= 192 && k <= 32) route_launch<32, 6>(a, scores, st);
     else if (E <= 256 && k <= 32) route_launch<32, 8>(a, scores, st);
     else if (E <= 512) route_launch<64, 8>(a, scores, st);
     else route_launch<64, 16>(a, scores, st);

@@ -152,6 +152,21 @@ def test_route_of_values_that_are_no_numbers(qg, score, bias):
         assert not ((ids == 2) | (ids == 5)).any()
 
 
+@pytest.mark.parametrize("score,renormalise", [("softmax", True), ("softmax", False), ("sigmoid", False)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_route_of_every_magnitude(qg, score, renormalise, bias):
+    # exponentials from 1 to what 64 bits do not hold, of 40 experts all chosen, and of equal, huge and tiny logits
+    case("route magnitudes", score, renormalise, bias)
+    row = torch.tensor([0.0, 1e-40, -1e-40, 2.0 ** -24, 1e-3, 0.3465735, -0.3465736, 0.69314718, 1.0, -1.0, 5.5, -5.5, 16.6, -16.6, 37.0, -37.0, 87.3, -87.3, 88.8, -88.8, -103.9, -104.1,
+                        300.0, -300.0, 708.0, -708.0, -745.0, 746.0, -801.0, 1e4, -1e4, 3e38, -3e38, 2.0, 2.0, 3.25, -3.25, 10.0, -10.0, 0.125])
+    logits = torch.stack([row, row.clamp(-60, 60), row.clamp(-1, 1), torch.full((40,), -3e38), torch.full((40,), 7.0), row.clamp(max=0)])
+    b = 0.3 * torch.randn(40, generator=gen(3)) if bias else None
+    ids, weights = qg.qg_route(logits.cuda(), 40, bias=None if b is None else b.cuda(), score=score, renormalise=renormalise)
+    want, w = plain_route(logits, 40, b, score, 1, 1, 1, renormalise, 1.0)
+    assert torch.equal(ids.cpu(), want)
+    near(weights.cpu(), w, 2 * U * w.abs(), F32)
+
+
 def test_sigmoids_that_tie_rank_by_their_logits(qg):
     logits = torch.tensor([[50.0, 60.0, 40.0, 70.0, 45.0, 38.0, 80.0, 39.0]])
     ids, w = qg.qg_route(logits.cuda(), 4, score="sigmoid", groups=2, top_groups=2, group_best=2)
