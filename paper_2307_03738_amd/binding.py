@@ -833,7 +833,7 @@ def _matrix_rows(t: torch.Tensor, name: str, shape=None, types=_FLOATS):
 
 
 def _stream_of(*tensors) -> int:
-    """The current stream of the current device, which all of a call's tensors have to lie on."""
+    """The current stream of the current device, which all of a call's tensors have to lie on (those that the call makes lie where its first does)."""
     device = torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != device:
@@ -852,7 +852,7 @@ def qg_route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = No
     if score not in _SCORES:
         raise ValueError("score: softmax or sigmoid")
     bp = 0 if bias is None else _whole(bias, torch.float32, "bias", (experts,))
-    shape, device = (tokens, top_k), logits.device
+    shape, device, stream = (tokens, top_k), logits.device, _stream_of(logits, bias, ids, weights)
     if top_k <= 0:
         _check(2, "qg_route")
     if ids is None:
@@ -864,7 +864,7 @@ def qg_route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = No
     else:
         _whole(weights, torch.float32, "weights", shape)
     rc = (_LIB or lib()).qg_route(_ROUTE(lp, bp, ids.data_ptr(), weights.data_ptr(), tokens, stride, kind, experts, top_k, _SCORES[score],
-                                         groups, groups if top_groups is None else top_groups, group_best, 1 if renormalise else 0, scale), _stream_of(logits, bias, ids, weights))
+                                         groups, groups if top_groups is None else top_groups, group_best, 1 if renormalise else 0, scale), stream)
     if rc != 0:
         _check(rc, "qg_route")
     return ids, weights
@@ -880,6 +880,7 @@ def qg_expert_plan(ids: torch.Tensor, experts: int, out=None):
     ip, device = _whole(ids, torch.int32, "ids", shape), ids.device
     if experts <= 0 or top_k <= 0:
         _check(2, "qg_expert_plan")
+    stream = _stream_of(ids, *(() if out is None else out))
     if out is None:
         offsets, slot_tokens, slots = _ints(experts + 1, device), _ints(tokens * top_k, device), _rows(tokens, top_k, torch.int32, device)
     else:
@@ -887,8 +888,7 @@ def qg_expert_plan(ids: torch.Tensor, experts: int, out=None):
         _whole(offsets, torch.int32, "offsets", (experts + 1,))
         _whole(slot_tokens, torch.int32, "slot_tokens", (tokens * top_k,))
         _whole(slots, torch.int32, "slots", shape)
-    rc = (_LIB or lib()).qg_expert_plan(ip, tokens, top_k, experts, offsets.data_ptr(), slot_tokens.data_ptr(), slots.data_ptr(),
-                                       _stream_of(ids, offsets, slot_tokens, slots))
+    rc = (_LIB or lib()).qg_expert_plan(ip, tokens, top_k, experts, offsets.data_ptr(), slot_tokens.data_ptr(), slots.data_ptr(), stream)
     if rc != 0:
         _check(rc, "qg_expert_plan")
     return offsets, slot_tokens, slots
@@ -917,7 +917,7 @@ def qg_experts_product(packed: torch.Tensor, N: int, K: int, bits: int, group: i
     else:
         slots = rows.shape[0]
         rp = _whole(rows, torch.int32, "rows", (slots,))
-    columns = N // 2 if gated else N
+    columns, stream = N // 2 if gated else N, _stream_of(packed, x, offsets, rows, y, workspace)
     if y is None:
         y = _rows(slots, columns, x.dtype if dtype is None else dtype, x.device)
     else:
@@ -930,8 +930,7 @@ def qg_experts_product(packed: torch.Tensor, N: int, K: int, bits: int, group: i
         raise ValueError("workspace: expected a contiguous tensor")
     rc = L.qg_experts_product(_EXPERTS(packed.data_ptr(), xp, op, rp, y.data_ptr(), N, K, packed.stride(0), x_rows, xs, slots,
                                        bits, group, experts, kind, ykind, 1 if gated else 0,
-                                       workspace.data_ptr(), workspace.numel() * workspace.element_size()),
-                              _stream_of(packed, x, offsets, rows, y, workspace))
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
     if rc != 0:
         _check(rc, "qg_experts_product")
     return y
@@ -952,6 +951,7 @@ def qg_experts_combine(y: torch.Tensor, slots: torch.Tensor, weights: torch.Tens
     sp, wp = _whole(slots, torch.int32, "slots", shape), _whole(weights, torch.float32, "weights", shape)
     if dtype is None:
         dtype = out.dtype if out is not None else residual.dtype if residual is not None else y.dtype
+    stream = _stream_of(y, slots, weights, residual, out)
     if out is None:
         out = _rows(tokens, N, dtype, y.device)
     else:
@@ -962,8 +962,7 @@ def qg_experts_combine(y: torch.Tensor, slots: torch.Tensor, weights: torch.Tens
         if residual.dtype is not dtype:
             raise ValueError(f"residual: expected a {dtype} tensor")
         rp, rs, _ = _matrix_rows(residual, "residual", (tokens, N))
-    rc = (_LIB or lib()).qg_experts_combine(_COMBINE(y.data_ptr(), sp, wp, rp, out.data_ptr(), y_rows, tokens, N, rs, kind, okind, top_k),
-                                           _stream_of(y, slots, weights, residual, out))
+    rc = (_LIB or lib()).qg_experts_combine(_COMBINE(y.data_ptr(), sp, wp, rp, out.data_ptr(), y_rows, tokens, N, rs, kind, okind, top_k), stream)
     if rc != 0:
         _check(rc, "qg_experts_combine")
     return out

@@ -26,13 +26,37 @@ static inline int64_t qg_most_tiles(int64_t slots, int experts, int most)
     return (slots + used * (most - 1)) / most;
 }
 
+// Slots of an expert, from where to where: offsets are taken into 0 ... slots whatever they are.
+__device__ inline void expert_slots(const QgExpertsArgs &a, int e, int64_t &begin, int64_t &count)
+{
+    begin = a.offsets[e];
+    int64_t end = a.offsets[e + 1];
+    begin = begin < 0 ? 0 : begin > a.slots ? a.slots : begin;
+    end = end < 0 ? 0 : end > a.slots ? a.slots : end;
+    count = end > begin ? end - begin : 0;
+}
+
+// Tiles of `most` slots that the experts have, row_tiles at most.
+__device__ inline int expert_tiles(const QgExpertsArgs &a, int most)
+{
+    int64_t tiles = 0;
+    for (int e = threadIdx.x & 63; e < a.experts; e += 64) {
+        int64_t begin, count;
+        expert_slots(a, e, begin, count);
+        tiles += (count + most - 1) / most;
+    }
+    int sum = (int)(tiles < a.row_tiles ? tiles : a.row_tiles);
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) sum = min(sum + __shfl_xor(sum, off), a.row_tiles);
+    return __builtin_amdgcn_readfirstlane(sum);
+}
+
 struct ExpertTile {
     int expert, rows;          // rows 0: there is no such tile
     int64_t begin;             // its first slot
 };
 
 // Tile number `tile` of the experts' tiles of `most` slots, expert by expert: a wavefront adds up 64 experts' tiles at a time.
-// Offsets are taken into 0 ... slots whatever they are.
 __device__ inline ExpertTile expert_tile(const QgExpertsArgs &a, int64_t tile, int most)
 {
     const int lane = threadIdx.x & 63;
@@ -40,13 +64,7 @@ __device__ inline ExpertTile expert_tile(const QgExpertsArgs &a, int64_t tile, i
     for (int e0 = 0; e0 < a.experts; e0 += 64) {
         const int e = e0 + lane;
         int64_t begin = 0, count = 0;
-        if (e < a.experts) {
-            begin = a.offsets[e];
-            int64_t end = a.offsets[e + 1];
-            begin = begin < 0 ? 0 : begin > a.slots ? a.slots : begin;
-            end = end < 0 ? 0 : end > a.slots ? a.slots : end;
-            count = end > begin ? end - begin : 0;
-        }
+        if (e < a.experts) expert_slots(a, e, begin, count);
         const int mine = (int)((count + most - 1) / most);
         int upto = mine;
 #pragma unroll

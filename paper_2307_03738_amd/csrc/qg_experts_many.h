@@ -8,7 +8,7 @@
 //
 // That prompt now takes 1.50 to 1.57 ms, 0.93 to 0.97 PFLOP/s; a library's product of bf16 matrices reaches 1.20.  Both are held by power (the clock falls to 2.0 GHz; a loop of nothing but
 // matrix instructions reaches 1.65), here by 9 vector instructions beside each matrix instruction: a loop of just these and no memory makes 1.17 to 1.33.  Codes unpacked once for a
-// whole workgroup by way of LDS make 0.95 to 1.04 in such a loop.  8184 slots of 60 5120 x 1792 2-bit matrices, groups of 64: 235 us (0.64 PFLOP/s; 14 steps of 128 k, 10.5 vector instructions).
+// whole workgroup by way of LDS make 0.95 to 1.04 in such a loop.  8184 slots of 60 5120 x 1792 2-bit matrices, groups of 64: 209 us (0.71 PFLOP/s; 14 steps of 128 k, 10.5 vector instructions and more in the last tiles).
 #pragma once
 
 #include <type_traits>
@@ -207,13 +207,16 @@ __global__ __launch_bounds__(256, MOST == 1 ? 3 : 2) void experts_many(const QgM
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ int32_t ups[32 * MOST];
     // A die's workgroups (i % 8) take neighbouring pieces, eight blocks of columns by as many tiles of slots: they share X's rows and weights in its L2.
-    int block = blockIdx.x;
+    // Shares are of the tiles that there are, not of those that there could be: otherwise a die had up to 13 % more than its part (8184 slots of 60 experts: 236 us, 209 so).
+    const int tiles = expert_tiles(f.e, 32 * MOST);
+    int block = blockIdx.x >> 3;
     {
-        const int die = block & 7, each = f.blocks >> 3, more = f.blocks & 7;
-        block = die * each + (die < more ? die : more) + (block >> 3);
+        const int blocks = tiles * f.column_blocks, die = blockIdx.x & 7, each = blocks >> 3, more = blocks & 7;
+        if (block >= each + (die < more)) return;
+        block += die * each + (die < more ? die : more);
     }
-    const int band = block / (8 * f.e.row_tiles), across = min(8, f.column_blocks - 8 * band);
-    const int rest = block - band * 8 * f.e.row_tiles;
+    const int band = block / (8 * tiles), across = min(8, f.column_blocks - 8 * band);
+    const int rest = block - band * 8 * tiles;
     const ExpertTile t = expert_tile(f.e, rest / across, 32 * MOST);
     if (t.rows == 0) return;
     const int expert = __builtin_amdgcn_readfirstlane(t.expert), rows = __builtin_amdgcn_readfirstlane(t.rows);
