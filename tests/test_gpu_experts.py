@@ -330,6 +330,9 @@ FEW = [
     (2050, 288, 3, 96, some(60, 4, 3), False, BF16, F32, False, 0),
     (2050, 160, 2, 32, some(60, 4, 3), False, F32, F32, True, 0),
     (1030 * 2, 320, 2, 64, some(60, 4, 3), True, F16, F16, True, 0),
+    (1290, 192, 4, 64, some(130, 1, 60), False, BF16, F32, True, 0),              # many experts of many rows
+    (645 * 2, 128, 2, 32, some(70, 1, 300), True, F32, F32, True, 8),
+    (300, 384, 3, 128, some(200, 3, 500), False, F16, F32, True, 0),
     (64, 9600, 4, 128, [0, 1, 0, 0, 2, 0, 0, 0], False, F32, F32, True, 0),       # rows too long for a workgroup's own conversion of two
     (64, 4992, 2, 64, [0, 1, 0, 0, 2, 0, 0, 1], False, F32, F32, True, 0),        # ... of three
 ]
