@@ -36,19 +36,16 @@ __device__ inline void expert_slots(const QgExpertsArgs &a, int e, int64_t &begi
     count = end > begin ? end - begin : 0;
 }
 
-// Tiles of `most` slots that the experts have, row_tiles at most.
-__device__ inline int expert_tiles(const QgExpertsArgs &a, int most)
+// Sums of v over the lanes up to each, on the vector ALU: inside a row of 16 lanes, then rows' last sums to the rows behind them.
+__device__ inline int sum_upto(int v)
 {
-    int64_t tiles = 0;
-    for (int e = threadIdx.x & 63; e < a.experts; e += 64) {
-        int64_t begin, count;
-        expert_slots(a, e, begin, count);
-        tiles += (count + most - 1) / most;
-    }
-    int sum = (int)(tiles < a.row_tiles ? tiles : a.row_tiles);
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) sum = min(sum + __shfl_xor(sum, off), a.row_tiles);
-    return __builtin_amdgcn_readfirstlane(sum);
+    v += (int)dpp<0x111, 0xf>((uint32_t)v);
+    v += (int)dpp<0x112, 0xf>((uint32_t)v);
+    v += (int)dpp<0x114, 0xf>((uint32_t)v);
+    v += (int)dpp<0x118, 0xf>((uint32_t)v);
+    v += (int)dpp<0x142, 0xa>((uint32_t)v);
+    v += (int)dpp<0x143, 0xc>((uint32_t)v);
+    return v;
 }
 
 struct ExpertTile {
@@ -56,38 +53,53 @@ struct ExpertTile {
     int64_t begin;             // its first slot
 };
 
-// Tile number `tile` of the experts' tiles of `most` slots, expert by expert: a wavefront adds up 64 experts' tiles at a time.
+// 64 experts' tiles of `most` slots, an expert a lane.
+struct ExpertTiles {
+    int e0, begin, count, mine, upto;
+    __device__ inline ExpertTiles(const QgExpertsArgs &a, int first, int most) : e0(first)
+    {
+        const int e = first + (int)(threadIdx.x & 63);
+        int64_t from = 0, slots = 0;
+        if (e < a.experts) expert_slots(a, e, from, slots);
+        begin = (int)from;
+        count = (int)slots;
+        mine = (int)((slots + most - 1) / most);
+        upto = sum_upto(mine);
+    }
+    __device__ inline int total() const { return __builtin_amdgcn_readlane(upto, 63); }
+    // tile `tile` of these, if there is one
+    __device__ inline bool take(int64_t tile, int most, ExpertTile &t) const
+    {
+        const uint64_t past = __ballot(upto > tile);
+        if (!past) return false;
+        const int at = __builtin_ctzll(past);
+        const int64_t skip = (tile - __builtin_amdgcn_readlane(upto - mine, at)) * most, n = __builtin_amdgcn_readlane(count, at), left = n - skip;
+        t.expert = e0 + at;
+        t.begin = __builtin_amdgcn_readlane(begin, at) + skip;
+        t.rows = (int)(left < most ? left : most);
+        if (left <= 0 || left > n) t.rows = 0;          // (offsets that decrease, whose tiles do not add up in 32 bits)
+        return true;
+    }
+};
+
+// Tile number `tile` of the experts' tiles, expert by expert: a wavefront adds up 64 experts' tiles at a time.
 __device__ inline ExpertTile expert_tile(const QgExpertsArgs &a, int64_t tile, int most)
 {
-    const int lane = threadIdx.x & 63;
-    int64_t before = 0;
+    ExpertTile t = {0, 0, 0};
     for (int e0 = 0; e0 < a.experts; e0 += 64) {
-        const int e = e0 + lane;
-        int64_t begin = 0, count = 0;
-        if (e < a.experts) expert_slots(a, e, begin, count);
-        const int mine = (int)((count + most - 1) / most);
-        int upto = mine;
-#pragma unroll
-        for (int off = 1; off < 64; off *= 2) {
-            const int o = __shfl_up(upto, off);
-            if (lane >= off) upto += o;
-        }
-        const uint64_t past = __ballot(before + upto > tile);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            const int64_t first = before + __shfl(upto - mine, at);
-            ExpertTile t;
-            t.expert = e0 + at;
-            const int b = __shfl((int)begin, at), n = __shfl((int)count, at);
-            t.begin = b + (tile - first) * most;
-            const int64_t left = n - (tile - first) * most;
-            if (left <= 0 || left > n) return {0, 0, 0};         // (offsets that decrease, whose tiles do not add up in 32 bits)
-            t.rows = (int)(left < most ? left : most);
-            return t;
-        }
-        before += __shfl(upto, 63);
+        const ExpertTiles tiles(a, e0, most);
+        if (tiles.take(tile, most, t)) break;
+        tile -= tiles.total();
     }
-    return {0, 0, 0};
+    return t;
+}
+
+// As many as there are, row_tiles at most.
+__device__ inline int expert_tiles(const QgExpertsArgs &a, int most)
+{
+    int64_t sum = 0;
+    for (int e0 = 0; e0 < a.experts; e0 += 64) sum += ExpertTiles(a, e0, most).total();
+    return sum < 0 || sum > a.row_tiles ? a.row_tiles : (int)sum;
 }
 
 // Where the weights of a lane's output lie: addresses for the whole wavefront (of the first output's tile) and the lane's distance from them.
@@ -109,7 +121,16 @@ __device__ inline OutputWeights output_weights(const QgExpertsArgs &a, int exper
     return w;
 }
 
-__device__ inline float silu(float v) { return v / (1.0f + expf(-v)); }
+// v / (1 + e^-v) to 7 units of its last place: with t = e^-|v| = 2^n 2^f it is v t / (1 + t) below zero and v / (1 + t) above, so that nothing overflows and
+// what is below the normal numbers stays.  Half as many instructions as the library's exponential and a division (many rows of short K: 37 to 34 us together with scans on the vector ALU).
+__device__ inline float silu(float v)
+{
+    const float m = __builtin_fminf(__builtin_fabsf(v), 200.0f), n = __builtin_rintf(m * -0x1.715476p0f);
+    float f = __builtin_fmaf(m, -0x1.715476p0f, -n);               // log2 e in two parts
+    f = __builtin_fmaf(m, -0x1.4ae0cp-26f, f);
+    const float t = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
+    return v * (v < 0.0f ? t : 1.0f) * __builtin_amdgcn_rcpf(1.0f + t);
+}
 
 __device__ inline void store_typed(int type, void *p, int64_t i, float v)
 {

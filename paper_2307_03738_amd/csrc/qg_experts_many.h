@@ -174,7 +174,22 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
         __builtin_amdgcn_s_barrier();
     }
 
-    // out: the type is asked for once; rows lie in scalar addresses, a lane's column and half beside them
+    // powers of two back, gates into their ups; then out: the type is asked for once, rows lie in scalar addresses, a lane's column and half beside them
+    auto finish = [&](auto gated) {
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = 32 * m + 8 * (e / 4) + e % 4;
+                if (r >= t.rows) continue;
+                const int down = -ups[r + 4 * half];
+                const float v0 = __builtin_amdgcn_ldexpf(y[m][0][e], down), v1 = __builtin_amdgcn_ldexpf(y[m][1][e], down);
+                y[m][0][e] = decltype(gated)::value ? silu(v0) * v1 : v0;
+                y[m][1][e] = v1;
+            }
+    };
+    if (a.gated) finish(std::true_type());
+    else finish(std::false_type());
     const int64_t c = wave_column + r0;
     const bool first = c < a.columns, second = !a.gated && c + 32 < a.columns;
     auto store = [&](auto type) {
@@ -186,12 +201,10 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
             for (int e = 0; e < 16; ++e) {
                 const int r = 32 * m + 8 * (e / 4) + e % 4;
                 if (r >= t.rows) continue;
-                const int down = -ups[r + 4 * half];
-                const float v0 = __builtin_amdgcn_ldexpf(y[m][0][e], down), v1 = __builtin_amdgcn_ldexpf(y[m][1][e], down);
                 char *to = (char *)a.y + ((t.begin + r) * a.columns + wave_column) * SIZE + lane_at;
                 if (r + 4 * half < t.rows) {
-                    if (first) store_float<TYPE>(to, 0, a.gated ? silu(v0) * v1 : v0);
-                    if (second) store_float<TYPE>(to, 32, v1);
+                    if (first) store_float<TYPE>(to, 0, y[m][0][e]);
+                    if (second) store_float<TYPE>(to, 32, y[m][1][e]);
                 }
             }
     };
@@ -208,7 +221,9 @@ __global__ __launch_bounds__(256, MOST == 1 ? 3 : 2) void experts_many(const QgM
     __shared__ int32_t ups[32 * MOST];
     // A die's workgroups (i % 8) take neighbouring pieces, eight blocks of columns by as many tiles of slots: they share X's rows and weights in its L2.
     // Shares are of the tiles that there are, not of those that there could be: otherwise a die had up to 13 % more than its part (8184 slots of 60 experts: 236 us, 209 so).
-    const int tiles = expert_tiles(f.e, 32 * MOST);
+    // (up to 64 experts are looked at once, for the number of tiles and for the workgroup's own)
+    const ExpertTiles first(f.e, 0, 32 * MOST);
+    const int tiles = f.e.experts > 64 ? expert_tiles(f.e, 32 * MOST) : first.total() < 0 || first.total() > f.e.row_tiles ? f.e.row_tiles : first.total();
     int block = blockIdx.x >> 3;
     {
         const int blocks = tiles * f.column_blocks, die = blockIdx.x & 7, each = blocks >> 3, more = blocks & 7;
@@ -217,7 +232,9 @@ __global__ __launch_bounds__(256, MOST == 1 ? 3 : 2) void experts_many(const QgM
     }
     const int band = block / (8 * tiles), across = min(8, f.column_blocks - 8 * band);
     const int rest = block - band * 8 * tiles;
-    const ExpertTile t = expert_tile(f.e, rest / across, 32 * MOST);
+    ExpertTile t = {0, 0, 0};
+    if (f.e.experts > 64) t = expert_tile(f.e, rest / across, 32 * MOST);
+    else first.take(rest / across, 32 * MOST, t);
     if (t.rows == 0) return;
     const int expert = __builtin_amdgcn_readfirstlane(t.expert), rows = __builtin_amdgcn_readfirstlane(t.rows);
     const ExpertTile u = {expert, rows, (int64_t)__builtin_amdgcn_readfirstlane((int)t.begin)};
