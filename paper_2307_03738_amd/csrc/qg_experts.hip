@@ -22,9 +22,9 @@ RowsSpace rows_space(int64_t x_rows, int64_t K, int x_type)
 // Slots of a workgroup of the kernel of many rows, 64 or 32, or 0: the kernel of few rows.
 //
 // By the rows of an expert, on average: few rows up to 20 operand rows (two of fp32 each); beyond, tiles of 32 slots, three workgroups a compute unit, up to
-// 64 rows (128 of fp32, whose two parts make as much of a weight unpacked).  Each side measured, us: 32 experts' 4096 x 4096 4-bit matrices, groups of 64: 8 rows fp32
-// 81 by few against 96, 12 rows 101 against 99, 16 rows bf16 81 against 82, 24 rows 108 against 104; tiles of 32 against 64, bf16 48 rows 132, 142; fp32 48 rows
-// 179, 240; 100 rows fp32 (5632 x 2048) 416, 458; 512 rows: bf16, 8192 x 4096, groups of 32, 497, 418, fp32 groups of 128 547, 526.
+// 48 rows (128 of fp32, whose two parts make as much of a weight unpacked).  Each side measured, us: 32 experts' 4096 x 4096 4-bit matrices, groups of 64: 8 rows fp32
+// 81 by few against 96, 12 rows 101 against 99, 16 rows bf16 81 against 82, 24 rows 108 against 104; tiles of 32 against 64, groups of 128: bf16 44 rows 111, 117, 52 rows 124, 121;
+// groups of 32: 44 rows 143, 144, 60 rows 167, 153; fp32, groups of 64: 64 rows 193, 222, 136 rows 358, 366; 512 rows: bf16, 8192 x 4096, groups of 32, 497, 418, fp32 groups of 128 547, 526.
 //
 // And by workgroups: with fewer than one a compute unit tiles of 32, and where those are not 9 to 16 units the wavefronts of few rows, which also divide K.  2 experts, 300 rows, 1000 x 8192:
 // 98 (64), 77 (32), 36 (few); 2, 400 rows, 4096 x 4096: 55, 44, 50; 4, 2000 rows, 400 x 4096: 60, 51, 40; 3, 6000 rows, 1000 x 1024: 36, 37, 63.
@@ -34,7 +34,7 @@ int many_rows_of(const QgExpertsArgs &a, int parts)
     const int width = a.gated ? 128 : 256;
     const int64_t across = (a.columns + width - 1) / width;
     if (qg_most_tiles(a.slots, a.experts, 32) * across * 16 <= (int64_t)9 * qg_compute_units()) return 0;
-    if (a.slots <= (int64_t)64 * parts * a.experts || qg_most_tiles(a.slots, a.experts, 64) * across < qg_compute_units()) return 32;
+    if (a.slots <= (int64_t)(parts == 2 ? 128 : 48) * a.experts || qg_most_tiles(a.slots, a.experts, 64) * across < qg_compute_units()) return 32;
     return 64;
 }
 
