@@ -38,6 +38,7 @@ int many_rows_of(const QgExpertsArgs &a, int parts)
     return 64;
 }
 
+constexpr int MANY_SLICED = 3, MANY_SLICED_K = 1024;
 int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)
 {
     QgFewArgs f = {};
@@ -95,6 +96,7 @@ int many_plan(const QgExpertsArgs &a, int bits, int tile_rows, const RowsSpace &
     const int64_t blocks = (int64_t)f.e.row_tiles * f.column_blocks;
     if (blocks > QG_MOST_GROUPS) return QG_ERR_SHAPE;
     f.blocks = (int)blocks;
+    f.slices = tile_rows == 32 && blocks < (int64_t)MANY_SLICED * qg_compute_units() && a.K >= MANY_SLICED_K ? 3 : 1;
     return (bits == 4 ? qg_many_launch_b4 : bits == 3 ? qg_many_launch_b3 : qg_many_launch_b2)(f, p, st);
 }
 

@@ -23,6 +23,7 @@ struct QgManyArgs {
     int parts;
     int g32, gshift;
     int tile_rows;             // slots of a workgroup: 32 or 64
+    int slices;                // of K: 1, or 3, four wavefronts each
     int column_blocks;         // of 256 outputs
     int blocks;
 };
@@ -31,7 +32,7 @@ struct QgManyArgs {
 namespace {
 
 // MB: blocks of 32 slots.
-template <int BITS, int GP, int PARTS, int MB>
+template <int BITS, int GP, int PARTS, int MB, int SLICES>
 __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64_t column0, char *smem, int32_t *ups)
 {
     using F = Fmt<BITS>;
@@ -39,7 +40,8 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
     constexpr int ROWS = 32 * MB, STAGE = ROWS * 256 * PARTS;
     constexpr int COPIES = ROWS * PARTS / 16;                              // of 4 rows, a wavefront's
     const QgExpertsArgs &a = f.e;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
+    const int slice = SLICES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
     const int half = lane >> 5;
 
     // this lane's output
@@ -48,7 +50,8 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
     const int64_t n = (column < a.columns ? column : a.columns - 1) + (a.gated && half ? (int64_t)a.columns : 0);
     const OutputWeights at_n = output_weights(a, t.expert, n);
     const int last_group = a.K / a.group - 1;
-    const int steps = (a.K + 127) / 128;
+    const int steps = (a.K + 127) / 128, begin = steps * slice / SLICES, end = steps * (slice + 1) / SLICES;
+    char *const stages = smem + slice * 2 * STAGE;
 
     // the rows it copies: 16 bytes of row 4 j + lane / 16 each, octet (lane % 16) ^ (row % 16) of the 128 k, so that 16 rows' octets of the same k
     // lie on distinct banks
@@ -61,10 +64,10 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
             row = a.rows ? a.rows[t.begin + r] : t.begin + r;
             row = row >= 0 && row < a.x_rows ? row : a.x_rows;
         }
-        if (part == 0 && (lane & 15) == 0) ups[r] = f.up[row];
+        if (part == 0 && (lane & 15) == 0 && slice == 0) ups[r] = f.up[row];
         from[j] = (uint64_t)(uintptr_t)(f.xh + ((row * PARTS + part) * f.padded) * 2 + (((lane & 15) ^ (r & 15)) * 16));
     }
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)stages;
     auto copy = [&](int step, int stage) {
 #pragma unroll
         for (int j = 0; j < COPIES; ++j) {
@@ -101,15 +104,23 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
     const int r0 = lane & 31;
 
     Weights next;
-    copy(0, 0);
-    load(0, next);
+    if (begin < end) {
+        copy(begin, 0);
+        load(begin, next);
+    }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
-    for (int step = 0; step < steps; ++step) {
+    const int turns = (steps + SLICES - 1) / SLICES;               // as many for every slice, for their barriers
+    for (int turn = 0; turn < turns; ++turn) {
+        const int step = begin + turn;
+        if (SLICES > 1 && step >= end) {
+            __builtin_amdgcn_s_barrier();
+            continue;
+        }
         const Weights w = next;
-        const char *x = smem + (step & 1) * STAGE;
-        if (step + 1 < steps) {
-            copy(step + 1, (step + 1) & 1);
+        const char *x = stages + (turn & 1) * STAGE;
+        if (step + 1 < end) {
+            copy(step + 1, (turn + 1) & 1);
             load(step + 1, next);
         }
         // sixteens of k: operands of X are read AHEAD sixteens before they are multiplied, codes unpacked right before
@@ -174,6 +185,31 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
         __builtin_amdgcn_s_barrier();
     }
 
+    if constexpr (SLICES > 1) {
+        // slices meet: the first adds the others' sums in order (every wavefront is behind the last barrier: the stages are free)
+        float *sums = (float *)smem;
+        constexpr int OF_WAVE = MB * 32 * 64;
+        if (slice > 0) {
+            float *to = sums + ((slice - 1) * 4 + wave) * OF_WAVE + lane;
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) to[((m * 2 + b) * 16 + e) * 64] = y[m][b][e];
+        }
+        __syncthreads();
+        if (slice > 0) return;
+        for (int sl = 1; sl < SLICES; ++sl) {
+            const float *from = sums + ((sl - 1) * 4 + wave) * OF_WAVE + lane;
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[m][b][e] += from[((m * 2 + b) * 16 + e) * 64];
+        }
+    }
     // powers of two back, gates into their ups; then out: the type is asked for once, rows lie in scalar addresses, a lane's column and half beside them
     auto finish = [&](auto gated) {
 #pragma unroll
@@ -213,9 +249,9 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
     else store(std::integral_constant<int, QG_F16>());
 }
 
-// MOST: 32 slots in registers for three workgroups a compute unit, or 64 for two.
-template <int BITS, int GP, int PARTS, int MOST>
-__global__ __launch_bounds__(256, MOST == 1 ? 3 : 2) void experts_many(const QgManyArgs f)
+// MOST: 32 slots in registers for three workgroups a compute unit, or 64 for two.  SLICES: a workgroup has so many times four wavefronts, each four a slice of K.
+template <int BITS, int GP, int PARTS, int MOST, int SLICES>
+__global__ __launch_bounds__(256 * SLICES, MOST == 1 ? 3 : 2) void experts_many(const QgManyArgs f)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ int32_t ups[32 * MOST];
@@ -239,34 +275,36 @@ __global__ __launch_bounds__(256, MOST == 1 ? 3 : 2) void experts_many(const QgM
     const int expert = __builtin_amdgcn_readfirstlane(t.expert), rows = __builtin_amdgcn_readfirstlane(t.rows);
     const ExpertTile u = {expert, rows, (int64_t)__builtin_amdgcn_readfirstlane((int)t.begin)};
     const int64_t column0 = (int64_t)(8 * band + rest % across) * (f.e.gated ? 128 : 256);
-    if (rows <= 32) many_rows<BITS, GP, PARTS, 1>(f, u, column0, smem, ups);
-    else if constexpr (MOST == 2) many_rows<BITS, GP, PARTS, 2>(f, u, column0, smem, ups);
+    if (rows <= 32) many_rows<BITS, GP, PARTS, 1, SLICES>(f, u, column0, smem, ups);
+    else if constexpr (MOST == 2) many_rows<BITS, GP, PARTS, 2, SLICES>(f, u, column0, smem, ups);
 }
 
-template <int BITS, int GP, int PARTS, int MOST>
+template <int BITS, int GP, int PARTS, int MOST, int SLICES>
 int many_sized(const QgManyArgs &f, hipStream_t st)
 {
-    constexpr size_t lds = (size_t)2 * 32 * MOST * 256 * PARTS;
+    constexpr size_t of_stages = (size_t)SLICES * 2 * 32 * MOST * 256 * PARTS, of_sums = (size_t)(SLICES - 1) * 4 * 32 * MOST * 64 * 4;
+    constexpr size_t lds = of_stages > of_sums ? of_stages : of_sums;
     if (lds > 63 << 10) {
         static std::atomic<bool> prepared[64];      // once per device (devices past the table: every time)
         int dev = -1;
         if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = -1;
         if (dev < 0 || !prepared[dev].load(std::memory_order_acquire)) {
-            if (hipFuncSetAttribute((const void *)experts_many<BITS, GP, PARTS, MOST>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
+            if (hipFuncSetAttribute((const void *)experts_many<BITS, GP, PARTS, MOST, SLICES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
                 (void)hipGetLastError();
                 return QG_ERR_DEVICE;
             }
             if (dev >= 0) prepared[dev].store(true, std::memory_order_release);
         }
     }
-    experts_many<BITS, GP, PARTS, MOST><<<f.blocks, 256, lds, st>>>(f);
+    experts_many<BITS, GP, PARTS, MOST, SLICES><<<f.blocks, 256 * SLICES, lds, st>>>(f);
     return QG_OK;
 }
 
 template <int BITS, int GP, int PARTS>
 int many_typed(const QgManyArgs &f, hipStream_t st)
 {
-    return f.tile_rows == 32 ? many_sized<BITS, GP, PARTS, 1>(f, st) : many_sized<BITS, GP, PARTS, 2>(f, st);
+    if (f.slices > 1) return many_sized<BITS, GP, PARTS, 1, 3>(f, st);
+    return f.tile_rows == 32 ? many_sized<BITS, GP, PARTS, 1, 1>(f, st) : many_sized<BITS, GP, PARTS, 2, 1>(f, st);
 }
 
 template <int BITS>

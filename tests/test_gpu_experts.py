@@ -338,6 +338,20 @@ FEW = [
 ]
 
 
+# workgroups for less than a round: K in three slices, of different lengths, that end inside 128
+SLICED = [
+    (5130, 1056, 4, 32, [100, 77], False, F32, F32, True, 8),
+    (2570 * 2, 1152, 4, 64, [90, 3, 60], True, BF16, BF16, True, 0),
+    (5130, 1280, 4, 128, [33, 120], False, F16, F32, True, 0),
+    (5130, 1408, 4, 128, [33, 120], False, F32, F32, True, 0),
+    (5130, 1344, 4, 96, [128, 1], False, BF16, F32, False, 0),
+    (5130, 1056, 3, 32, [100, 77], False, BF16, F32, True, 0),
+    (2570 * 2, 1216, 3, 64, [100, 77], True, F32, F32, True, 8),
+    (5130, 1024, 3, 128, [100, 77], False, F16, F16, True, 0),
+    (5130, 1120, 2, 32, [100, 77], False, F16, F32, True, 0),
+    (2570 * 2, 1600, 2, 64, [100, 77], True, F32, BF16, True, 0),
+    (5130, 1024, 2, 256, [100, 77], False, BF16, BF16, True, 8),
+]
 # groups that are no whole 32 k: pieces of 8 and of 16 k, words of zero-points that end inside 128 k, K that ends inside 32, few rows and many
 CELLS = [
     (130, 1000, 4, 8, ODD, False, F32, F32, True, 8),
@@ -360,7 +374,7 @@ CELLS = [
 ]
 
 
-@pytest.mark.parametrize("N,K,bits,group,counts,gated,xt,yt,given,gap", PRODUCTS + WIDE + FEW + CELLS)
+@pytest.mark.parametrize("N,K,bits,group,counts,gated,xt,yt,given,gap", PRODUCTS + WIDE + FEW + SLICED + CELLS)
 def test_products_match_64_bits(qg, N, K, bits, group, counts, gated, xt, yt, given, gap):
     case("product", N, K, bits, group, counts[:6], gated, xt, yt, given)
     g = gen(N + K + len(counts))
@@ -388,11 +402,11 @@ def test_products_match_64_bits(qg, N, K, bits, group, counts, gated, xt, yt, gi
         assert (y[[3, 5]] == 0).all()
 
 
-@pytest.mark.parametrize("N,counts", [(96, [1, 0, 0, 2, 0, 0, 0, 0]), (96, [2, 3]), (96, [40, 3]), (96, [300, 9]), (7168, [64, 90]), (5120, [400, 300])])
+@pytest.mark.parametrize("N,counts", [(96, [1, 0, 0, 2, 0, 0, 0, 0]), (96, [2, 3]), (96, [40, 3]), (96, [300, 9]), (7168, [64, 90]), (5120, [400, 300]), (5120, [100, 77])])
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
 def test_values_that_are_no_numbers_stay_in_their_rows(qg, N, counts, dt):
     case("nan", N, counts, dt)
-    K, group = 256, 64
+    K, group = 1152 if counts == [100, 77] else 256, 64
     packed, W = blobs(qg, len(counts), N, K, 4, group, 5)
     offsets = offsets_of(counts)
     x = torch.randn(offsets[-1], K, generator=gen(1)).to(dt)
