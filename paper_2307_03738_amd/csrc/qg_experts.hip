@@ -38,7 +38,6 @@ int many_rows_of(const QgExpertsArgs &a, int parts)
     return 64;
 }
 
-constexpr int MANY_SLICED = 3, MANY_SLICED_K = 1024;
 int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)
 {
     QgFewArgs f = {};
@@ -78,6 +77,11 @@ int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepa
     (bits == 4 ? qg_few_launch_b4 : bits == 3 ? qg_few_launch_b3 : qg_few_launch_b2)(f, p, st);
     return QG_OK;
 }
+
+// Workgroups of 32 slots that make less than a round (three a compute unit) take K in three slices, where it has eight steps at least: 130 tokens' three of three 2646 x 7104 3-bit
+// matrices, bf16, 50 us, without 69; 100 tokens' two of four 4096 x 4096 fp32 35, 44.  (Tiles of 64 where those make one to two workgroups a compute unit stay: 1305 tokens' seven
+// of 26 497 x 2432 59, in 32 sliced 70.)
+constexpr int MANY_SLICED = 3, MANY_SLICED_K = 1024;
 
 int many_plan(const QgExpertsArgs &a, int bits, int tile_rows, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)
 {

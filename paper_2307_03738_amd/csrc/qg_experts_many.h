@@ -6,6 +6,8 @@
 // of X for two 32 x 32 x 16 matrix instructions (half of LDS's rate at full speed of the matrix cores).  Two workgroups share a compute unit: with 128
 // slots and one wavefront a SIMD nothing covers what a wavefront waits for (4096 tokens, two of eight gated 22016 x 4096 4-bit matrices: 2.55 ms against 1.71 at that time).
 //
+// Where workgroups are few they have twelve wavefronts, four for each third of K, which add their sums up in LDS at the end (many_plan says when).
+//
 // That prompt now takes 1.50 to 1.57 ms, 0.93 to 0.97 PFLOP/s; a library's product of bf16 matrices reaches 1.20.  Both are held by power (the clock falls to 2.0 GHz; a loop of nothing but
 // matrix instructions reaches 1.65), here by 9 vector instructions beside each matrix instruction: a loop of just these and no memory makes 1.17 to 1.33.  Codes unpacked once for a
 // whole workgroup by way of LDS make 0.95 to 1.04 in such a loop.  8184 slots of 60 5120 x 1792 2-bit matrices, groups of 64: 209 us (0.71 PFLOP/s; 14 steps of 128 k, 10.5 vector instructions and more in the last tiles).

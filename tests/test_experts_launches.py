@@ -68,11 +68,12 @@ PRODUCTS = [
     (96, 32, 4096, 1408, 3, 64, F32, 0, [("prepare_rows", [3, 256]), ("experts_few", [3, 2, 2, 4, 0])], 8),
     (96, 32, 4096, 1440, 2, 96, BF16, 0, [("prepare_rows", [2, 256]), ("experts_few", [2, 0, 2, 4, 0])], 16),
     (366, 64, 2816, 2048, 4, 32, BF16, 1, [("prepare_rows", [4, 256]), ("experts_few", [4, 1, 2, 4, 0])], 16),
-    (8192, 8, 22016, 4096, 4, 128, BF16, 1, [("prepare_rows", [4, 64]), ("experts_many", [4, 4, 1, 2])], 64),
-    (1280, 32, 4096, 4096, 4, 64, F32, 1, [("prepare_rows", [4, 256]), ("experts_many", [4, 2, 2, 1])], 32),
-    (8184, 60, 5120, 1792, 2, 64, F16, 0, [("prepare_rows", [2, 64]), ("experts_many", [2, 2, 1, 2])], 64),
-    (719, 2, 5130, 160, 4, 32, F32, 0, [("prepare_rows", [4, 256]), ("experts_many", [4, 1, 2, 2])], 64),
-    (173, 5, 7170, 192, 3, 64, F32, 0, [("prepare_rows", [3, 256]), ("experts_many", [3, 2, 2, 1])], 32),
+    (8192, 8, 22016, 4096, 4, 128, BF16, 1, [("prepare_rows", [4, 64]), ("experts_many", [4, 4, 1, 2, 1])], 64),
+    (1280, 32, 4096, 4096, 4, 64, F32, 1, [("prepare_rows", [4, 256]), ("experts_many", [4, 2, 2, 1, 1])], 32),
+    (8184, 60, 5120, 1792, 2, 64, F16, 0, [("prepare_rows", [2, 64]), ("experts_many", [2, 2, 1, 2, 1])], 64),
+    (719, 2, 5130, 160, 4, 32, F32, 0, [("prepare_rows", [4, 256]), ("experts_many", [4, 1, 2, 2, 1])], 64),
+    (173, 5, 7170, 192, 3, 64, F32, 0, [("prepare_rows", [3, 256]), ("experts_many", [3, 2, 2, 1, 1])], 32),
+    (177, 2, 5130, 1056, 4, 32, F32, 0, [("prepare_rows", [4, 256]), ("experts_many", [4, 1, 2, 1, 3])], 32),     # less than a round of workgroups: K in slices
     (300, 2, 1000, 8192, 4, 128, BF16, 0, [("prepare_rows", [4, 256]), ("experts_few", [4, 4, 2, 8, 0])], 16),
     (4, 32, 2816, 4096, 4, 64, F32, 1, [("experts_few", [4, 2, 2, 8, 1])], 2),                              # not many workgroups: eight wavefronts each
     (16, 8, 4096, 4096, 4, 128, BF16, 0, [("prepare_rows", [4, 256]), ("experts_few", [4, 4, 2, 8, 0])], 16),
@@ -91,7 +92,7 @@ def test_products_take_the_kernels_that_are_meant(tmp_path, slots, experts, N, K
     columns = N // 2 if gated else N
     if tile:
         if name == "experts_many":
-            assert x * y >= most_tiles(slots, experts, tile) * -(-columns // (128 if gated else 256))
+            assert x * y >= most_tiles(slots, experts, tile) * -(-columns // (128 if gated else 256)) and lanes == 256 * template[4]
         elif y == 1:                           # 1, 2 or 4 tiles of 64 outputs
             assert x % most_tiles(slots, experts, tile) == 0
             wide = [-(-columns // (w * (32 if gated else 64))) for w in (1, 2, 4)]
