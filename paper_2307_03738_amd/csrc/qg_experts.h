@@ -121,15 +121,18 @@ __device__ inline OutputWeights output_weights(const QgExpertsArgs &a, int exper
     return w;
 }
 
-// v / (1 + e^-v) to 7 units of its last place: with t = e^-|v| = 2^n 2^f it is v t / (1 + t) below zero and v / (1 + t) above, so that nothing overflows and
-// what is below the normal numbers stays.  Half as many instructions as the library's exponential and a division (many rows of short K: 37 to 34 us together with scans on the vector ALU).
+// v / (1 + e^-v) to 8 x 2^-24 of itself: with t = e^-|v| = 2^n e, e = 2^f, it is v / (1 + t) above zero and 2^n (v e / (1 + t)) below, the power of two last, so that nothing
+// overflows and a result is rounded to the steps below the normal numbers once, by itself (t is such a number from v = -87 on, where v t is one from -92 on only).  n ends at
+// |v| = 200, where e takes over and becomes 0.  Half as many instructions as the library's exponential and a division
+// (many rows of short K: 37 to 34 us together with scans on the vector ALU).
 __device__ inline float silu(float v)
 {
-    const float m = __builtin_fminf(__builtin_fabsf(v), 200.0f), n = __builtin_rintf(m * -0x1.715476p0f);
-    float f = __builtin_fmaf(m, -0x1.715476p0f, -n);               // log2 e in two parts
-    f = __builtin_fmaf(m, -0x1.4ae0cp-26f, f);
-    const float t = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
-    return v * (v < 0.0f ? t : 1.0f) * __builtin_amdgcn_rcpf(1.0f + t);
+    const float n = __builtin_rintf(__builtin_fminf(__builtin_fabsf(v), 200.0f) * -0x1.715476p0f);
+    float f = __builtin_fmaf(__builtin_fabsf(v), -0x1.715476p0f, -n);              // log2 e in two parts
+    f = __builtin_fmaf(__builtin_fabsf(v), -0x1.4ae0cp-26f, f);
+    const float e = __builtin_amdgcn_exp2f(f), above = v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_ldexpf(e, (int)n));
+    const float below = __builtin_amdgcn_ldexpf(above * e, (int)n);
+    return v < 0.0f ? below : above;
 }
 
 __device__ inline void store_typed(int type, void *p, int64_t i, float v)
