@@ -480,7 +480,7 @@ int qg_expert_plan(const int32_t *ids, int64_t tokens, int top_k, int experts, i
  *   y[p][n] = sum_k What_e[n][k] x[k]                  (N columns), or, gated, with gate and up side by side as in qg_gemv_swiglu,
  *   y[p][n] = silu(gate[n]) * up[n]                    (N / 2 columns: What_e rows [0, N / 2) are gate, the others up)
  * per group as s * sum (q - z) x, sums in fp32, on the matrix cores: q - z as it is, each row of X times a power of two as f16 (bf16, fp32:
- * the one that brings its largest |x| to [2^14, 2^15)), fp32 in two parts: 2^-22 of an x is left out, and what lies below 2^-39 of its row's largest.  (The power of two is
+ * the one that brings its largest |x| to [2^14, 2^15)): of a bf16 2^-39 of its row's largest is left out at most; fp32 in two parts: 2^-23 of an x, or 2^-51 of its row's largest if that is more.  (The power of two is
  * taken back from the sums: scales of 2^80 and more may make them infinite on the way.)  Groups of whole 32 k have tiles for many rows; other groups take their rows in tiles of 16
  * (fp32: 8).  Gated matrices have to be smaller than 8 GB each.  A call enqueues one kernel or two.
  * A row outside 0 ... x_rows - 1 counts as zeros.  Rows of y past offsets[experts] are left as they were.  NaN and infinity in X

@@ -130,9 +130,12 @@ __device__ inline void words_of(const uint4 *v, int i, uint32_t *w)
     }
 }
 
-// A row of X enters as f16: f16 as it is; bf16 and fp32 times a power of two that puts the largest |x| of the row's part into
-// [2^14, 2^15), so that what f16 leaves out of a bf16 is below 2^-39 of that largest; fp32 in two parts, x less the first in the second
-// (2^-22 of x is left out).  Rows with NaN or infinity are not scaled.
+// A row of X enters as f16: f16 as it is; bf16 and fp32 times a power of two that puts the largest |x| of the row into [2^14, 2^15).  f16's smallest step is
+// 2^-24, so that a bf16's eight bits are whole down to 2^-31 of that largest, and what is left out of it below that is 2^-39 of the largest at most.
+// fp32 goes in two parts, x less the first in the second, which is 2^SECOND_UP times as large as it would be (at most 2^3 before, 2^15 so: it fits), with weights or sums that are as
+// much smaller: its 2^-25 then are 2^-51 of the largest, and 2^-23 of x is left out, or 2^-51 of the row's largest if that is more.  (Without the power 2^-39: ordinary values beside one that
+// is 2^20 times as large kept 19 bits.)  Rows with NaN or infinity are not scaled.
+constexpr int SECOND_UP = 12;
 __device__ inline int row_exponent(uint32_t most)          // most: pattern of the largest |x|
 {
     return most == 0 || most >= 0x7f800000u ? 0 : 141 - (most < 0x00800000u ? 1 : (int)(most >> 23));
@@ -144,7 +147,14 @@ __device__ inline uint32_t two_halves(float a, float b)    // both rounded to ne
 __device__ inline float left_over(float x)                  // of the first part
 {
     const float h = (float)(_Float16)x;
-    return __builtin_fabsf(h) == __builtin_inff() ? 0.0f : x - h;
+    return __builtin_fabsf(h) == __builtin_inff() ? 0.0f : (x - h) * (float)(1 << SECOND_UP);
+}
+// Weights for the second part: q - z is a whole number below 16, exact so, too.
+__device__ inline void second_weights(HalfOperand &o)
+{
+    const _Float16 down = (_Float16)(1.0f / (float)(1 << SECOND_UP));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o.h[i] *= half2v{down, down};
 }
 
 }  // namespace

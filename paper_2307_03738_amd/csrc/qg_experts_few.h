@@ -280,7 +280,8 @@ __global__ __launch_bounds__(64 * WAVES, GP < 0 ? 2 : 4) void experts_few(const 
         }
     }
 
-    // slices meet
+    // slices meet; a row's second part was SECOND_UP higher than its first
+    if (f.parts == 2 && (v & 1)) up += SECOND_UP;
     float *sums = (float *)smem;
     if constexpr (SELF) __syncthreads();
 #pragma unroll

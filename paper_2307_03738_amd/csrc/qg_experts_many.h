@@ -125,8 +125,9 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
             copy(step + 1, (turn + 1) & 1);
             load(step + 1, next);
         }
-        // sixteens of k: operands of X are read AHEAD sixteens before they are multiplied, codes unpacked right before
-        constexpr int KS = 2 * GP, AHEAD = 2;
+        // sixteens of k: operands of X are read AHEAD sixteens before they are multiplied (one where two would not fit into the registers: fp32 with a scale for each 32 k,
+        // 390 slots of three 2646 x 7104 3-bit matrices in slices: 82 us, with two 89), codes unpacked right before
+        constexpr int KS = 2 * GP, AHEAD = PARTS == 2 && GP == 1 ? 1 : 2;
         HalfOperand xo[8][MB * PARTS];
         auto read = [&](int k) {
 #pragma unroll
@@ -169,11 +170,16 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
                         for (int b = 0; b < 2; ++b) unpack_halves<BITS>(p[b], hc, zc[b], o[b]);
                     }
 #pragma unroll
-                    for (int m = 0; m < MB; ++m)
+                    for (int part = 0; part < PARTS; ++part) {
+                        // (in place: 2 to 5 % of an fp32 call's time, with a scale for each 32 k up to 11; operands of their own up to 14 and 20)
+                        if (part)
 #pragma unroll
-                        for (int part = 0; part < PARTS; ++part)
+                            for (int b = 0; b < 2; ++b) second_weights(o[b]);
+#pragma unroll
+                        for (int m = 0; m < MB; ++m)
 #pragma unroll
                             for (int b = 0; b < 2; ++b) sum[m][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xo[k][m * PARTS + part].v, o[b].v, sum[m][b], 0, 0, 0);
+                    }
                 }
             }
 #pragma unroll

@@ -1,10 +1,10 @@
-"""A layer of experts at its edges: gates far below zero.
+"""A layer of experts at its edges: gates far below zero, small values beside large ones.
 
 U = 2^-24, the unit roundoff of fp32; each test derives its bound, set before any of these ran."""
 import pytest
 import torch
 
-from tests.test_gpu_experts import F32, INF, U, case, near
+from tests.test_gpu_experts import F32, INF, U, case, gen, near, offsets_of
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,31 @@ def test_infinite_gates(qg):
     x[:, 0] = torch.tensor([INF, -INF, 1.0])
     y = qg.qg_experts_product(qg.qg_pack(q, s, z, 4, 32)[None], 128, 32, 4, 32, x.cuda(), torch.tensor([0, 3], dtype=torch.int32).cuda(), gated=True).cpu()
     assert (y[0] == INF).all() and torch.isnan(y[1]).all() and torch.isfinite(y[2]).all()      # v / (1 + e^-v) at -infinity is a quotient of infinities
+
+
+# --- fp32 rows of wide range ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("N,K,bits,group,counts", [
+    (64, 64, 4, 32, [0, 1, 0, 0]), (70, 256, 4, 128, [3, 12]), (70, 160, 3, 32, [3, 12]), (70, 192, 2, 64, [3, 12]), (70, 96, 4, 16, [3, 12]), (70, 80, 4, 8, [3, 12]), (70, 96, 2, 16, [3, 12]),
+    (7170, 160, 4, 32, [40, 33, 64]), (7170, 192, 3, 64, [40, 33, 64]), (7170, 256, 2, 128, [40, 33, 64]),
+    (5130, 384, 4, 128, [129, 600]), (5130, 320, 2, 64, [300, 419]), (5130, 160, 3, 32, [300, 419]), (5130, 1056, 4, 32, [100, 77]), (5130, 1280, 2, 128, [100, 77])])
+def test_small_values_beside_a_large_one_count_in_full(qg, N, K, bits, group, counts):
+    # A channel 2^20 to 2^21 above the others, whose weights are zero (q = z), and one other value a row: y is one product.  An x is off by 2^-23 of itself or 2^-51 of the row's
+    # largest (2^-30 here); its parts' products add up with one rounding (2 U, if cut off), the scale's and the sum of a row's parts are one each.
+    case("wide range", N, K, bits, group, counts)
+    E, g = len(counts), gen(N + K)
+    q = torch.randint(0, 2 ** bits, (E, N, K), generator=g, dtype=torch.uint8)
+    s = 0.5 + torch.rand(E, N, K // group, generator=g)
+    z = torch.randint(0, 2 ** bits, (E, N, K // group), generator=g, dtype=torch.uint8)
+    q[:, :, 0] = z[:, :, 0]
+    packed = torch.stack([qg.qg_pack(q[e].cuda(), s[e].cuda(), z[e].cuda(), bits, group) for e in range(E)])
+    offsets = offsets_of(counts)
+    x = torch.zeros(offsets[-1], K)
+    x[:, 0] = 2.0 ** 20 * (1 + torch.rand(len(x), generator=g))
+    at = 1 + 7 * torch.arange(len(x)) % (K - 1)
+    small = 1 + torch.rand(len(x), generator=g)
+    x[torch.arange(len(x)), at] = small
+    y = qg.qg_experts_product(packed, N, K, bits, group, x.cuda(), torch.tensor(offsets, dtype=torch.int32).cuda()).cpu()
+    expert = torch.repeat_interleave(torch.arange(E), torch.tensor(counts))
+    w = s[expert, :, at // group].double() * (q[expert, :, at].double() - z[expert, :, at // group].double())
+    near(y, small.double()[:, None] * w, (6 * U * small.double()[:, None] + 2.0 ** -30) * w.abs(), F32)
