@@ -98,7 +98,7 @@ int many_plan(const QgExpertsArgs &a, int bits, int tile_rows, const RowsSpace &
     const int width = a.gated ? 128 : 256;
     f.column_blocks = (a.columns + width - 1) / width;
     const int64_t blocks = (int64_t)f.e.row_tiles * f.column_blocks;
-    if (blocks > QG_MOST_GROUPS) return QG_ERR_SHAPE;
+    if (blocks > 0x7fffffff - QG_MOST_GROUPS) return QG_ERR_SHAPE;
     f.blocks = (int)blocks;
     f.slices = tile_rows == 32 && blocks < (int64_t)MANY_SLICED * qg_compute_units() && a.K >= MANY_SLICED_K ? 3 : 1;
     return (bits == 4 ? qg_many_launch_b4 : bits == 3 ? qg_many_launch_b3 : qg_many_launch_b2)(f, p, st);

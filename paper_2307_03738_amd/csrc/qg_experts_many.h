@@ -263,14 +263,15 @@ __global__ __launch_bounds__(256 * SLICES, MOST == 1 ? 3 : 2) void experts_many(
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ int32_t ups[32 * MOST];
-    // A die's workgroups (i % 8) take neighbouring pieces, eight blocks of columns by as many tiles of slots: they share X's rows and weights in its L2.
+    // A die's workgroups (number % 8) take neighbouring pieces, eight blocks of columns by as many tiles of slots: they share X's rows and weights in its L2.
     // Shares are of the tiles that there are, not of those that there could be: otherwise a die had up to 13 % more than its part (8184 slots of 60 experts: 236 us, 209 so).
     // (up to 64 experts are looked at once, for the number of tiles and for the workgroup's own)
     const ExpertTiles first(f.e, 0, 32 * MOST);
     const int tiles = f.e.experts > 64 ? expert_tiles(f.e, 32 * MOST) : first.total() < 0 || first.total() > f.e.row_tiles ? f.e.row_tiles : first.total();
-    int block = blockIdx.x >> 3;
+    const int number = blockIdx.y * gridDim.x + blockIdx.x;
+    int block = number >> 3;
     {
-        const int blocks = tiles * f.column_blocks, die = blockIdx.x & 7, each = blocks >> 3, more = blocks & 7;
+        const int blocks = tiles * f.column_blocks, die = number & 7, each = blocks >> 3, more = blocks & 7;
         if (block >= each + (die < more)) return;
         block += die * each + (die < more ? die : more);
     }
@@ -304,7 +305,10 @@ int many_sized(const QgManyArgs &f, hipStream_t st)
             if (dev >= 0) prepared[dev].store(true, std::memory_order_release);
         }
     }
-    experts_many<BITS, GP, PARTS, MOST, SLICES><<<f.blocks, 256 * SLICES, lds, st>>>(f);
+    // (K is in slices where workgroups are few: lanes of a dimension number less than 2^32)
+    const unsigned across = (unsigned)(f.blocks < QG_MOST_GROUPS ? f.blocks : QG_MOST_GROUPS);
+    const dim3 grid(across, (f.blocks + across - 1) / across);
+    experts_many<BITS, GP, PARTS, MOST, SLICES><<<grid, 256 * SLICES, lds, st>>>(f);
     return QG_OK;
 }
 

@@ -1,10 +1,10 @@
-"""A layer of experts at its edges: gates far below zero, small values beside large ones.
+"""A layer of experts at its edges: gates far below zero, small values beside large ones, more workgroups than a launch has in one dimension.
 
 U = 2^-24, the unit roundoff of fp32; each test derives its bound, set before any of these ran."""
 import pytest
 import torch
 
-from tests.test_gpu_experts import F32, INF, U, case, gen, near, offsets_of
+from tests.test_gpu_experts import BF16, F32, INF, U, blobs, case, gen, near, offsets_of, product_want
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +78,21 @@ def test_small_values_beside_a_large_one_count_in_full(qg, N, K, bits, group, co
     expert = torch.repeat_interleave(torch.arange(E), torch.tensor(counts))
     w = s[expert, :, at // group].double() * (q[expert, :, at].double() - z[expert, :, at // group].double())
     near(y, small.double()[:, None] * w, (6 * U * small.double()[:, None] + 2.0 ** -30) * w.abs(), F32)
+
+
+# --- the most workgroups ----------------------------------------------------------------------------------------
+
+def test_more_workgroups_than_a_dimension_has(qg):
+    # 2^23 workgroups and 48892 more, of 64 rows each; every row is one of three
+    case("workgroups", 540000000)
+    N, K, group, slots = 8, 32, 32, 540000000
+    packed, W = blobs(qg, 2, N, K, 4, group, 13)
+    x = torch.randn(3, K, generator=gen(14)).to(BF16)
+    rows = torch.arange(3, dtype=torch.int32, device="cuda").repeat(slots // 3)
+    offsets = torch.tensor([0, slots // 2, slots], dtype=torch.int32, device="cuda")
+    y = qg.qg_experts_product(packed, N, K, 4, group, x.cuda(), offsets, rows=rows)
+    for e in range(2):
+        got = y[e * slots // 2: (e + 1) * slots // 2].view(-1, 3, N)
+        assert bool((got == got[:1]).all())
+        want, slack = product_want(W[e: e + 1], x, [0, 3], None, False, group)
+        near(got[0].cpu(), want, slack, BF16)
