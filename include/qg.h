@@ -453,7 +453,8 @@ typedef enum { QG_SOFTMAX = 0, QG_SIGMOID = 1 } qg_score;
  * largest p (+ bias) (group_best 2; of the one, if there is one).  weights = p, without the bias, times scale; renormalised: p over the sum of the chosen ones' p
  * (0 where that is 0) times scale.  Scores that rank are kept in 64 bits.
  * An expert whose logit (or bias) is -infinity is switched off; where fewer than top_k are left the last ids are -1 and their weights 0.
- * NaN among a token's logits, or biases: experts that have it are switched off, and the token's weights are NaN. */
+ * NaN among a token's logits, or biases: experts that have it are switched off, and the token's weights are NaN; but what is NaN in the bias of an expert that the token's own
+ * logit switches off does not count (a token without experts has weights of 0 whatever the biases are). */
 typedef struct qg_route_desc {
     const void *logits;   /* [tokens][experts] of `type`, rows logits_stride elements apart */
     const float *bias;    /* [experts], or NULL */

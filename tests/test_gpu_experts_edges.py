@@ -1,10 +1,12 @@
-"""A layer of experts at its edges: gates far below zero, small values beside large ones, more workgroups than a launch has in one dimension.
+"""A layer of experts at its edges: gates far below zero, small values beside large ones, values that are no numbers for every width of a token's lanes, more workgroups than a launch has in one dimension.
 
 U = 2^-24, the unit roundoff of fp32; each test derives its bound, set before any of these ran."""
+import math
+
 import pytest
 import torch
 
-from tests.test_gpu_experts import BF16, F32, INF, U, blobs, case, gen, near, offsets_of, product_want
+from tests.test_gpu_experts import BF16, F32, INF, U, blobs, case, gen, near, offsets_of, plain_route, product_want
 
 pytestmark = pytest.mark.gpu
 
@@ -78,6 +80,38 @@ def test_small_values_beside_a_large_one_count_in_full(qg, N, K, bits, group, co
     expert = torch.repeat_interleave(torch.arange(E), torch.tensor(counts))
     w = s[expert, :, at // group].double() * (q[expert, :, at].double() - z[expert, :, at // group].double())
     near(y, small.double()[:, None] * w, (6 * U * small.double()[:, None] + 2.0 ** -30) * w.abs(), F32)
+
+
+# --- choices of values that are no numbers ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("experts,groups,top_groups", [(12, 1, 1), (12, 4, 2), (100, 10, 7), (150, 1, 1), (150, 10, 6), (250, 10, 6), (300, 1, 1), (300, 12, 5), (600, 12, 5)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("best", [1, 2])
+@pytest.mark.parametrize("bias", ["none", "numbers", "switched off", "no number"])
+def test_choices_of_values_that_are_no_numbers(qg, experts, groups, top_groups, score, best, bias):
+    # every width of a token's lanes; of neighbouring tokens one has a NaN; an expert that its logit switches off does not show that its bias is NaN
+    case("route nan", experts, groups, score, best, bias)
+    g = gen(experts + groups)
+    logits = torch.randn(11, experts, generator=g)
+    logits[1, 3] = math.nan
+    logits[3, experts - 1] = math.nan
+    logits[5] = math.nan
+    logits[6, 5] = -INF
+    logits[7] = -INF
+    logits[8, [4, 7]] = INF
+    logits[9, experts // 2:] = -INF
+    b = None if bias == "none" else 0.2 * torch.randn(experts, generator=g)
+    if bias == "switched off":
+        b[[2, experts - 1]] = -INF
+    if bias == "no number":
+        b[5] = math.nan
+    for renormalise in (True, False):
+        ids, w = qg.qg_route(logits.cuda(), 4, bias=None if b is None else b.cuda(), score=score, groups=groups, top_groups=top_groups, group_best=best, renormalise=renormalise)
+        want, ww = plain_route(logits, 4, b, score, groups, top_groups, best, renormalise, 1.0)
+        assert torch.equal(ids.cpu(), want)
+        assert torch.equal(torch.isnan(w.cpu()), torch.isnan(ww))
+        assert torch.isnan(ww).any() and not torch.isnan(ww[6:8]).any()
+        near(w.cpu().nan_to_num(0), ww.nan_to_num(0), 2 * U * ww.nan_to_num(0).abs(), F32)
 
 
 # --- the most workgroups ----------------------------------------------------------------------------------------
