@@ -1,4 +1,4 @@
-"""A layer of experts at its edges: gates far below zero, small values beside large ones, values that are no numbers for every width of a token's lanes, more workgroups than a launch has in one dimension.
+"""A layer of experts at its edges: gates far below zero, small values beside large ones, values that are no numbers for every width of a token's lanes, offsets that no plan makes for the kernels of many rows, more workgroups than a launch has in one dimension.
 
 U = 2^-24, the unit roundoff of fp32; each test derives its bound, set before any of these ran."""
 import math
@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from tests.test_gpu_experts import BF16, F32, INF, U, blobs, case, gen, near, offsets_of, plain_route, product_want
+from tests.test_gpu_experts import BF16, F16, F32, INF, U, blobs, case, gen, near, offsets_of, plain_route, product_want
 
 pytestmark = pytest.mark.gpu
 
@@ -112,6 +112,31 @@ def test_choices_of_values_that_are_no_numbers(qg, experts, groups, top_groups, 
         assert torch.equal(torch.isnan(w.cpu()), torch.isnan(ww))
         assert torch.isnan(ww).any() and not torch.isnan(ww[6:8]).any()
         near(w.cpu().nan_to_num(0), ww.nan_to_num(0), 2 * U * ww.nan_to_num(0).abs(), F32)
+
+
+# --- offsets ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("E,N,K,slots,dt", [(3, 7170, 192, 200, F32), (3, 7170, 192, 140, BF16), (2, 5130, 320, 719, F16), (2, 5130, 1056, 177, BF16), (70, 2600, 64, 4000, BF16), (70, 2600, 64, 5000, F32),
+                                            (9, 130, 64, 40, F32)])
+def test_offsets_that_no_plan_makes(qg, E, N, K, slots, dt):
+    # tiles of 32 and of 64 slots, K in slices, more experts than a wavefront has lanes, few rows
+    case("offsets", E, N, K, slots, dt)
+    group, guard = 64 if K % 64 == 0 else 32, 5
+    one, W = blobs(qg, 1, N, K, 4, group, 12)
+    packed = one.expand(E, one.shape[1]).contiguous()
+    x = torch.randn(slots, K, generator=gen(E)).to(dt)
+    want, slack = product_want(W, x, [0, slots], None, False, group)
+    plan = torch.arange(E + 1) * slots // E
+    far = plan.clone()
+    far[1::3], far[2::3] = 1 << 30, -(1 << 31)
+    for offsets in (plan.flip(0), plan + slots, plan - slots, far, torch.cat([plan[1:], plan[:1]]), torch.full((E + 1,), (1 << 31) - 1), torch.where(torch.arange(E + 1) % 2 == 0, 0, slots)):
+        y = torch.full((slots + 2 * guard, N), 7.0, device="cuda")
+        qg.qg_experts_product(packed, N, K, 4, group, x.cuda(), offsets.int().cuda(), y=y[guard: slots + guard], dtype=F32)
+        y = y.cpu()
+        assert (y[:guard] == 7).all() and (y[-guard:] == 7).all()
+        # all experts have the same matrix: a row that any of them has taken holds its product
+        rows = (y[guard:-guard] != 7).any(1)
+        near(y[guard:-guard][rows], want[rows], slack[rows], F32)
 
 
 # --- the most workgroups ----------------------------------------------------------------------------------------
