@@ -1,4 +1,4 @@
-"""A layer of experts at its edges: gates far below zero, small values beside large ones, values that are no numbers for every width of a token's lanes, offsets that no plan makes for the kernels of many rows, more workgroups than a launch has in one dimension.
+"""A layer of experts at its edges: gates far below zero, small values beside large ones, values that are no numbers for every width of a token's lanes, offsets that no plan makes for the kernels of many rows, more workgroups than a launch has in one dimension, the layer's wiring within what its parts may be off by.
 
 U = 2^-24, the unit roundoff of fp32; each test derives its bound, set before any of these ran."""
 import math
@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from tests.test_gpu_experts import BF16, F16, F32, INF, U, blobs, case, gen, near, offsets_of, plain_route, product_want
+from tests.test_gpu_experts import BF16, F16, F32, INF, U, blobs, case, gen, layer, near, offsets_of, plain_route, product_want
 
 pytestmark = pytest.mark.gpu
 
@@ -155,3 +155,35 @@ def test_more_workgroups_than_a_dimension_has(qg):
         assert bool((got == got[:1]).all())
         want, slack = product_want(W[e: e + 1], x, [0, 3], None, False, group)
         near(got[0].cpu(), want, slack, BF16)
+
+
+# --- together ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens,bits,group", [(1, 4, 32), (13, 3, 64), (150, 2, 64), (40, 4, 16)])
+def test_a_layer_is_off_by_no_more_than_its_parts(qg, tokens, bits, group):
+    # h within the gated product's slack; y within that through |What| and its own product's; each weight 2 U; the sum's k + 2 roundings
+    case("layer parts", tokens, bits, group)
+    E, N, K, k = 9, 192, 256, 3
+    up, Wu = blobs(qg, E, 2 * N, K, bits, group, 1)
+    down, Wd = blobs(qg, E, K, N, bits, group, 2)
+    x, logits = torch.randn(tokens, K, generator=gen(tokens)), 2 * torch.randn(tokens, E, generator=gen(tokens + 1))
+    logits[:, 4] = -INF
+    got = layer(qg, up, down, N, K, bits, group, x.cuda(), logits.cuda(), k).cpu()
+    best, ids = logits.double().topk(k, 1)
+    weights = best.softmax(1)
+    want, slack, size = x.double().clone(), torch.zeros(tokens, K, dtype=torch.float64), x.double().abs()
+    for j in range(k):
+        for e in range(E):
+            t = (ids[:, j] == e).nonzero()[:, 0]
+            if len(t) == 0:
+                continue
+            h, eh = product_want(Wu[e: e + 1], x[t], [0, len(t)], None, True, group)
+            eh = eh + U * (h.abs() + eh) + 2.0 ** -149
+            y, ey = product_want(Wd[e: e + 1], h, [0, len(t)], None, False, group)
+            ey = ey + eh @ Wd[e].abs().t()
+            ey = ey + U * (y.abs() + ey)
+            w = weights[t, j: j + 1]
+            want[t] += w * y
+            slack[t] += w * ey + 2 * U * w * (y.abs() + ey)
+            size[t] += w * (y.abs() + ey)
+    near(got, want, slack + (k + 2) * U * size, F32)
