@@ -22,12 +22,14 @@ RowsSpace rows_space(int64_t x_rows, int64_t K, int x_type)
 // Slots of a workgroup of the kernel of many rows, 64 or 32, or 0: the kernel of few rows.
 //
 // By the rows of an expert, on average: few rows up to 20 operand rows (two of fp32 each); beyond, tiles of 32 slots, three workgroups a compute unit, up to
-// 48 rows (128 of fp32, whose two parts make as much of a weight unpacked).  Each side measured, us: 32 experts' 4096 x 4096 4-bit matrices, groups of 64: 8 rows fp32
-// 81 by few against 96, 12 rows 101 against 99, 16 rows bf16 81 against 82, 24 rows 108 against 104; tiles of 32 against 64, groups of 128: bf16 44 rows 111, 117, 52 rows 124, 121;
-// groups of 32: 44 rows 143, 144, 60 rows 167, 153; fp32, groups of 64: 64 rows 193, 222, 136 rows 358, 366; 512 rows: bf16, 8192 x 4096, groups of 32, 497, 418, fp32 groups of 128 547, 526.
+// 48 rows (128 of fp32, whose two parts make as much of a weight unpacked).  Each side measured, us a call, matrices that no cache holds, random choices (some experts have twice the average):
+// 32 experts' 4096 x 4096 4-bit matrices, groups of 64, few rows against tiles of 32: fp32 8 rows 84, 82, 10 rows 92, 111, 12 rows 108, 116, 16 rows 128, 120; bf16 16 rows 86, 94 (tiles of 64: 76),
+// 20 rows 95, 84 (64: 104), 24 rows 112, 88; tiles of 32 against 64: bf16, groups of 128, 43 rows 109, 117, 51 rows 125, 127, 59 rows 130, 126; groups of 32, 43 rows 139, 149,
+// 51 rows 164, 152; fp32, groups of 64, 98 rows 304, 314, 134 rows 382, 395, 158 rows 430, 449; 8 experts' gated 8192 x 4096, 504 rows: bf16, groups of 32, 495, 404, fp32, groups of 128, 568, 501.
 //
-// And by workgroups: with fewer than one a compute unit tiles of 32, and where those are not 9 to 16 units the wavefronts of few rows, which also divide K.  2 experts, 300 rows, 1000 x 8192:
-// 98 (64), 77 (32), 36 (few); 2, 400 rows, 4096 x 4096: 55, 44, 50; 4, 2000 rows, 400 x 4096: 60, 51, 40; 3, 6000 rows, 1000 x 1024: 36, 37, 63.
+// And by workgroups: with fewer than one a compute unit tiles of 32, and where those are not 9 to 16 units the wavefronts of few rows, which also divide K.  Few rows, tiles of 32 (with K in
+// slices, where many_plan has them so) and of 64, groups of 128, bf16: 2 experts' 148 rows of 1000 x 8192 34, 50, 83; two's 197 of 4096 x 4096 48, 32, 47; four's 492 of 400 x 4096 39, 38, 54 (fp32 57, 43, 74: the slices
+// came after this limit, which fp32 would have lower); three's 1969 of 1000 x 1024 59, 44, 35.
 int many_rows_of(const QgExpertsArgs &a, int parts)
 {
     if (a.group % 32 || a.slots * parts <= (int64_t)20 * a.experts) return 0;
@@ -79,8 +81,8 @@ int few_plan(const QgExpertsArgs &a, int bits, const RowsSpace &s, const QgPrepa
 }
 
 // Workgroups of 32 slots that make less than a round (three a compute unit) take K in three slices, where it has eight steps at least: 130 tokens' three of three 2646 x 7104 3-bit
-// matrices, bf16, 50 us, without 69; 100 tokens' two of four 4096 x 4096 fp32 35, 44.  (Tiles of 64 where those make one to two workgroups a compute unit stay: 1305 tokens' seven
-// of 26 497 x 2432 59, in 32 sliced 70.)
+// matrices, groups of 64, bf16, 50 us, without 69; 100 tokens' two of four 4096 x 4096 fp32 36, 47.  (Tiles of 64 where those make one to two workgroups a compute unit stay: 1305 tokens' seven
+// of 26 497 x 2432 64, in 32 sliced 75.)
 constexpr int MANY_SLICED = 3, MANY_SLICED_K = 1024;
 
 int many_plan(const QgExpertsArgs &a, int bits, int tile_rows, const RowsSpace &s, const QgPrepareArgs &p, hipStream_t st)

@@ -6,7 +6,8 @@
 // in a ring of twice 128 k that no register leaves by a copy (which would wait for it; rings of 1, 2, 3, 4 times: 22.9, 22.5, 23.2, 24.9 us for one token, 57.5, 59.1 for 61 tokens), and into the
 // 16 x 16 x 32 matrix instruction as q - z.  fp32 sums of a group (or 128 k of it) are multiplied by its scale.
 // Measured: 61 tokens' six of 64 2816 x 2048 4-bit matrices in groups of 32, 237 MB: 49 us, 4.8 TB/s (a copy 5.4); one token's two of eight
-// 22016 x 4096, 91 MB: 22 us as a caller sees it; 24 tokens' four of 32 4096 x 1408 3-bit, 80 MB: 22.5 us, of which 3 are the launch and the meeting.
+// 22016 x 4096, 91 MB: 22 us as a caller sees it; 24 tokens' four of 32 4096 x 1408 3-bit, 80 MB: 22.5 us, of which 3 are the launch and the meeting.  (With the same matrices
+// call after call; with matrices in turn that no cache holds 55, 22 and 25 us.)
 //
 // A call with about one row for each expert that it uses does without prepare_rows: its workgroups convert their rows into LDS themselves (SELF), which is a kernel less
 // (one token, two of eight 22016 x 4096 4-bit matrices: 23.5 us against 28.1; four of 32 2816 x 4096: 15.1, 18.4).  With more rows that costs every workgroup more than

@@ -8,7 +8,7 @@
 //
 // Where workgroups are few they have twelve wavefronts, four for each third of K, which add their sums up in LDS at the end (many_plan says when).
 //
-// That prompt now takes 1.50 to 1.57 ms, 0.93 to 0.97 PFLOP/s; a library's product of bf16 matrices reaches 1.20.  Both are held by power (the clock falls to 2.0 GHz; a loop of nothing but
+// That prompt now takes 1.48 to 1.57 ms, 0.93 to 0.98 PFLOP/s, in fp32 2.5; a library's product of bf16 matrices reaches 1.20.  Both are held by power (the clock falls to 2.0 GHz; a loop of nothing but
 // matrix instructions reaches 1.65), here by 9 vector instructions beside each matrix instruction: a loop of just these and no memory makes 1.17 to 1.33.  Codes unpacked once for a
 // whole workgroup by way of LDS make 0.95 to 1.04 in such a loop.  8184 slots of 60 5120 x 1792 2-bit matrices, groups of 64: 209 us (0.71 PFLOP/s; 14 steps of 128 k, 10.5 vector instructions and more in the last tiles).
 #pragma once
@@ -126,7 +126,7 @@ __device__ inline void many_rows(const QgManyArgs &f, const ExpertTile &t, int64
             load(step + 1, next);
         }
         // sixteens of k: operands of X are read AHEAD sixteens before they are multiplied (one where two would not fit into the registers: fp32 with a scale for each 32 k,
-        // 390 slots of three 2646 x 7104 3-bit matrices in slices: 82 us, with two 89), codes unpacked right before
+        // 390 slots of three 2646 x 7104 3-bit matrices, groups of 96, in slices: 82 us, with two 89), codes unpacked right before
         constexpr int KS = 2 * GP, AHEAD = PARTS == 2 && GP == 1 ? 1 : 2;
         HalfOperand xo[8][MB * PARTS];
         auto read = [&](int k) {
